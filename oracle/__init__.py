@@ -112,6 +112,18 @@ def lib():
         _lib.oracle_gelu_tanh.restype = ctypes.c_double
         _lib.oracle_gelu_tanh.argtypes = [ctypes.c_double]
         _lib.oracle_max_threads.restype = ctypes.c_int
+        dbl = ctypes.c_double
+        _lib.oracle_qk_norm_rope.restype = ctypes.c_int
+        _lib.oracle_qk_norm_rope.argtypes = [i64, i32, i32, i32, i32, dbl, i64, i32, vp, i64, vp, vp,
+                                             vp, vp]
+        _lib.oracle_qk_norm_rope_backward.restype = ctypes.c_int
+        _lib.oracle_qk_norm_rope_backward.argtypes = [i64, i32, i32, i32, i32, dbl, i64, i32, vp, i64,
+                                                      vp, vp, vp, vp, i64, vp, vp]
+        _lib.oracle_paged_attention.restype = ctypes.c_int
+        _lib.oracle_paged_attention.argtypes = [vp, vp, vp, i64, i32, dbl, i64, vp, i64, vp, vp, vp,
+                                                vp, i64]
+        _lib.oracle_cache_evict.restype = ctypes.c_int
+        _lib.oracle_cache_evict.argtypes = [i64, i64, vp, vp, vp, vp, i64, vp, vp]
     return _lib
 
 
@@ -422,3 +434,77 @@ def gelu_tanh_grad(x: float) -> float:
 
 def max_threads() -> int:
     return int(lib().oracle_max_threads())
+
+
+# ---- attention ------------------------------------------------------------------------------
+class _Cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("D", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("pos_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("ld_pages", ctypes.c_int64),
+                ("pages", ctypes.c_void_p)]
+
+
+def _f32(x):
+    return np.ascontiguousarray(x, dtype=np.float32)
+
+
+def qk_norm_rope(x, ldx, heads, D, rot_dim, form, w, rot, pos, eps, dtype):
+    """Norm and rotation of every head; unrounded [tokens][heads][D].  ``rot``: [positions][rot_dim]
+    (cosines, sines), ``form`` "halves" or "pairs"."""
+    _check_dtype(x, dtype, "x")
+    pos, w, rot = _as_i64(pos), _f32(w), _f32(rot)
+    ref = np.zeros((len(pos), heads, D))
+    rc = lib().oracle_qk_norm_rope(len(pos), heads, D, rot_dim, form == "pairs", eps, rot.shape[0],
+                                   _DTYPES[dtype], _ptr(x), ldx, _ptr(w), _ptr(rot), _ptr(pos),
+                                   _ptr(ref))
+    if rc != 0:
+        raise ValueError("oracle_qk_norm_rope rejected its arguments")
+    return ref
+
+
+def qk_norm_rope_backward(x, ldx, heads, D, rot_dim, form, w, rot, pos, eps, dtype, g, ldg):
+    """Unrounded (dx [tokens][heads][D], dw [D])."""
+    _check_dtype(x, dtype, "x")
+    _check_dtype(g, dtype, "g")
+    pos, w, rot = _as_i64(pos), _f32(w), _f32(rot)
+    dx, dw = np.zeros((len(pos), heads, D)), np.zeros(D)
+    rc = lib().oracle_qk_norm_rope_backward(len(pos), heads, D, rot_dim, form == "pairs", eps,
+                                            rot.shape[0], _DTYPES[dtype], _ptr(x), ldx, _ptr(w),
+                                            _ptr(rot), _ptr(pos), _ptr(g), ldg, _ptr(dx), _ptr(dw))
+    if rc != 0:
+        raise ValueError("oracle_qk_norm_rope_backward rejected its arguments")
+    return dx, dw
+
+
+def paged_attention(k, v, dtype, D, kv_heads, page_size, n_pages, strides, pages, q, ldq, q_heads,
+                    lens, scale, window=0, totals=None):
+    """Unrounded (out [n][q_heads][D], lse [n][q_heads], totals or None).  ``strides``: (page,
+    position, head) in elements; ``pages``: [n][ld_pages]; ``totals``: [n][ldt] to add to."""
+    for a, what in ((k, "k"), (v, "v"), (q, "q")):
+        _check_dtype(a, dtype, what)
+    pages, lens = _as_i64(pages), _as_i64(lens)
+    c = _Cache(_DTYPES[dtype], D, kv_heads, page_size, n_pages, *strides, pages.shape[1],
+               pages.ctypes.data)
+    n = len(lens)
+    out, lse = np.zeros((n, q_heads, D)), np.zeros((n, q_heads))
+    tot = None if totals is None else np.array(totals, dtype=np.float64)
+    rc = lib().oracle_paged_attention(ctypes.byref(c), _ptr(k), _ptr(v), n, q_heads, scale, window,
+                                      _ptr(q), ldq, _ptr(lens), _ptr(out), _ptr(lse), _ptr(tot),
+                                      0 if tot is None else tot.shape[1])
+    if rc != 0:
+        raise ValueError("oracle_paged_attention rejected its arguments")
+    return out, lse, tot
+
+
+def cache_evict(lens, budget, totals, pos=None, horizon=None):
+    """(new lengths, [n][ldt] old position of what is at each place below the new length)."""
+    lens, totals = _as_i64(lens), _f32(totals)
+    pos = None if pos is None else _as_i64(pos)
+    horizon = None if horizon is None else _as_i64(horizon)
+    new, keep = np.zeros_like(lens), np.full(totals.shape, -1, dtype=np.int64)
+    rc = lib().oracle_cache_evict(len(lens), budget, _ptr(lens), _ptr(totals), _ptr(pos),
+                                  _ptr(horizon), totals.shape[1], _ptr(new), _ptr(keep))
+    if rc != 0:
+        raise ValueError("oracle_cache_evict rejected its arguments")
+    return new, keep

@@ -670,3 +670,165 @@ int oracle_eq_eval(const oracle_eq_node* nodes, int32_t n_nodes, int32_t root, i
     }
   return 0;
 }
+
+/* ---- attention ------------------------------------------------------------------------------- */
+
+/* The two entries of rotated pair i. */
+static void rot_pair(int32_t i, int32_t rot_dim, int32_t pairs, int32_t* a, int32_t* b) {
+  *a = pairs ? 2 * i : i;
+  *b = pairs ? 2 * i + 1 : i + rot_dim / 2;
+}
+
+static double head_rstd(const void* x, int64_t at, int32_t D, int32_t dtype, double eps) {
+  double sum = 0.0;
+  for (int32_t e = 0; e < D; ++e) sum += oracle_widen(x, at + e, dtype) * oracle_widen(x, at + e, dtype);
+  return 1.0 / sqrt(sum / D + eps);
+}
+
+int oracle_qk_norm_rope(int64_t tokens, int32_t heads, int32_t D, int32_t rot_dim, int32_t pairs,
+                        double eps, int64_t n_positions, int32_t dtype, const void* x, int64_t ldx,
+                        const float* w, const float* rot, const int64_t* pos, double* ref64) {
+  if (tokens < 0 || heads < 0 || D <= 0 || rot_dim < 0 || rot_dim > D || rot_dim % 2) return -1;
+  for (int64_t t = 0; t < tokens; ++t)
+    for (int32_t h = 0; h < heads; ++h) {
+      const int64_t at = t * ldx + (int64_t)h * D;
+      double* y = ref64 + (t * heads + h) * D;
+      const int held = pos[t] >= 0 && pos[t] < n_positions;
+      const double r = head_rstd(x, at, D, dtype, eps);
+      for (int32_t e = 0; e < D; ++e) y[e] = held ? oracle_widen(x, at + e, dtype) * r * w[e] : 0.0;
+      for (int32_t i = 0; held && i < rot_dim / 2; ++i) {
+        int32_t a, b;
+        rot_pair(i, rot_dim, pairs, &a, &b);
+        const double c = rot[pos[t] * rot_dim + i], s = rot[pos[t] * rot_dim + rot_dim / 2 + i];
+        const double ya = y[a], yb = y[b];
+        y[a] = ya * c - yb * s;
+        y[b] = yb * c + ya * s;
+      }
+    }
+  return 0;
+}
+
+int oracle_qk_norm_rope_backward(int64_t tokens, int32_t heads, int32_t D, int32_t rot_dim,
+                                 int32_t pairs, double eps, int64_t n_positions, int32_t dtype,
+                                 const void* x, int64_t ldx, const float* w, const float* rot,
+                                 const int64_t* pos, const void* g, int64_t ldg, double* dx,
+                                 double* dw) {
+  if (tokens < 0 || heads < 0 || D <= 0 || rot_dim < 0 || rot_dim > D || rot_dim % 2) return -1;
+  double* u = malloc(sizeof(double) * (size_t)D);
+  if (!u) return -1;
+  for (int32_t e = 0; e < D; ++e) dw[e] = 0.0;
+  for (int64_t t = 0; t < tokens; ++t)
+    for (int32_t h = 0; h < heads; ++h) {
+      const int64_t at = t * ldx + (int64_t)h * D, ga = t * ldg + (int64_t)h * D;
+      double* d = dx + (t * heads + h) * D;
+      if (pos[t] < 0 || pos[t] >= n_positions) {
+        for (int32_t e = 0; e < D; ++e) d[e] = 0.0;
+        continue;
+      }
+      const double r = head_rstd(x, at, D, dtype, eps);
+      for (int32_t e = 0; e < D; ++e) u[e] = oracle_widen(g, ga + e, dtype);
+      for (int32_t i = 0; i < rot_dim / 2; ++i) {   /* turned back */
+        int32_t a, b;
+        rot_pair(i, rot_dim, pairs, &a, &b);
+        const double c = rot[pos[t] * rot_dim + i], s = rot[pos[t] * rot_dim + rot_dim / 2 + i];
+        const double va = u[a], vb = u[b];
+        u[a] = va * c + vb * s;
+        u[b] = vb * c - va * s;
+      }
+      double mean = 0.0;
+      for (int32_t e = 0; e < D; ++e) {
+        const double xn = oracle_widen(x, at + e, dtype) * r;
+        dw[e] += u[e] * xn;
+        u[e] *= w[e];
+        mean += u[e] * xn / D;
+      }
+      for (int32_t e = 0; e < D; ++e) d[e] = r * (u[e] - oracle_widen(x, at + e, dtype) * r * mean);
+    }
+  free(u);
+  return 0;
+}
+
+/* Element offset of head h of position t of sequence b, or -1. */
+static int64_t cache_at(const oracle_cache* c, int64_t b, int64_t t, int32_t h) {
+  const int64_t page = c->pages[b * c->ld_pages + t / c->page_size];
+  if (page < 0 || page >= c->n_pages) return -1;
+  return page * c->page_stride + t % c->page_size * c->pos_stride + (int64_t)h * c->head_stride;
+}
+
+int oracle_paged_attention(const oracle_cache* c, const void* k, const void* v, int64_t n_seqs,
+                           int32_t q_heads, double scale, int64_t window, const void* q, int64_t ldq,
+                           const int64_t* len, double* out, double* lse, double* totals,
+                           int64_t ldt) {
+  if (c->D <= 0 || c->kv_heads <= 0 || q_heads % c->kv_heads) return -1;
+  for (int64_t b = 0; b < n_seqs; ++b)
+    for (int32_t h = 0; h < q_heads; ++h) {
+      const int32_t hk = h / (q_heads / c->kv_heads);
+      const int64_t n = len[b], t0 = window > 0 && n > window ? n - window : 0;
+      double* o = out + (b * q_heads + h) * c->D;
+      for (int32_t e = 0; e < c->D; ++e) o[e] = 0.0;
+      double* s = malloc(sizeof(double) * (size_t)(n + 1));
+      if (!s) return -1;
+      double top = -INFINITY, sum = 0.0;
+      for (int64_t t = t0; t < n; ++t) {
+        const int64_t at = cache_at(c, b, t, hk);
+        s[t] = -INFINITY;
+        if (at < 0) continue;
+        s[t] = 0.0;
+        for (int32_t e = 0; e < c->D; ++e)
+          s[t] += oracle_widen(q, b * ldq + (int64_t)h * c->D + e, c->dtype) *
+                  oracle_widen(k, at + e, c->dtype);
+        s[t] *= scale;
+        if (s[t] > top) top = s[t];
+      }
+      for (int64_t t = t0; t < n; ++t)
+        if (cache_at(c, b, t, hk) >= 0) sum += exp(s[t] - top);
+      lse[b * q_heads + h] = sum > 0.0 ? top + log(sum) : -INFINITY;
+      for (int64_t t = t0; t < n; ++t) {
+        const int64_t at = cache_at(c, b, t, hk);
+        if (at < 0) continue;
+        const double p = exp(s[t] - top) / sum;
+        for (int32_t e = 0; e < c->D; ++e) o[e] += p * oracle_widen(v, at + e, c->dtype);
+        if (totals) totals[b * ldt + t] += p;
+      }
+      free(s);
+    }
+  return 0;
+}
+
+/* Whether total x leaves before total y (a NaN ranks above every number). */
+static int less_total(float x, float y) {
+  if (x != x) return 0;
+  return y != y || x < y;
+}
+
+int oracle_cache_evict(int64_t n_seqs, int64_t budget, const int64_t* len, const float* totals,
+                       const int64_t* pos, const int64_t* horizon, int64_t ldt, int64_t* len_out,
+                       int64_t* keep) {
+  for (int64_t b = 0; b < n_seqs; ++b) {
+    const int64_t n = len[b];
+    const float* w = totals + b * ldt;
+    char* gone = calloc((size_t)n + 1, 1);
+    if (!gone) return -1;
+    int64_t left = n;
+    while (left > budget) {   /* the least candidate, the lowest of equals */
+      int64_t best = -1;
+      for (int64_t t = 0; t < n; ++t) {
+        if (gone[t] || (pos && pos[b * ldt + t] >= horizon[b])) continue;
+        if (best < 0 || less_total(w[t], w[best])) best = t;
+      }
+      if (best < 0) break;
+      gone[best] = 1;
+      --left;
+    }
+    int64_t from = left;
+    for (int64_t t = 0; t < left; ++t) {
+      keep[b * ldt + t] = t;
+      if (!gone[t]) continue;
+      while (gone[from]) ++from;
+      keep[b * ldt + t] = from++;
+    }
+    len_out[b] = left;
+    free(gone);
+  }
+  return 0;
+}

@@ -168,6 +168,42 @@ int oracle_eq_eval(const oracle_eq_node* nodes, int32_t n_nodes, int32_t root, i
                    int32_t n, const oracle_eq_leaf* leaves, int32_t n_leaves, void* out,
                    int64_t ldo, int32_t out_type, double* ref64);
 
+/* Norm and rotation of `heads` heads per token (D entries each, head h of token t at x + t*ldx + h*D):
+ * y = x / sqrt(mean x^2 + eps) * w, then the pairs of y's first rot_dim entries -- (i, i + rot_dim/2),
+ * or (2i, 2i + 1) where pairs != 0 -- become (a c - b s, b c + a s), c and s from row pos[t] of rot
+ * (rot_dim/2 cosines, then rot_dim/2 sines).  A position outside [0, n_positions) gives zeros.
+ * ref64: tokens x heads x D unrounded values. */
+int oracle_qk_norm_rope(int64_t tokens, int32_t heads, int32_t D, int32_t rot_dim, int32_t pairs,
+                        double eps, int64_t n_positions, int32_t dtype, const void* x, int64_t ldx,
+                        const float* w, const float* rot, const int64_t* pos, double* ref64);
+/* The gradients of sum(g * y): dx (tokens x heads x D) and dw (D), by the formulas of the chain
+ * rule. */
+int oracle_qk_norm_rope_backward(int64_t tokens, int32_t heads, int32_t D, int32_t rot_dim,
+                                 int32_t pairs, double eps, int64_t n_positions, int32_t dtype,
+                                 const void* x, int64_t ldx, const float* w, const float* rot,
+                                 const int64_t* pos, const void* g, int64_t ldg, double* dx,
+                                 double* dw);
+
+/* A paged cache: entry e of head h of position t of sequence b at
+ * pages[b*ld_pages + t/page_size]*page_stride + (t%page_size)*pos_stride + h*head_stride + e; a page
+ * outside [0, n_pages) holds nothing. */
+typedef struct {
+  int32_t dtype, D, kv_heads, page_size;
+  int64_t n_pages, page_stride, pos_stride, head_stride, ld_pages;
+  const int64_t* pages;
+} oracle_cache;
+/* Attention of one token per sequence: out (n_seqs x q_heads x D), lse (n_seqs x q_heads) and, where
+ * totals is not NULL, totals[b*ldt + t] += sum over heads of the softmax weight, t < len[b]. */
+int oracle_paged_attention(const oracle_cache* c, const void* k, const void* v, int64_t n_seqs,
+                           int32_t q_heads, double scale, int64_t window, const void* q, int64_t ldq,
+                           const int64_t* len, double* out, double* lse, double* totals, int64_t ldt);
+/* Eviction of sequence positions: keep[b*ldt + i], i < len_out[b], is the old position of what is at
+ * i afterwards (see the rules in the C ABI's header: least total first, ties by position, protected
+ * ones stay, the kept ones behind the new length fill the free places in order). */
+int oracle_cache_evict(int64_t n_seqs, int64_t budget, const int64_t* len, const float* totals,
+                       const int64_t* pos, const int64_t* horizon, int64_t ldt, int64_t* len_out,
+                       int64_t* keep);
+
 /* Helpers the tests pin on their own: exact widening and the round-to-nearest-even narrowing
  * used for every output element. */
 double   oracle_widen(const void* base, int64_t idx, int32_t dtype);

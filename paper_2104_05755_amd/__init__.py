@@ -1,5 +1,6 @@
 """MI355X (gfx950) TPP library: thin Python binding of the C ABI in include/tpp_brgemm.h,
-include/tpp_transform.h, include/tpp_embedding.h and include/tpp_equation.h.
+include/tpp_transform.h, include/tpp_embedding.h, include/tpp_equation.h and
+include/tpp_attention.h.
 
 Argument marshalling only: every step of the computation runs in the HIP kernels of
 ``libtpp_mi355x.so``.  The functions keep the C names; pointers are plain integers (device
@@ -35,6 +36,7 @@ TPP_LAYOUT_A_TRANS, TPP_LAYOUT_B_TRANS = 256, 512
 TPP_RED_SUM, TPP_RED_MUL, TPP_RED_MIN, TPP_RED_MAX = 0, 1, 2, 3
 TPP_RED_BY_COLS, TPP_RED_BY_ROWS, TPP_RED_X, TPP_RED_X2 = 1, 2, 4, 8
 TPP_TR_TRANSPOSE, TPP_TR_VNNI, TPP_TR_VNNI_TO_VNNI_T = 0, 1, 2
+TPP_ROT_HALVES, TPP_ROT_PAIRS = 0, 1
 
 _c_void_p, _i64, _i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
 
@@ -121,6 +123,36 @@ _sig("tpp_reduce_batched", _i32, _i32, _i32, _i64, _i32, _c_void_p, _i64, _i64, 
      ctypes.c_uint32, _c_void_p, _c_void_p, _i64, _c_void_p)
 _sig("tpp_transform_batched", _i32, _i32, _i32, _i32, _i64, _i64, _i32, _i32, _c_void_p, _i64,
      _c_void_p, _i64, _i64, _c_void_p)
+
+
+class tpp_qk_desc(ctypes.Structure):
+    _fields_ = [("head_dim", _i32), ("rot_dim", _i32), ("rot_form", _i32), ("q_heads", _i32),
+                ("k_heads", _i32), ("dtype", _i32), ("eps", ctypes.c_float), ("n_positions", _i64)]
+
+
+class tpp_kv_cache(ctypes.Structure):
+    _fields_ = [("k", _c_void_p), ("v", _c_void_p), ("dtype", _i32), ("head_dim", _i32),
+                ("kv_heads", _i32), ("page_size", _i32), ("n_pages", _i64), ("page_stride", _i64),
+                ("pos_stride", _i64), ("head_stride", _i64)]
+
+
+class tpp_attn_desc(ctypes.Structure):
+    _fields_ = [("q_heads", _i32), ("out_type", _i32), ("scale", ctypes.c_float), ("window", _i64),
+                ("max_len", _i64)]
+
+
+_qkd, _kvc = ctypes.POINTER(tpp_qk_desc), ctypes.POINTER(tpp_kv_cache)
+_sig("tpp_qk_norm_rope", _i32, _qkd, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _c_void_p,
+     _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p, _i64, _c_void_p)
+_sig("tpp_qk_norm_rope_backward", _i32, _qkd, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p,
+     _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p,
+     _i64, _c_void_p, _c_void_p, _c_void_p)
+_sig("tpp_qk_norm_rope_append", _i32, _qkd, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64,
+     _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64, _kvc, _c_void_p, _c_void_p)
+_sig("tpp_paged_attention", _i32, ctypes.POINTER(tpp_attn_desc), _kvc, _i64, _c_void_p, _i64,
+     _c_void_p, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p)
+_sig("tpp_cache_evict", _i32, _kvc, _i64, _i64, _i64, _c_void_p, _c_void_p, _i64, _c_void_p,
+     _c_void_p, _c_void_p, _i64, _c_void_p, _c_void_p, _c_void_p, _c_void_p)
 
 
 def _p(x):
@@ -299,6 +331,44 @@ def tpp_equation_execute(nodes, root, m, n, args, out, ldo, out_type, stream=Non
     ga = b"".join([pack(_p(x) or 0, ld, dt, TPP_BC[bc]) for x, ld, dt, bc in args])
     _check(_lib.tpp_equation_execute(arr, len(nodes), root, m, n, ga or None, len(args), _p(out),
                                      ldo, out_type, stream), "tpp_equation_execute")
+
+
+def tpp_qk_norm_rope(desc, tokens, q, ldq, k, ldk, wq, wk, rot, pos, q_out, ldqo, k_out, ldko,
+                     stream=None):
+    _check(_lib.tpp_qk_norm_rope(desc, tokens, _p(q), ldq, _p(k), ldk, _p(wq), _p(wk), _p(rot),
+                                 _p(pos), _p(q_out), ldqo, _p(k_out), ldko, stream),
+           "tpp_qk_norm_rope")
+
+
+def tpp_qk_norm_rope_backward(desc, tokens, q, ldq, k, ldk, wq, wk, rot, pos, gq, ldgq, gk, ldgk, dq,
+                              lddq, dk, lddk, dwq, dwk, stream=None):
+    _check(_lib.tpp_qk_norm_rope_backward(
+        desc, tokens, _p(q), ldq, _p(k), ldk, _p(wq), _p(wk), _p(rot), _p(pos), _p(gq), ldgq,
+        _p(gk), ldgk, _p(dq), lddq, _p(dk), lddk, _p(dwq), _p(dwk), stream),
+        "tpp_qk_norm_rope_backward")
+
+
+def tpp_qk_norm_rope_append(desc, tokens, q, ldq, k, ldk, v, ldv, wq, wk, rot, pos, q_out, ldqo,
+                            cache, slot, stream=None):
+    """cache: tpp_kv_cache; slot: int64 cache slots (page * page_size + place) of the tokens."""
+    _check(_lib.tpp_qk_norm_rope_append(
+        desc, tokens, _p(q), ldq, _p(k), ldk, _p(v), ldv, _p(wq), _p(wk), _p(rot), _p(pos),
+        _p(q_out), ldqo, cache, _p(slot), stream), "tpp_qk_norm_rope_append")
+
+
+def tpp_paged_attention(desc, cache, n_seqs, q, ldq, lens, pages, ld_pages, out, ldo, lse, totals_in,
+                        totals_out, ldt, stream=None):
+    """desc: tpp_attn_desc, cache: tpp_kv_cache; lse and the totals may be None."""
+    _check(_lib.tpp_paged_attention(desc, cache, n_seqs, _p(q), ldq, _p(lens), _p(pages), ld_pages,
+                                    _p(out), ldo, _p(lse), _p(totals_in), _p(totals_out), ldt,
+                                    stream), "tpp_paged_attention")
+
+
+def tpp_cache_evict(cache, n_seqs, max_len, budget, lens, pages, ld_pages, totals, pos, horizon, ldt,
+                    len_out, totals_out, pos_out, stream=None):
+    _check(_lib.tpp_cache_evict(cache, n_seqs, max_len, budget, _p(lens), _p(pages), ld_pages,
+                                _p(totals), _p(pos), _p(horizon), ldt, _p(len_out), _p(totals_out),
+                                _p(pos_out), stream), "tpp_cache_evict")
 
 
 def tpp_status_string(s: int) -> str:

@@ -15,7 +15,8 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libtpp_mi355x.so")
 OBJDIR = os.path.join(PKG, "_build")
 SOURCES = ["tpp_api.hip", "brgemm_kernels.hip", "brgemm_dl_kernels.hip", "reduce_kernels.hip",
-           "transform_kernels.hip", "embedding_kernels.hip", "equation.hip"]
+           "transform_kernels.hip", "embedding_kernels.hip", "equation.hip", "rope_kernels.hip",
+           "attention_kernels.hip", "cache_kernels.hip"]
 # brgemm_dl_inst.hip is compiled once per part: (object stem, preprocessor definitions)
 DL_PARTS = [("dl_bk32", ["-DDL_BK32"])] + [
     (f"dl_t{t}_a{a}_b{b}", [f"-DDL_TILE={t}", f"-DDL_AT={a}", f"-DDL_BT={b}"])

@@ -6,6 +6,7 @@
 
 #include <string>
 
+#include "tpp_attention.h"
 #include "tpp_brgemm.h"
 #include "tpp_embedding.h"
 #include "tpp_equation.h"
@@ -267,5 +268,75 @@ const char* equation_plan(const tpp_eq_node* nodes, int32_t n_nodes, int32_t roo
 const char* equation_compile(const tpp_eq_node* nodes, int32_t n_nodes, int32_t root,
                              EqProgram& prog, bool* too_many_tmps);
 hipError_t launch_equation(const EqProgram& prog, hipStream_t stream);
+
+// Norms and rotation of query and key heads (rope_kernels.hip).  A side is the heads of the queries or
+// of the keys.
+struct QkSide {
+  const void* x;      // inputs, ldx apart per token
+  const void* g;      // backward: gradients of the outputs
+  void* out;          // outputs (backward: gradients of the inputs); null: the cache
+  const float* w;
+  float* dw;          // backward
+  int64_t ldx, ldg, ldo;
+  int32_t heads;
+};
+struct QkParams {
+  QkSide side[2];     // queries, keys
+  const void* v;      // append: values, ldv apart
+  int64_t ldv;
+  const float* rot;
+  const int64_t* pos;
+  const int64_t* slot;   // append: cache slot of each token (else null)
+  void *kc, *vc;         // the pools, as tpp_kv_cache
+  int64_t n_slots, page_stride, pos_stride, head_stride;
+  FastDiv page;          // page_size
+  int32_t page_size;
+  int64_t tokens, n_positions;
+  int32_t d, rot_dim, pairs, bf16;
+  float eps;
+};
+hipError_t launch_qk(const QkParams& p, hipStream_t stream);
+// Floats of work space of the backward pass, and the pass; without work space (work null) the weights'
+// sums run unsplit.
+int64_t qk_backward_work_floats(const QkParams& p);
+hipError_t launch_qk_backward(const QkParams& p, float* work, hipStream_t stream);
+
+// Attention of one token per sequence over a paged cache (attention_kernels.hip).
+struct AttnParams {
+  const void *q, *k, *v;
+  int64_t ldq, ldo, ldt, ld_pages, n_pages;
+  int64_t page_stride, pos_stride, head_stride;
+  const int64_t* len;
+  const int64_t* pages;
+  void* out;
+  float* lse;
+  const float* totals_in;
+  float* totals_out;
+  int64_t n_seqs, max_len, window;
+  FastDiv page;
+  int32_t page_size, q_heads, kv_heads, d, bf16, out_bf16;
+  float scale;
+};
+int64_t attn_work_floats(const AttnParams& p);
+hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream);
+
+// Eviction from a paged cache (cache_kernels.hip).
+struct EvictParams {
+  void *k, *v;
+  int64_t ld_pages, n_pages, page_stride, pos_stride, head_stride;
+  int32_t page_size, kv_heads, d, es;
+  FastDiv page;
+  int64_t n_seqs, max_len, budget, ldt;
+  const int64_t* len;
+  const int64_t* pages;
+  const float* totals;
+  const int64_t* pos;
+  const int64_t* horizon;
+  int64_t* len_out;
+  float* totals_out;
+  int64_t* pos_out;
+};
+int64_t evict_work_floats(const EvictParams& p);
+hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream);
 
 }  // namespace tpp

@@ -1,8 +1,9 @@
 // tpp_api.hip -- the C ABI of include/tpp_brgemm.h, include/tpp_transform.h,
-// include/tpp_embedding.h and include/tpp_equation.h: argument checks,
+// include/tpp_embedding.h, include/tpp_equation.h and include/tpp_attention.h: argument checks,
 // the dispatch cache, kernel selection and launches.  Host code only; the kernels live in
 // brgemm_kernels.hip, brgemm_dl_kernels.hip, reduce_kernels.hip, transform_kernels.hip,
-// embedding_kernels.hip and equation.hip (which also holds the equation planner).
+// embedding_kernels.hip, equation.hip (which also holds the equation planner), rope_kernels.hip,
+// attention_kernels.hip and cache_kernels.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -180,7 +181,7 @@ int32_t choose_kernel(const tpp_brgemm_kernel_s& h, const tpp::BrgemmParams& p) 
 // a device synchronisation, since queued work may still use the old one), kept until exit.  The
 // caller keeps `hold` (the cache's lock) until its kernels are enqueued, so another host thread
 // cannot free the buffer between the lookup and the launch that uses it.
-enum WorkPurpose { WORK_REDUCE = 0, WORK_SPLIT = 1 };
+enum WorkPurpose { WORK_REDUCE = 0, WORK_SPLIT = 1, WORK_ROPE = 2, WORK_ATTENTION = 3, WORK_EVICT = 4 };
 struct WorkBuffer {
   float* ptr = nullptr;
   int64_t floats = 0;
@@ -265,6 +266,21 @@ float* capture_buffer(void* stream, unsigned long long id, int64_t floats) {
   cb.ptr = static_cast<float*>(ptr);
   cb.floats = size;
   return cb.ptr;
+}
+
+// Work space of `floats` floats for one call on `stream`: the stream's work buffer of that purpose
+// or, under capture, the capture's own.  *out is null where none is needed, and where a capture can
+// have none.
+tpp_status call_work(int purpose, void* stream, int64_t floats, float** out,
+                     std::unique_lock<std::mutex>& hold) {
+  *out = nullptr;
+  if (floats <= 0) return TPP_OK;
+  unsigned long long capture = 0;
+  if (capturing(stream, &capture)) {
+    *out = capture_buffer(stream, capture, floats);
+    return TPP_OK;
+  }
+  return work_buffer(purpose, stream, floats, out, hold);
 }
 
 // What one launch runs: the kernel instance, the split of its stage (or pair) list and the
@@ -975,6 +991,275 @@ tpp_status tpp_transform_batched(int32_t kind, int32_t m, int32_t n, int64_t ld_
                                  void* stream) {
   return transform_impl(kind, m, n, ld_in, ld_out, dtype, alpha, in, in_stride, out, out_stride,
                         G, stream);
+}
+
+}  // extern "C"
+
+// ---- attention (include/tpp_attention.h) --------------------------------------------------------
+
+namespace {
+
+tpp_status check_cache(const tpp_kv_cache* c, int32_t most_dim) {
+  if (!c) return fail(TPP_ERR_INVALID_ARG, "NULL cache");
+  if (!valid_dtype(c->dtype)) return fail(TPP_ERR_INVALID_ARG, "cache: unknown datatype code");
+  if (c->head_dim <= 0 || c->kv_heads <= 0 || c->page_size <= 0 || c->n_pages < 0)
+    return fail(TPP_ERR_INVALID_ARG, "cache: head_dim, kv_heads, page_size must be > 0, n_pages >= 0");
+  if (c->page_stride < 0 || c->pos_stride < 0 || c->head_stride < 0)
+    return fail(TPP_ERR_INVALID_ARG, "cache: strides must be >= 0");
+  if (c->n_pages > 0 && (!c->k || !c->v)) return fail(TPP_ERR_INVALID_ARG, "cache: NULL pool");
+  if (c->n_pages > INT64_MAX / c->page_size)
+    return fail(TPP_ERR_INVALID_ARG, "cache: n_pages * page_size does not fit 64 bits");
+  if (c->head_dim > most_dim)
+    return fail(TPP_ERR_UNSUPPORTED, "cache: head_dim %d is above %d", c->head_dim, most_dim);
+  return TPP_OK;
+}
+
+// The description and the forward inputs of the norm-and-rotation calls; fills p but for outputs.
+tpp_status check_qk(const tpp_qk_desc* d, int64_t tokens, const void* q, int64_t ldq, const void* k,
+                    int64_t ldk, const float* wq, const float* wk, const float* rot,
+                    const int64_t* d_pos, tpp::QkParams& p) {
+  if (!d) return fail(TPP_ERR_INVALID_ARG, "NULL desc");
+  if (tokens < 0) return fail(TPP_ERR_INVALID_ARG, "tokens < 0");
+  if (d->head_dim <= 0 || d->q_heads < 0 || d->k_heads < 0 || d->n_positions < 0)
+    return fail(TPP_ERR_INVALID_ARG, "head_dim must be > 0, heads and n_positions >= 0");
+  if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 2 != 0)
+    return fail(TPP_ERR_INVALID_ARG, "rot_dim must be even and in [0, head_dim]");
+  if (d->rot_form != TPP_ROT_HALVES && d->rot_form != TPP_ROT_PAIRS)
+    return fail(TPP_ERR_INVALID_ARG, "unknown rotation form %d", d->rot_form);
+  if (!valid_dtype(d->dtype)) return fail(TPP_ERR_INVALID_ARG, "unknown datatype code");
+  if (!std::isfinite(d->eps) || d->eps < 0) return fail(TPP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  const int64_t fq = (int64_t)d->q_heads * d->head_dim, fk = (int64_t)d->k_heads * d->head_dim;
+  if (ldq < fq || ldk < fk) return fail(TPP_ERR_INVALID_ARG, "ldq or ldk below heads * head_dim");
+  if (d->head_dim > 512) return fail(TPP_ERR_UNSUPPORTED, "head_dim %d is above 512", d->head_dim);
+  if ((int64_t)d->q_heads + 2 * (int64_t)d->k_heads > (1 << 20))
+    return fail(TPP_ERR_UNSUPPORTED, "more than 2^20 heads");
+  if (tokens > 0) {
+    if (!d_pos || (d->rot_dim > 0 && d->n_positions > 0 && !rot))
+      return fail(TPP_ERR_INVALID_ARG, "NULL positions or rotation table");
+    if ((d->q_heads > 0 && (!q || !wq)) || (d->k_heads > 0 && (!k || !wk)))
+      return fail(TPP_ERR_INVALID_ARG, "NULL queries, keys or norm weights");
+  }
+  p = tpp::QkParams();
+  p.side[0] = {q, nullptr, nullptr, wq, nullptr, ldq, 0, 0, d->q_heads};
+  p.side[1] = {k, nullptr, nullptr, wk, nullptr, ldk, 0, 0, d->k_heads};
+  p.rot = rot;
+  p.pos = d_pos;
+  p.tokens = tokens;
+  p.n_positions = d->n_positions;
+  p.d = d->head_dim;
+  p.rot_dim = d->rot_dim;
+  p.pairs = d->rot_form == TPP_ROT_PAIRS;
+  p.bf16 = d->dtype == TPP_DT_BF16;
+  p.eps = d->eps;
+  return TPP_OK;
+}
+
+// An output (or gradient) of `heads` heads per token.
+tpp_status check_heads(const char* what, const tpp::QkParams& p, int side, const void* ptr, int64_t ld) {
+  if (ld < (int64_t)p.side[side].heads * p.d)
+    return fail(TPP_ERR_INVALID_ARG, "leading dimension of %s below heads * head_dim", what);
+  if (!ptr && p.side[side].heads > 0 && p.tokens > 0) return fail(TPP_ERR_INVALID_ARG, "NULL %s", what);
+  return TPP_OK;
+}
+
+tpp_status launched(const char* what, hipError_t e) {
+  if (e == hipErrorInvalidConfiguration)
+    return fail(TPP_ERR_UNSUPPORTED, "%s needs more than 2^31 - 1 workgroups", what);
+  if (e != hipSuccess) return fail(TPP_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
+  return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+tpp_status tpp_qk_norm_rope(const tpp_qk_desc* desc, int64_t tokens, const void* q, int64_t ldq,
+                            const void* k, int64_t ldk, const float* wq, const float* wk,
+                            const float* rot, const int64_t* d_pos, void* q_out, int64_t ldqo,
+                            void* k_out, int64_t ldko, void* stream) {
+  tpp::QkParams p;
+  if (tpp_status s = check_qk(desc, tokens, q, ldq, k, ldk, wq, wk, rot, d_pos, p)) return s;
+  if (tpp_status s = check_heads("q_out", p, 0, q_out, ldqo)) return s;
+  if (tpp_status s = check_heads("k_out", p, 1, k_out, ldko)) return s;
+  if (tokens == 0) return ok();
+  p.side[0].out = q_out;
+  p.side[0].ldo = ldqo;
+  p.side[1].out = k_out;
+  p.side[1].ldo = ldko;
+  return launched("norm and rotation", tpp::launch_qk(p, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_qk_norm_rope_append(const tpp_qk_desc* desc, int64_t tokens, const void* q, int64_t ldq,
+                                   const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                   const float* wq, const float* wk, const float* rot,
+                                   const int64_t* d_pos, void* q_out, int64_t ldqo,
+                                   const tpp_kv_cache* cache, const int64_t* d_slot, void* stream) {
+  tpp::QkParams p;
+  if (tpp_status s = check_qk(desc, tokens, q, ldq, k, ldk, wq, wk, rot, d_pos, p)) return s;
+  if (tpp_status s = check_heads("q_out", p, 0, q_out, ldqo)) return s;
+  if (tpp_status s = check_heads("v", p, 1, v, ldv)) return s;
+  if (tpp_status s = check_cache(cache, 512)) return s;
+  if (cache->head_dim != desc->head_dim || cache->kv_heads != desc->k_heads ||
+      cache->dtype != desc->dtype)
+    return fail(TPP_ERR_INVALID_ARG, "cache and desc differ in head_dim, key heads or dtype");
+  if (tokens == 0) return ok();
+  if (!d_slot) return fail(TPP_ERR_INVALID_ARG, "NULL slots");
+  p.side[0].out = q_out;
+  p.side[0].ldo = ldqo;
+  p.v = v;
+  p.ldv = ldv;
+  p.slot = d_slot;
+  p.kc = cache->k;
+  p.vc = cache->v;
+  p.n_slots = cache->n_pages * cache->page_size;
+  p.page_stride = cache->page_stride;
+  p.pos_stride = cache->pos_stride;
+  p.head_stride = cache->head_stride;
+  p.page = tpp::FastDiv(cache->page_size);
+  p.page_size = cache->page_size;
+  return launched("norm and rotation", tpp::launch_qk(p, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_qk_norm_rope_backward(const tpp_qk_desc* desc, int64_t tokens, const void* q,
+                                     int64_t ldq, const void* k, int64_t ldk, const float* wq,
+                                     const float* wk, const float* rot, const int64_t* d_pos,
+                                     const void* gq, int64_t ldgq, const void* gk, int64_t ldgk,
+                                     void* dq, int64_t lddq, void* dk, int64_t lddk, float* dwq,
+                                     float* dwk, void* stream) {
+  tpp::QkParams p;
+  if (tpp_status s = check_qk(desc, tokens, q, ldq, k, ldk, wq, wk, rot, d_pos, p)) return s;
+  if (tpp_status s = check_heads("gq", p, 0, gq, ldgq)) return s;
+  if (tpp_status s = check_heads("gk", p, 1, gk, ldgk)) return s;
+  if (tpp_status s = check_heads("dq", p, 0, dq, lddq)) return s;
+  if (tpp_status s = check_heads("dk", p, 1, dk, lddk)) return s;
+  if ((p.side[0].heads > 0 && !dwq) || (p.side[1].heads > 0 && !dwk))
+    return fail(TPP_ERR_INVALID_ARG, "NULL dwq or dwk");
+  p.side[0].g = gq;
+  p.side[0].ldg = ldgq;
+  p.side[0].out = dq;
+  p.side[0].ldo = lddq;
+  p.side[0].dw = dwq;
+  p.side[1].g = gk;
+  p.side[1].ldg = ldgk;
+  p.side[1].out = dk;
+  p.side[1].ldo = lddk;
+  p.side[1].dw = dwk;
+  float* work = nullptr;
+  std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
+  if (tpp_status s = call_work(WORK_ROPE, stream, tpp::qk_backward_work_floats(p), &work, hold)) return s;
+  return launched("norm and rotation", tpp::launch_qk_backward(p, work, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_paged_attention(const tpp_attn_desc* desc, const tpp_kv_cache* cache, int64_t n_seqs,
+                               const void* q, int64_t ldq, const int64_t* d_len,
+                               const int64_t* d_pages, int64_t ld_pages, void* out, int64_t ldo,
+                               float* lse, const float* totals_in, float* totals_out, int64_t ldt,
+                               void* stream) {
+  if (!desc) return fail(TPP_ERR_INVALID_ARG, "NULL desc");
+  if (tpp_status s = check_cache(cache, 256)) return s;
+  if (cache->head_dim < 8) return fail(TPP_ERR_UNSUPPORTED, "head_dim %d is below 8", cache->head_dim);
+  if (n_seqs < 0 || desc->max_len < 0 || desc->window < 0)
+    return fail(TPP_ERR_INVALID_ARG, "n_seqs, max_len and window must be >= 0");
+  if (desc->max_len > (1 << 30)) return fail(TPP_ERR_UNSUPPORTED, "max_len is above 2^30");
+  if (desc->q_heads <= 0 || desc->q_heads % cache->kv_heads != 0)
+    return fail(TPP_ERR_INVALID_ARG, "q_heads must be a positive multiple of kv_heads");
+  if (!valid_dtype(desc->out_type)) return fail(TPP_ERR_INVALID_ARG, "unknown output datatype");
+  if (!std::isfinite(desc->scale)) return fail(TPP_ERR_INVALID_ARG, "scale must be finite");
+  const int64_t f = (int64_t)desc->q_heads * cache->head_dim;
+  if (ldq < f || ldo < f) return fail(TPP_ERR_INVALID_ARG, "ldq or ldo below q_heads * head_dim");
+  if (ld_pages < (desc->max_len + cache->page_size - 1) / cache->page_size)
+    return fail(TPP_ERR_INVALID_ARG, "ld_pages below the pages of max_len positions");
+  if (totals_out && ldt < desc->max_len) return fail(TPP_ERR_INVALID_ARG, "ldt < max_len");
+  if (totals_in && !totals_out) return fail(TPP_ERR_INVALID_ARG, "totals_in without totals_out");
+  if (n_seqs == 0) return ok();
+  if (!q || !out || !d_len || (desc->max_len > 0 && !d_pages))
+    return fail(TPP_ERR_INVALID_ARG, "NULL queries, output, lengths or page table");
+  tpp::AttnParams p = {};
+  p.q = q;
+  p.k = cache->k;
+  p.v = cache->v;
+  p.ldq = ldq;
+  p.ldo = ldo;
+  p.ldt = ldt;
+  p.ld_pages = ld_pages;
+  p.n_pages = cache->n_pages;
+  p.page_stride = cache->page_stride;
+  p.pos_stride = cache->pos_stride;
+  p.head_stride = cache->head_stride;
+  p.len = d_len;
+  p.pages = d_pages;
+  p.out = out;
+  p.lse = lse;
+  p.totals_in = totals_in;
+  p.totals_out = totals_out;
+  p.n_seqs = n_seqs;
+  p.max_len = desc->max_len;
+  p.window = desc->window;
+  p.page = tpp::FastDiv(cache->page_size);
+  p.page_size = cache->page_size;
+  p.q_heads = desc->q_heads;
+  p.kv_heads = cache->kv_heads;
+  p.d = cache->head_dim;
+  p.bf16 = cache->dtype == TPP_DT_BF16;
+  p.out_bf16 = desc->out_type == TPP_DT_BF16;
+  p.scale = desc->scale;
+  float* work = nullptr;
+  std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
+  const int64_t need = tpp::attn_work_floats(p);
+  if (tpp_status s = call_work(WORK_ATTENTION, stream, need, &work, hold)) return s;
+  if (need > 0 && !work && totals_out)
+    return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
+  return launched("attention", tpp::launch_attn(p, work, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_cache_evict(const tpp_kv_cache* cache, int64_t n_seqs, int64_t max_len, int64_t budget,
+                           const int64_t* d_len, const int64_t* d_pages, int64_t ld_pages,
+                           const float* totals, const int64_t* d_pos, const int64_t* d_horizon,
+                           int64_t ldt, int64_t* len_out, float* totals_out, int64_t* pos_out,
+                           void* stream) {
+  if (tpp_status s = check_cache(cache, 512)) return s;
+  if (n_seqs < 0 || max_len < 0 || budget < 0 || max_len > (1 << 30))
+    return fail(TPP_ERR_INVALID_ARG, "n_seqs, max_len and budget must be >= 0, max_len at most 2^30");
+  if (ldt < max_len) return fail(TPP_ERR_INVALID_ARG, "ldt < max_len");
+  if (ld_pages < (max_len + cache->page_size - 1) / cache->page_size)
+    return fail(TPP_ERR_INVALID_ARG, "ld_pages below the pages of max_len positions");
+  if ((d_pos != nullptr) != (d_horizon != nullptr) || (d_pos != nullptr) != (pos_out != nullptr))
+    return fail(TPP_ERR_INVALID_ARG, "d_pos, d_horizon and pos_out are given or NULL together");
+  if (n_seqs == 0) return ok();
+  if (!d_len || !len_out || (max_len > 0 && (!d_pages || !totals || !totals_out)))
+    return fail(TPP_ERR_INVALID_ARG, "NULL lengths, page table or totals");
+  tpp::EvictParams p = {};
+  p.k = cache->k;
+  p.v = cache->v;
+  p.ld_pages = ld_pages;
+  p.n_pages = cache->n_pages;
+  p.page_stride = cache->page_stride;
+  p.pos_stride = cache->pos_stride;
+  p.head_stride = cache->head_stride;
+  p.page_size = cache->page_size;
+  p.kv_heads = cache->kv_heads;
+  p.d = cache->head_dim;
+  p.es = cache->dtype == TPP_DT_BF16 ? 2 : 4;
+  p.page = tpp::FastDiv(cache->page_size);
+  p.n_seqs = n_seqs;
+  p.max_len = max_len;
+  p.budget = budget;
+  p.ldt = ldt;
+  p.len = d_len;
+  p.pages = d_pages;
+  p.totals = totals;
+  p.pos = d_pos;
+  p.horizon = d_horizon;
+  p.len_out = len_out;
+  p.totals_out = totals_out;
+  p.pos_out = pos_out;
+  float* work = nullptr;
+  std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
+  const int64_t need = tpp::evict_work_floats(p);
+  if (tpp_status s = call_work(WORK_EVICT, stream, need, &work, hold)) return s;
+  if (need > 0 && !work)
+    return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
+  return launched("eviction", tpp::launch_evict(p, work, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -134,13 +134,46 @@ def prepare_step(step, dev: dict, device="cuda"):
     return step
 
 
+_ROT = {"halves": tpp.TPP_ROT_HALVES, "pairs": tpp.TPP_ROT_PAIRS}
+
+
+def kv_cache(k: torch.Tensor, v: torch.Tensor, dtype: str) -> tpp.tpp_kv_cache:
+    """The description of two pools [page][place][head][dim] (any strides but the last)."""
+    n, page, heads, dim = k.shape
+    assert k.stride() == v.stride() and k.stride(3) == 1 and k.shape == v.shape
+    return tpp.tpp_kv_cache(k.data_ptr(), v.data_ptr(), _DT[dtype], dim, heads, page, n, k.stride(0),
+                            k.stride(1), k.stride(2))
+
+
 def launch_step(st, dev: dict, stream: Optional[int] = None):
     """One step of a chained workload (see ``workloads.TransformStep``, ``ReduceStep``,
-    ``EmbeddingStep`` and ``EquationStep``)."""
+    ``EmbeddingStep``, ``EquationStep``, ``AppendStep``, ``AttentionStep`` and ``EvictStep``)."""
     if stream is None:
         stream = tpp.current_stream()
     if isinstance(st, DeviceCall):
         launch(st, stream)
+    elif hasattr(st, "rot_form"):   # norms and rotation into the cache
+        x, es = dev[st.qkv].data_ptr(), 2
+        hq, hk, d = st.q_heads, st.k_heads, st.dim
+        ld = (hq + 2 * hk) * d
+        rot = dev[st.rot]
+        desc = tpp.tpp_qk_desc(d, st.rot_dim, _ROT[st.rot_form], hq, hk, tpp.TPP_DT_BF16, st.eps,
+                               rot.shape[0])
+        tpp.tpp_qk_norm_rope_append(desc, st.tokens, x, ld, x + hq * d * es, ld,
+                                    x + (hq + hk) * d * es, ld, dev[st.wq], dev[st.wk], rot,
+                                    dev[st.pos], dev[st.q], hq * d,
+                                    kv_cache(dev[st.kc], dev[st.vc], "bf16"), dev[st.slot], stream)
+    elif hasattr(st, "attn_out"):   # attention
+        totals, pages, f = dev[st.totals], dev[st.pages], st.q_heads * st.dim
+        desc = tpp.tpp_attn_desc(st.q_heads, tpp.TPP_DT_BF16, st.scale, 0, st.max_len)
+        tpp.tpp_paged_attention(desc, kv_cache(dev[st.kc], dev[st.vc], "bf16"), st.seqs, dev[st.q], f,
+                                dev[st.lens], pages, pages.shape[1], dev[st.attn_out], f, None,
+                                totals, totals, totals.shape[1], stream)
+    elif hasattr(st, "budget"):     # eviction
+        totals, pages, pos = dev[st.totals], dev[st.pages], dev[st.cached_pos]
+        tpp.tpp_cache_evict(kv_cache(dev[st.kc], dev[st.vc], "bf16"), st.seqs, st.max_len, st.budget,
+                            dev[st.lens], pages, pages.shape[1], totals, pos, dev[st.horizon],
+                            totals.shape[1], dev[st.lens], totals, pos, stream)
     elif hasattr(st, "nodes"):      # matrix equation
         args = [(dev[name], ld, _DT[dt], bc) for name, ld, dt, bc in st.leaves]
         tpp.tpp_equation_execute(st.nodes, st.root, st.m, st.n, args, dev[st.out], st.ldo,

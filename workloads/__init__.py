@@ -24,6 +24,9 @@ base + r + c*ld, the way Alg. 6 lays out its blocked tensors with the b_m / b_k 
                 pass through both layers (weight transposes, GELU_inv fused into the data
                 gradient, weight gradients batch-reduced over token blocks, bias gradients by the
                 Reduce TPP)
+  decode_step   the attention half of a transformer layer serving one token per sequence: QKV
+                projection, norms and rotation into a paged cache, attention, output projection,
+                eviction
 
 The default sizes are the full sizes; every generator takes smaller sizes for oracle-speed tests.
 """
@@ -162,6 +165,67 @@ class EquationStep:
     out: str
     ldo: int
     out_type: str
+
+
+@dataclass
+class AppendStep:
+    """Norms and rotation of the query and key heads of ``tokens`` packed projections (array ``qkv``:
+    q_heads, k_heads and k_heads value heads of ``dim`` per token), keys and values into the paged
+    cache ``kc`` / ``vc`` ([page][place][head][dim]) at the slots of ``slot``, queries to ``q``."""
+    tokens: int
+    q_heads: int
+    k_heads: int
+    dim: int
+    rot_dim: int
+    rot_form: str
+    eps: float
+    page: int
+    qkv: str = "qkv"
+    q: str = "q"
+    wq: str = "wq"
+    wk: str = "wk"
+    rot: str = "rot"
+    pos: str = "pos"
+    slot: str = "slot"
+    kc: str = "kc"
+    vc: str = "vc"
+
+
+@dataclass
+class AttentionStep:
+    """Attention of one token per sequence over the cache, the weights totalled in ``totals``."""
+    seqs: int
+    q_heads: int
+    k_heads: int
+    dim: int
+    page: int
+    max_len: int
+    scale: float
+    q: str = "q"
+    lens: str = "lens"
+    pages: str = "pages"
+    kc: str = "kc"
+    vc: str = "vc"
+    attn_out: str = "o"
+    totals: str = "totals"
+
+
+@dataclass
+class EvictStep:
+    """Every sequence of the cache cut to ``budget`` positions; all arrays in place."""
+    seqs: int
+    k_heads: int
+    dim: int
+    page: int
+    max_len: int
+    budget: int
+    lens: str = "lens"
+    pages: str = "pages"
+    kc: str = "kc"
+    vc: str = "vc"
+    totals: str = "totals"
+    cached_pos: str = "cached_pos"
+    horizon: str = "horizon"
 
 
 @dataclass
@@ -468,6 +532,58 @@ def softmax(seed: int = 10, keys: int = 512, columns: int = 32768) -> Workload:
     y = EquationStep([("leaf", 0), ("leaf", 1), ("rcp", 1), ("mul", 0, 2)], 3, keys, columns,
                      [("xe", keys, "f32", "none"), ("s", 1, "f32", "row")], "y", keys, "bf16")
     return Workload("softmax", arrays, [], steps=[red_max, e, red_sum, y])
+
+
+def decode_step(seed: int = 11, seqs: int = 16, max_len: int = 512, budget: int = 448,
+                recent: int = 64, hidden: int = 1024, q_heads: int = 16, k_heads: int = 4,
+                page: int = 16, eps: float = 1e-6) -> Workload:
+    """The attention half of a transformer layer that serves one new token per sequence, as a chain:
+      1. BRGEMM: QKV = Wqkv X, the columns of X the sequences' tokens (bf16)
+      2. norms and rotation of the query and key heads; keys and values into the paged cache
+      3. attention over the cache, the softmax weights added to every position's total
+      4. BRGEMM: Y = Wo O
+      5. eviction: sequences longer than ``budget`` lose their positions of least total weight, but
+         none of the ``recent`` latest.
+    The caches hold N(0, 1) entries, lengths are spread up to max_len; positions in the text run on
+    from the cached ones, a few of which are gone already."""
+    rng = np.random.default_rng(seed)
+    dim = hidden // q_heads
+    f_qkv = (q_heads + 2 * k_heads) * dim
+    old = np.linspace(0, max_len - 1, seqs).round().astype(np.int64)   # cached before this step
+    rng.shuffle(old)
+    per = -(-max_len // page)
+    n_pages = seqs * per + 1
+    pages = rng.permutation(n_pages)[:seqs * per].reshape(seqs, per).astype(np.int64)
+    cached_pos = np.cumsum(rng.integers(1, 3, (seqs, max_len)), 1).astype(np.int64)
+    pos = np.array([cached_pos[b, n - 1] + 1 if n else 0 for b, n in enumerate(old)], np.int64)
+    for b, n in enumerate(old):
+        cached_pos[b, n] = pos[b]
+    totals = (rng.random((seqs, max_len)) ** 4 * 4).astype(np.float32)
+    for b, n in enumerate(old):
+        totals[b, n:] = 0
+    slot = np.array([pages[b, n // page] * page + n % page for b, n in enumerate(old)], np.int64)
+    n_pos = 2 * max_len + 1
+    ang = np.arange(n_pos)[:, None] * 10000.0 ** (-np.arange(0, dim, 2) / dim)
+    nan16 = lambda *s: np.full(s, 0x7FC0, np.uint16)
+    arrays = dict(
+        x=bf16_bits(_normal(rng, (seqs, hidden), 1.0)),
+        wqkv=bf16_bits(_normal(rng, (hidden, f_qkv), hidden ** -0.5)),
+        wo=bf16_bits(_normal(rng, (q_heads * dim, hidden), hidden ** -0.5)),
+        qkv=nan16(seqs, f_qkv), q=nan16(seqs, q_heads * dim), o=nan16(seqs, q_heads * dim),
+        y=nan16(seqs, hidden), wq=(1 + _normal(rng, (dim,), 0.1)), wk=(1 + _normal(rng, (dim,), 0.1)),
+        rot=np.concatenate([np.cos(ang), np.sin(ang)], 1).astype(np.float32), pos=pos, slot=slot,
+        kc=bf16_bits(_normal(rng, (n_pages, page, k_heads, dim), 1.0)),
+        vc=bf16_bits(_normal(rng, (n_pages, page, k_heads, dim), 1.0)), pages=pages, lens=old + 1,
+        totals=totals, cached_pos=cached_pos, horizon=pos - recent + 1)
+    one = dict(gm=1, gn=1, a_step_m=0, b_step_n=0, c_step_m=0, c_step_n=0, bias_step_m=0)
+    proj = lambda m, k, a, b, c: Call(m, seqs, k, m, k, m, "bf16", "bf16", 0.0, "stride", m * k,
+                                      k * seqs, set(), G=1, grid=dict(one), count=1, a=a, b=b, c=c)
+    qkv = proj(f_qkv, hidden, "wqkv", "x", "qkv")
+    out = proj(hidden, q_heads * dim, "wo", "o", "y")
+    steps = [qkv, AppendStep(seqs, q_heads, k_heads, dim, dim, "halves", eps, page),
+             AttentionStep(seqs, q_heads, k_heads, dim, page, max_len, dim ** -0.5), out,
+             EvictStep(seqs, k_heads, dim, page, max_len, budget)]
+    return Workload("decode_step", arrays, [qkv, out], steps=steps)
 
 
 CONFIGS = {
