@@ -2,10 +2,31 @@
 // gfx950.
 //
 // Per sequence and query head: scores s_t = scale q . k_t over the positions that are held, their
-// softmax, and the sum of the values with it.  One workgroup per sequence and query head walks the
-// positions 256 at a time, a score per lane, with the running maximum and sum of the softmax: when the
-// maximum grows the sums so far are scaled down, so that every position is read once.
+// softmax, and the sum of the values with it, in one pass with the running maximum m and sum l of the
+// softmax (when m grows, the sums so far are scaled down).  Scores are kept times log2 e, so that the
+// exponential is the hardware's exp2.
+//
+// A workgroup takes one key head of one sequence, up to 16 (or 32) of the query heads that read it, and
+// a span of positions; its four wavefronts take the span's tiles in turn and meet at the end.  Both
+// products are matrix instructions whose operands never leave registers:
+//   S^T = K Q^T   A: keys as they lie in memory (a lane holds consecutive entries of one key), B: queries
+//   O^T = V^T P^T B: the softmax weights where the first product left them (a lane has the weights of one
+//                 query head and of the keys whose values it loads), A: values, turned within a lane.
+// The order of the entries in the first product and of the keys in the second is free, which is what
+// lets both operands of each fit the layouts: no lane exchanges anything but the maximum.
+//   bf16: 32 keys a tile, v_mfma_f32_16x16x32_bf16; a lane loads whole chunks of V of 8 keys and turns
+//         them with byte permutes.  The weights enter as two bf16 parts, hi + lo, since one would cost
+//         an fp32 output 2^-9 of its value; the matrix instructions are far from being the bound.
+//   fp32: 16 keys a tile, v_mfma_f32_16x16x4_f32, whose operands are single entries: nothing to turn.
+// Fewer queries than 16 leave columns of the instructions idle, which costs nothing: a tile of 16 KB
+// (128 entries a head) takes about 600 cycles of a SIMD's matrix unit, and 5000 of its share of HBM.
+//
+// The rows' addresses are looked up once per span and kept in LDS.  A position that is not held gets the
+// address of one that is, and a mark that sets its score to -inf: loads need no branches, and nothing
+// but held positions is ever read.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "brgemm_device.h"
 #include "internal.h"
@@ -15,11 +36,19 @@ namespace {
 
 using namespace dev;
 
-constexpr int AT = 256;
+constexpr int AT = 256;          // threads of a workgroup: 4 wavefronts
+constexpr int AW = AT / 64;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float load_elem(const void* p, int64_t at, bool bf16) {
   return bf16 ? bf16_bits_to_f32(gld<uint16_t>(static_cast<const uint16_t*>(p) + at))
               : gld<float>(static_cast<const float*>(p) + at);
+}
+__device__ __forceinline__ void store_elem(void* p, int64_t at, float v, bool bf16) {
+  if (bf16)
+    gst<uint16_t>(static_cast<uint16_t*>(p) + at, f32_to_bf16_bits(v));
+  else
+    gst<float>(static_cast<float*>(p) + at, v);
 }
 
 // Element offset of position t of sequence b (head 0), or -1 where no page holds it.
@@ -34,96 +63,542 @@ __device__ __forceinline__ int32_t length_of(const AttnParams& p, int64_t b) {
   const int64_t n = gld<int64_t>(p.len + b);
   return (int32_t)(n < 0 ? 0 : n > p.max_len ? p.max_len : n);
 }
-
-__device__ __forceinline__ float score(const AttnParams& p, const float* q, int64_t row) {
-  float s = 0.0f;
-  for (int32_t e = 0; e < p.d; ++e) s += q[e] * load_elem(p.k, row + e, p.bf16);
-  return s * p.scale;
+// First position inside the window.
+__device__ __forceinline__ int32_t window_start(const AttnParams& p, int32_t n) {
+  return p.window > 0 && n > p.window ? (int32_t)(n - p.window) : 0;
 }
 
-__global__ __launch_bounds__(AT) void attn_simple_kernel(AttnParams p, float* lse) {
-  __shared__ float q[256], prob[AT];
-  __shared__ int64_t rows[AT];
-  __shared__ float red[AT];
-  const int tid = threadIdx.x;
-  const int64_t b = blockIdx.x;
-  const int32_t h = blockIdx.y, hk = h / (p.q_heads / p.kv_heads);
+// The maximum, or the sum, over the four groups of 16 lanes.
+__device__ __forceinline__ float groups_max(float v) {
+  auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+__device__ __forceinline__ float groups_sum(float v) {
+  auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+
+// v moved down by d dwords (0 .. 4), zeros behind.
+__device__ __forceinline__ u32x4 shift_dwords(u32x4 v, int32_t d) {
+  if (d & 1) v = (u32x4){v.y, v.z, v.w, 0u};
+  if (d & 2) v = (u32x4){v.z, v.w, 0u, 0u};
+  if (d & 4) v = (u32x4){0u, 0u, 0u, 0u};
+  return v;
+}
+
+// How much sums of maximum m count in sums of maximum top (>= m; both may be -inf, and sums may be NaN).
+__device__ __forceinline__ float share(float m, float top) {
+  return m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+}
+
+constexpr int32_t BLOCK = 1024;   // positions whose addresses are in LDS at a time
+constexpr int JOINED = 4;         // partial results that a lane of the joining kernel has in flight
+constexpr int32_t MEET = 8;       // query heads whose sums are in LDS at a time
+
+// What one launch needs beside AttnParams.
+struct AttnPlan {
+  int32_t span;       // positions of a workgroup
+  int32_t splits;     // spans of a sequence
+  int32_t group;      // query heads of a key head
+  int32_t tiles;      // query-head tiles of a key head
+  FastDiv div_splits, div_tiles, div_y;   // splits, tiles, kv_heads * tiles
+  // Partial results (null: the workgroup writes the outputs): sums [row][split][D], then maxima and
+  // sums of weights [row][split], row = sequence * q_heads + head; scores [row][max_len] for totals.
+  float *o, *m, *l, *s;
+};
+
+// The kernel's shapes by type: keys of a tile, entries of a key step and of a lane's chunk of it.
+template <bool BF16>
+struct Shape {
+  static constexpr int KEYS = BF16 ? 32 : 16;
+  static constexpr int STEP = BF16 ? 32 : 16;
+  static constexpr int CH = BF16 ? 8 : 4;
+  static constexpr int SUB = KEYS / 16;
+  static constexpr int VKEYS = 4 * SUB;     // keys whose values a lane loads
+};
+
+// DP: entries of a head the instance covers (D <= DP); TAIL: D < DP; NT: tiles of 16 query heads.
+template <bool BF16, int DP, bool TAIL, int NT>
+__global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
+  using S = Shape<BF16>;
+  constexpr int ES = BF16 ? 2 : 4;
+  constexpr int KEYS = S::KEYS, CH = S::CH, SUB = S::SUB, VKEYS = S::VKEYS;
+  constexpr int NK = DP / S::STEP;                   // steps of the first product
+  constexpr int VC = BF16 && DP > 64 ? 8 : 4;        // entries of a lane's chunk of a value
+  constexpr int NV = DP / (16 * VC);                 // chunks
+  typedef typename std::conditional<VC * ES == 16, u32x4, u32x2>::type vchunk;
+  typedef typename std::conditional<VC * ES == 16, u32x4_a2, u32x2_a2>::type vchunk_any;
+
+  extern __shared__ __align__(16) char lds[];
+  int64_t* rows = reinterpret_cast<int64_t*>(lds);   // byte offset of each position, bit 0: masked
+  __shared__ int32_t first_held;
+  __shared__ float wave_m[AW][NT * 16], wave_l[AW][NT * 16];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 15, grp = lane >> 4;
+  const int32_t by = fdiv(blockIdx.x, pl.div_splits), split = (int32_t)blockIdx.x - by * pl.splits;
+  const int32_t seq = fdiv(by, pl.div_y), y = by - seq * p.kv_heads * pl.tiles;
+  const int32_t hk = fdiv(y, pl.div_tiles), ht = y - hk * pl.tiles;
+  const int64_t b = seq;
+  const int32_t D = TAIL ? p.d : DP;
   const int32_t n = length_of(p, b);
-  const int64_t lo64 = p.window > 0 && n > p.window ? n - p.window : 0;
-  for (int32_t e = tid; e < p.d; e += AT) q[e] = load_elem(p.q, b * p.ldq + (int64_t)h * p.d + e, p.bf16);
-  float m = -INFINITY, l = 0.0f, o = 0.0f;   // o: entry tid of the output
-  for (int32_t t0 = (int32_t)lo64; t0 < n; t0 += AT) {
+  const int32_t lo = window_start(p, n);
+  const int32_t c0 = lo / KEYS * KEYS + split * pl.span;   // this span: [c0, c1)
+  const int32_t c1 = c0 + pl.span < n ? c0 + pl.span : n;
+  const int32_t nq = pl.group - ht * 16 * NT < 16 * NT ? pl.group - ht * 16 * NT : 16 * NT;
+  const int32_t h0 = hk * pl.group + ht * 16 * NT;          // first query head
+  if (c0 >= n && (pl.o || split > 0)) return;               // (an unsplit launch writes its zeros)
+
+  // ---- queries: the first product's B operand -----------------------------------------------------
+  u32x4 qf[NT][NK];
+  const char* qb = static_cast<const char*>(p.q) + (b * p.ldq + (int64_t)h0 * D) * ES;
+#pragma unroll
+  for (int q = 0; q < NT; ++q)
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      const int32_t h = q * 16 + col, e = s * S::STEP + grp * CH;
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (h < nq && e < D) {
+        const int32_t e0 = TAIL && e > D - CH ? D - CH : e;
+        v = gld<u32x4_a2>(qb + ((int64_t)h * D + e0) * ES);
+        if (TAIL) v = BF16 ? shift_down(v, e - e0) : shift_dwords(v, e - e0);
+      }
+      qf[q][s] = v;
+    }
+
+  const char* kb = static_cast<const char*>(p.k) + hk * p.head_stride * ES;
+  const char* vb = static_cast<const char*>(p.v) + hk * p.head_stride * ES;
+  u32x4 kf[SUB][NK];
+  vchunk vf[VKEYS][NV];
+  const auto load_k = [&](int32_t i0) {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const char* row = kb + (rows[i0 + u * 16 + col] & ~int64_t(1));
+#pragma unroll
+      for (int s = 0; s < NK; ++s) {
+        const int32_t e = s * S::STEP + grp * CH;
+        kf[u][s] = gld<u32x4_a2>(row + (TAIL && e > D - CH ? D - CH : e) * ES);
+      }
+    }
+  };
+  uint32_t masks = 0;   // bit k: key k of this lane is masked
+  const auto load_v = [&](int32_t i0) {
+    masks = 0;
+#pragma unroll
+    for (int k = 0; k < VKEYS; ++k) {
+      const int64_t row = rows[i0 + (k >> 2) * 16 + grp * 4 + (k & 3)];
+      masks |= (uint32_t)(row & 1) << k;
+#pragma unroll
+      for (int c = 0; c < NV; ++c) {
+        const int32_t e = (c * 16 + col) * VC;
+        vf[k][c] = gld<vchunk_any>(vb + (row & ~int64_t(1)) + (TAIL && e > D - VC ? D - VC : e) * ES);
+      }
+    }
+  };
+
+  f32x4 acc[NT][NV * VC];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int q = 0; q < NT; ++q) {
+    m[q] = -INFINITY;
+    l[q] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV * VC; ++j) acc[q][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  const float sl2 = p.scale * LOG2E;
+
+  constexpr int32_t step = AW * KEYS, NONE = 0x7fffffff;
+  for (int32_t t0 = c0; t0 < c1; t0 += BLOCK) {
+    // ---- addresses of the block's rows --------------------------------------------------------------
+    const int32_t cnt = c1 - t0 < BLOCK ? (c1 - t0 + KEYS - 1) / KEYS * KEYS : BLOCK;
+    __syncthreads();   // the block before is done with
+    if (tid == 0) first_held = NONE;
     __syncthreads();
-    const int32_t t = t0 + tid;
-    const int64_t row = t < n ? row_of(p, b, t) : -1;
-    float s = -INFINITY;
-    if (row >= 0) s = score(p, q, row + hk * p.head_stride);
-    rows[tid] = row;
-    red[tid] = s;
+    int32_t mine = NONE;
+    for (int32_t i = tid; i < cnt; i += AT) {
+      const int32_t t = t0 + i;
+      const int64_t row = t >= lo && t < c1 ? row_of(p, b, t) : -1;
+      if (row >= 0 && mine == NONE) mine = i;
+      rows[i] = row < 0 ? -1 : row * ES;
+    }
+    if (mine != NONE) atomicMin(&first_held, mine);
     __syncthreads();
-    float top = m;
-    for (int i = 0; i < AT; ++i) top = fmaxf(top, red[i]);
-    const float base = top == -INFINITY ? 0.0f : top;
-    prob[tid] = row >= 0 ? expf(s - base) : 0.0f;
+    if (first_held == NONE) continue;   // the same for the whole workgroup
+    const int64_t safe = rows[first_held] | 1;
+    for (int32_t i = tid; i < cnt; i += AT)
+      if (rows[i] < 0) rows[i] = safe;
     __syncthreads();
-    const float down = m == -INFINITY ? 0.0f : expf(m - base);
-    l *= down;
-    o *= down;
-    m = top;
-    for (int i = 0; i < AT; ++i) {
-      if (rows[i] < 0) continue;
-      l += prob[i];
-      if (tid < p.d) o += prob[i] * load_elem(p.v, rows[i] + hk * p.head_stride + tid, p.bf16);
+
+    // ---- its tiles ----------------------------------------------------------------------------------
+    int32_t i0 = wave * KEYS;
+    if (i0 < cnt) {
+      load_k(i0);
+      load_v(i0);
+      for (;;) {
+        const int32_t next = i0 + step < cnt ? i0 + step : -1;   // the same for the whole wavefront
+        float sc[NT][VKEYS];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+          f32x4 st[NT];
+#pragma unroll
+          for (int q = 0; q < NT; ++q) st[q] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int s = 0; s < NK; ++s) {
+            u32x4 a = kf[u][s];
+            if constexpr (TAIL) {
+              const int32_t e = s * S::STEP + grp * CH, over = e > D - CH ? e - (D - CH) : 0;
+              a = BF16 ? shift_down(a, over < 8 ? over : 8) : shift_dwords(a, over < 4 ? over : 4);
+            }
+#pragma unroll
+            for (int q = 0; q < NT; ++q) {
+              if constexpr (BF16) {
+                st[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                                __builtin_bit_cast(bf16x8, qf[q][s]),
+                                                                st[q], 0, 0, 0);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  st[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]),
+                                                               __uint_as_float(qf[q][s][e]), st[q], 0, 0, 0);
+              }
+            }
+          }
+#pragma unroll
+          for (int q = 0; q < NT; ++q)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              sc[q][u * 4 + r] = (masks >> (u * 4 + r)) & 1 ? -INFINITY : st[q][r] * sl2;
+        }
+        if (next >= 0) load_k(next);   // behind the products that read the registers
+        __builtin_amdgcn_sched_barrier(0);
+
+        if (pl.s) {   // the scores, for the totals
+#pragma unroll
+          for (int q = 0; q < NT; ++q) {
+            const int32_t h = q * 16 + col;
+            if (h < nq) {
+              float* to = pl.s + (b * p.q_heads + h0 + h) * p.max_len;
+#pragma unroll
+              for (int k = 0; k < VKEYS; ++k) {
+                const int32_t t = t0 + i0 + (k >> 2) * 16 + grp * 4 + (k & 3);
+                if (t < n) gst<float>(to + t, sc[q][k]);
+              }
+            }
+          }
+        }
+        // ---- softmax: the maximum over the tile, the sums so far scaled down to it ------------------
+        u32x4 hi[NT], lw[NT];
+        float pr[NT][VKEYS];
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+          float top = sc[q][0];
+#pragma unroll
+          for (int k = 1; k < VKEYS; ++k) top = fmaxf(top, sc[q][k]);
+          top = fmaxf(m[q], groups_max(top));
+          const float base = top == -INFINITY ? 0.0f : top;
+          const float down = __builtin_amdgcn_exp2f(m[q] - base);
+          m[q] = top;
+          l[q] *= down;
+#pragma unroll
+          for (int k = 0; k < VKEYS; ++k) {
+            pr[q][k] = __builtin_amdgcn_exp2f(sc[q][k] - base);
+            l[q] += pr[q][k];
+          }
+#pragma unroll
+          for (int j = 0; j < NV * VC; ++j) acc[q][j] *= down;
+          if constexpr (BF16) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float a = pr[q][2 * k], c = pr[q][2 * k + 1];
+              const uint32_t h = pack_bf16x2(a, c);
+              hi[q][k] = h;
+              lw[q][k] = pack_bf16x2(a - __uint_as_float(h << 16), c - __uint_as_float(h & 0xffff0000u));
+            }
+          }
+        }
+        // ---- the values -----------------------------------------------------------------------------
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          if constexpr (BF16) {
+#pragma unroll
+            for (int j = 0; j < VC; ++j) {
+              // entry j of the chunks of 8 keys, two keys a dword
+              u32x4 a;
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                a[k] = __builtin_amdgcn_perm(vf[2 * k + 1][c][j / 2], vf[2 * k][c][j / 2],
+                                             j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+              for (int q = 0; q < NT; ++q) {
+                f32x4& o = acc[q][c * VC + j];
+                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                            __builtin_bit_cast(bf16x8, hi[q]), o, 0, 0, 0);
+                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                            __builtin_bit_cast(bf16x8, lw[q]), o, 0, 0, 0);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < VC; ++j)
+#pragma unroll
+              for (int k = 0; k < VKEYS; ++k)
+#pragma unroll
+                for (int q = 0; q < NT; ++q)
+                  acc[q][c * VC + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                      __uint_as_float(vf[k][c][j]), pr[q][k], acc[q][c * VC + j], 0, 0, 0);
+          }
+        }
+        if (next < 0) break;
+        load_v(next);
+        __builtin_amdgcn_sched_barrier(0);
+        i0 = next;
+      }
     }
   }
-  if (tid < p.d) {
-    const float v = l > 0.0f || l != l ? o / l : 0.0f;
-    const int64_t at = b * p.ldo + (int64_t)h * p.d + tid;
-    if (p.out_bf16)
-      gst<uint16_t>(static_cast<uint16_t*>(p.out) + at, f32_to_bf16_bits(v));
-    else
-      gst<float>(static_cast<float*>(p.out) + at, v);
+
+  // ---- the wavefronts meet ------------------------------------------------------------------------
+#pragma unroll
+  for (int q = 0; q < NT; ++q) {
+    l[q] = groups_sum(l[q]);
+    if (grp == 0) {
+      wave_m[wave][q * 16 + col] = m[q];
+      wave_l[wave][q * 16 + col] = l[q];
+    }
   }
-  if (tid == 0) {
-    const float z = l == 0.0f ? -INFINITY : m + logf(l);
-    if (p.lse) gst<float>(p.lse + b * p.q_heads + h, z);
-    if (lse) gst<float>(lse + b * p.q_heads + h, z);
+  float* part = reinterpret_cast<float*>(lds);   // [wavefront][query of the pass][D]
+  for (int32_t g0 = 0; g0 < nq; g0 += MEET) {
+    const int32_t ng = nq - g0 < MEET ? nq - g0 : MEET;
+    __syncthreads();   // the rows' addresses, or the pass before, are done with
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+      const int32_t h = q * 16 + col - g0;
+      if (h < 0 || h >= ng) continue;
+      float top = wave_m[0][g0 + h];
+#pragma unroll
+      for (int w = 1; w < AW; ++w) top = fmaxf(top, wave_m[w][g0 + h]);
+      const float down = share(m[q], top);
+#pragma unroll
+      for (int c = 0; c < NV; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int32_t e = (c * 16 + grp * 4 + r) * VC;
+          float* to = part + (wave * ng + h) * D + (TAIL && e > D - VC ? D - VC : e);
+#pragma unroll
+          for (int j = 0; j < VC; ++j) to[j] = acc[q][c * VC + j][r] * down;
+        }
+    }
+    __syncthreads();
+    for (int32_t i = tid; i < ng * D; i += AT) {
+      const int32_t hp = i / D, h = g0 + hp, e = i - hp * D;
+      float top = wave_m[0][h];
+#pragma unroll
+      for (int w = 1; w < AW; ++w) top = fmaxf(top, wave_m[w][h]);
+      float sum = 0.0f, o = 0.0f;
+#pragma unroll
+      for (int w = 0; w < AW; ++w) {
+        sum += wave_l[w][h] * share(wave_m[w][h], top);
+        o += part[w * ng * D + i];
+      }
+      const int64_t row = b * p.q_heads + h0 + h;
+      if (pl.o) {
+        const int64_t at = row * pl.splits + split;
+        gst<float>(pl.o + at * D + e, o);
+        if (e == 0) {
+          gst<float>(pl.m + at, top);
+          gst<float>(pl.l + at, sum);
+        }
+      } else {
+        store_elem(p.out, b * p.ldo + (int64_t)(h0 + h) * D + e, sum == 0.0f ? 0.0f : o / sum, p.out_bf16);
+        if (e == 0 && p.lse)
+          gst<float>(p.lse + row, sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2);
+      }
+    }
   }
 }
 
-__global__ __launch_bounds__(AT) void attn_totals_kernel(AttnParams p, const float* lse) {
-  __shared__ float q[256];
-  const int tid = threadIdx.x;
-  const int64_t b = blockIdx.x;
-  const int32_t n = length_of(p, b), t = blockIdx.y * AT + tid;
-  const int64_t row = t < n && (p.window == 0 || t >= n - p.window) ? row_of(p, b, t) : -1;
-  float sum = 0.0f;
-  for (int32_t h = 0; h < p.q_heads; ++h) {
+// The spans' partial results joined: the first `rows` workgroups a (sequence, query head) each, whose
+// wavefronts take the spans in turn; the others, with totals, 256 positions of a sequence each.
+// NE: entries of a lane.
+template <int NE>
+__global__ __launch_bounds__(AT) void attn_join_kernel(AttnParams p, AttnPlan pl, int32_t rows,
+                                                       int32_t blocks, int32_t keys) {
+  __shared__ float lse[AT];
+  __shared__ float part[AW][NE * 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if ((int32_t)blockIdx.x < rows) {
+    const int64_t row = blockIdx.x;
+    const int32_t b = (int32_t)row / p.q_heads, h = (int32_t)row - b * p.q_heads;
+    const int32_t n = length_of(p, b), lo = window_start(p, n) / keys * keys;
+    const int32_t used = n > lo ? (n - lo + pl.span - 1) / pl.span : 0;
+    const float* mm = pl.m + row * pl.splits;
+    const float* ll = pl.l + row * pl.splits;
+    float top = -INFINITY;
+    for (int32_t s = lane; s < used; s += 64) top = fmaxf(top, gld<float>(mm + s));
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    float sum = 0.0f, o[NE];
+#pragma unroll
+    for (int i = 0; i < NE; ++i) o[i] = 0.0f;
+    for (int32_t s0 = 0; s0 < used; s0 += 64) {
+      const float f = s0 + lane < used ? share(gld<float>(mm + s0 + lane), top) : 0.0f;
+      if (s0 + lane < used) sum += gld<float>(ll + s0 + lane) * f;
+      const int32_t end = used - s0 < 64 ? used - s0 : 64;
+      for (int32_t s = wave; s < end; s += JOINED * AW) {   // JOINED spans' rows in flight
+        float x[JOINED][NE];
+#pragma unroll
+        for (int u = 0; u < JOINED; ++u)
+#pragma unroll
+          for (int i = 0; i < NE; ++i)
+            x[u][i] = s + u * AW < end && lane + 64 * i < p.d
+                          ? gld<float>(pl.o + (row * pl.splits + s0 + s + u * AW) * p.d + lane + 64 * i)
+                          : 0.0f;
+#pragma unroll
+        for (int u = 0; u < JOINED; ++u) {
+          const float fs = __shfl(f, (s + u * AW) & 63, 64);   // 0 past the last span
+#pragma unroll
+          for (int i = 0; i < NE; ++i) o[i] += x[u][i] * fs;
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+#pragma unroll
+    for (int i = 0; i < NE; ++i) part[wave][lane + 64 * i] = o[i];
     __syncthreads();
-    for (int32_t e = tid; e < p.d; e += AT)
-      q[e] = load_elem(p.q, b * p.ldq + (int64_t)h * p.d + e, p.bf16);
+    if (tid < p.d) {
+      const float v = ((part[0][tid] + part[1][tid]) + part[2][tid]) + part[3][tid];
+      store_elem(p.out, b * p.ldo + (int64_t)h * p.d + tid, sum == 0.0f ? 0.0f : v / sum, p.out_bf16);
+    }
+    if (tid == 0 && p.lse)
+      gst<float>(p.lse + row, sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2);
+    return;
+  }
+  // ---- totals: every weight from its score --------------------------------------------------------
+  const int32_t w = (int32_t)blockIdx.x - rows;
+  const int64_t b = w / blocks;
+  const int32_t n = length_of(p, b), start = window_start(p, n), lo = start / keys * keys;
+  const int32_t t = (w - (int32_t)b * blocks) * AT + tid;
+  if (t - tid >= n) return;
+  const int32_t used = n > lo ? (n - lo + pl.span - 1) / pl.span : 0;
+  const bool held = t < n && t >= start && row_of(p, b, t) >= 0;
+  float total = 0.0f;
+  for (int32_t hb = 0; hb < p.q_heads; hb += AT) {
     __syncthreads();
-    if (row >= 0)
-      sum += expf(score(p, q, row + h / (p.q_heads / p.kv_heads) * p.head_stride) -
-                  gld<float>(lse + b * p.q_heads + h));
+    if (hb + tid < p.q_heads) {
+      const int64_t at = (b * p.q_heads + hb + tid) * pl.splits;
+      float top = -INFINITY, sum = 0.0f;
+      for (int32_t s = 0; s < used; ++s) {
+        const float v = gld<float>(pl.m + at + s), x = gld<float>(pl.l + at + s);
+        const float up = fmaxf(top, v);
+        sum = sum * share(top, up) + x * share(v, up);
+        top = up;
+      }
+      lse[tid] = top + __builtin_amdgcn_logf(sum);
+    }
+    __syncthreads();
+    const int32_t heads = p.q_heads - hb < AT ? p.q_heads - hb : AT;
+    if (held)
+      for (int32_t h = 0; h < heads; ++h) {
+        const float s = gld<float>(pl.s + (b * p.q_heads + hb + h) * p.max_len + t);
+        total += __builtin_amdgcn_exp2f(s - lse[h]);
+      }
   }
   if (t < n) {
     const int64_t at = b * p.ldt + t;
-    gst<float>(p.totals_out + at, (p.totals_in ? gld<float>(p.totals_in + at) : 0.0f) + sum);
+    gst<float>(p.totals_out + at, (p.totals_in ? gld<float>(p.totals_in + at) : 0.0f) + total);
   }
+}
+
+// Tiles of 16 query heads per workgroup: two read the keys and values once for twice the heads, and have
+// the registers for it up to 128 entries a head.
+int32_t head_tiles(const AttnParams& p) { return p.q_heads / p.kv_heads > 16 && p.d <= 128 ? 2 : 1; }
+
+// Spans of at most a block where that gives the 256 compute units four workgroups each, down to one tile
+// per wavefront; `split` false: the whole sequence.
+AttnPlan plan(const AttnParams& p, bool split) {
+  AttnPlan pl = {};
+  pl.group = p.q_heads / p.kv_heads;
+  const int32_t nt = head_tiles(p);
+  pl.tiles = (pl.group + 16 * nt - 1) / (16 * nt);
+  const int32_t keys = p.bf16 ? 32 : 16, step = AW * keys;
+  // positions of a sequence that can count, from a tile's first one on
+  const int64_t range = p.window > 0 && p.window < p.max_len ? p.window + keys : p.max_len;
+  const int64_t units = p.n_seqs * p.kv_heads * pl.tiles;
+  int64_t span = (range * units / 1024 + step - 1) / step * step;
+  if (span < step) span = step;
+  if (span > BLOCK) span = BLOCK;
+  if (!split) span = range < step ? step : (range + step - 1) / step * step;
+  pl.span = (int32_t)span;
+  pl.splits = range > span ? (int32_t)((range + span - 1) / span) : 1;
+  pl.div_splits = FastDiv(pl.splits);
+  pl.div_tiles = FastDiv(pl.tiles);
+  pl.div_y = FastDiv((int64_t)p.kv_heads * pl.tiles);
+  return pl;
+}
+
+template <bool BF16, int DP, int NT>
+void launch_tail(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t bytes, hipStream_t stream) {
+  if (p.d < DP)
+    hipLaunchKernelGGL((attn_kernel<BF16, DP, true, NT>), grid, dim3(AT), bytes, stream, p, pl);
+  else
+    hipLaunchKernelGGL((attn_kernel<BF16, DP, false, NT>), grid, dim3(AT), bytes, stream, p, pl);
+}
+
+template <bool BF16, int NT>
+void launch_dim(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t bytes, hipStream_t stream) {
+  if (p.d <= 64) launch_tail<BF16, 64, NT>(p, pl, grid, bytes, stream);
+  else if (NT == 2 || p.d <= 128) launch_tail<BF16, 128, NT>(p, pl, grid, bytes, stream);
+  else launch_tail<BF16, 256, 1>(p, pl, grid, bytes, stream);
 }
 
 }  // namespace
 
-int64_t attn_work_floats(const AttnParams& p) { return p.totals_out ? p.n_seqs * p.q_heads : 0; }
+int64_t attn_work_floats(const AttnParams& p) {
+  const AttnPlan pl = plan(p, true);
+  if (pl.splits == 1 && !p.totals_out) return 0;
+  const int64_t rows = p.n_seqs * p.q_heads;
+  return rows * pl.splits * (p.d + 2) + (p.totals_out ? rows * p.max_len : 0);
+}
 
 hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
-  if (p.n_seqs > 0x7fffffff || p.q_heads > 65535) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(attn_simple_kernel, dim3((uint32_t)p.n_seqs, p.q_heads), dim3(AT), 0, stream, p,
-                     work);
-  if (p.totals_out && p.max_len > 0)
-    hipLaunchKernelGGL(attn_totals_kernel, dim3((uint32_t)p.n_seqs, (uint32_t)((p.max_len + AT - 1) / AT)),
-                       dim3(AT), 0, stream, p, work);
+  AttnPlan pl = plan(p, work != nullptr);
+  const int64_t rows = p.n_seqs * p.q_heads;
+  const int64_t blocks = work && p.totals_out ? (p.max_len + AT - 1) / AT : 0;
+  const int64_t wgs = (int64_t)pl.splits * p.kv_heads * pl.tiles * p.n_seqs;
+  const int64_t joins = rows + blocks * p.n_seqs;
+  if (p.n_seqs > 0x7fffffff || wgs > 0x7fffffff || joins > 0x7fffffff)
+    return hipErrorInvalidConfiguration;
+  if (work) {
+    pl.o = work;
+    pl.m = pl.o + rows * pl.splits * p.d;
+    pl.l = pl.m + rows * pl.splits;
+    pl.s = p.totals_out ? pl.l + rows * pl.splits : nullptr;
+  }
+  const int32_t nt = head_tiles(p), meet = pl.group < MEET ? pl.group : MEET;
+  const size_t addr = (size_t)(pl.span < BLOCK ? pl.span : BLOCK) * 8, part = (size_t)AW * meet * p.d * 4;
+  const size_t bytes = addr > part ? addr : part;
+  const dim3 grid((uint32_t)wgs);
+  if (p.bf16)
+    nt == 1 ? launch_dim<true, 1>(p, pl, grid, bytes, stream)
+            : launch_dim<true, 2>(p, pl, grid, bytes, stream);
+  else
+    nt == 1 ? launch_dim<false, 1>(p, pl, grid, bytes, stream)
+            : launch_dim<false, 2>(p, pl, grid, bytes, stream);
+  if (work) {
+    const dim3 jgrid((uint32_t)joins);
+    const int32_t keys = p.bf16 ? 32 : 16;
+#define TPP_JOIN(NE)                                                                              \
+  hipLaunchKernelGGL((attn_join_kernel<NE>), jgrid, dim3(AT), 0, stream, p, pl, (int32_t)rows,    \
+                     (int32_t)blocks, keys)
+    if (p.d <= 64) TPP_JOIN(1);
+    else if (p.d <= 128) TPP_JOIN(2);
+    else TPP_JOIN(4);
+#undef TPP_JOIN
+  }
   return hipGetLastError();
 }
 
