@@ -4,10 +4,13 @@
 // A row is one head of one token: y = x r w with r = 1 / sqrt(mean(x^2) + eps), then the pairs of its
 // first rot_dim entries turned by the token's angles.  Both are linear in y, so a row needs one sum
 // over its entries and one pass; the backward pass turns the gradient back (the rotation's transpose),
-// u = g w, and needs one more sum, of u xn.
+// u = g w, and needs one more sum, of u xn.  8 (16) operations per entry of 2 or 4 bytes: bound by HBM.
 //
-// One wavefront per row: a unit is a rotated pair or an entry behind the rotated part, lane l has the
-// units l, l + 64, ...
+// Rows of whole 16-byte chunks: a lane has two chunks of a row, placed so that what the rotation turns
+// together is in one lane -- chunks at i and i + rot_dim / 2 in the halves form (behind the rotated part
+// at i and half of the rest on), any two in the pairs form -- and the sums fold over the 4 to 64 lanes
+// of the row by register permutes.  A wavefront has 64 / lanes rows.  Other rows: one per wavefront, a
+// rotated pair or an entry behind the rotated part to a lane, four rows in flight.
 #include <hip/hip_runtime.h>
 
 #include "brgemm_device.h"
@@ -19,6 +22,7 @@ namespace {
 using namespace dev;
 
 constexpr int QT = 256;   // threads per workgroup: 4 wavefronts
+constexpr int QW = QT / 64;
 
 __device__ __forceinline__ float load_elem(const void* p, int64_t at, bool bf16) {
   return bf16 ? bf16_bits_to_f32(gld<uint16_t>(static_cast<const uint16_t*>(p) + at))
@@ -31,11 +35,333 @@ __device__ __forceinline__ void store_elem(void* p, int64_t at, float v, bool bf
     gst<float>(static_cast<float*>(p) + at, v);
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int h = 32; h > 0; h >>= 1) v += __shfl_xor(v, h, 64);
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// The sum over groups of LANES (4 .. 64) consecutive lanes, in every one of them.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += dpp<0xB1>(v);                           // lane ^ 1
+  v += dpp<0x4E>(v);                           // lane ^ 2
+  if constexpr (LANES >= 8) v += dpp<0x141>(v);    // the other quad of 8
+  if constexpr (LANES >= 16) v += dpp<0x140>(v);   // the other 8 of 16
+  if constexpr (LANES >= 32) {
+    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  }
+  if constexpr (LANES >= 64) {
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  }
   return v;
 }
+
+// First element of head `head` of cache slot `slot` (inside the pools).
+__device__ __forceinline__ int64_t slot_base(const QkParams& p, int64_t slot, int32_t head) {
+  const int64_t page = p.n_slots <= 0x7fffffff ? (int64_t)fdiv((uint32_t)slot, p.page)
+                                               : slot / p.page_size;
+  return page * p.page_stride + (slot - page * p.page_size) * p.pos_stride + head * p.head_stride;
+}
+
+// Both sides are read before the choice (a lane's own choice of a kernel argument's address would put
+// the arguments into scratch memory).
+template <typename T>
+__device__ __forceinline__ T pick(bool c, T a, T b) {
+  return c ? a : b;
+}
+
+// A row of the forward pass: where it comes from and goes to.
+struct Row {
+  const void* x;
+  void* out;            // null: not written
+  const float* w;       // null: a value, copied
+  int64_t from, to;     // elements
+  int64_t pos;          // -1: padding
+};
+__device__ __forceinline__ Row row_at(const QkParams& p, int32_t row, int32_t per_token,
+                                      const FastDiv& div) {
+  Row r;
+  const int64_t t = fdiv((uint32_t)row, div);
+  int32_t head = row - (int32_t)t * per_token;
+  const int64_t pos = gld<int64_t>(p.pos + t);
+  r.pos = pos >= 0 && pos < p.n_positions ? pos : -1;
+  const bool q = head < p.side[0].heads;
+  if (!q) head -= p.side[0].heads;
+  const bool v = !q && head >= p.side[1].heads;
+  if (v) head -= p.side[1].heads;
+  r.x = pick(q, p.side[0].x, pick(v, p.v, p.side[1].x));
+  r.w = pick<const float*>(q, p.side[0].w, pick<const float*>(v, nullptr, p.side[1].w));
+  r.from = t * pick(q, p.side[0].ldx, pick(v, p.ldv, p.side[1].ldx)) + (int64_t)head * p.d;
+  r.out = pick(q, p.side[0].out, p.side[1].out);
+  r.to = t * pick(q, p.side[0].ldo, p.side[1].ldo) + (int64_t)head * p.d;
+  if (!q && p.slot) {
+    const int64_t slot = gld<int64_t>(p.slot + t);
+    const bool held = r.pos >= 0 && slot >= 0 && slot < p.n_slots;
+    r.out = pick<void*>(held, pick(v, p.vc, p.kc), nullptr);
+    if (held) r.to = slot_base(p, slot, head);
+  }
+  return r;
+}
+
+// ---- rows of whole chunks -----------------------------------------------------------------------
+// V entries of a 16-byte chunk.
+template <bool BF16>
+struct Chunk {
+  static constexpr int V = BF16 ? 8 : 4;
+  static constexpr int ES = BF16 ? 2 : 4;
+};
+template <bool BF16>
+__device__ __forceinline__ u32x4 load_chunk(const void* p, int64_t at) {
+  return gld<u32x4_a2>(static_cast<const char*>(p) + at * Chunk<BF16>::ES);
+}
+template <bool BF16>
+__device__ __forceinline__ void widen(u32x4 w, float (&x)[Chunk<BF16>::V]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (BF16) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    } else {
+      x[e] = __uint_as_float(w[e]);
+    }
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ void store_chunk(void* p, int64_t at, const float (&v)[Chunk<BF16>::V]) {
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (BF16) w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+    else w[e] = __float_as_uint(v[e]);
+  }
+  gst<u32x4_a2>(static_cast<char*>(p) + at * Chunk<BF16>::ES, w);
+}
+template <int V>
+__device__ __forceinline__ void load_floats(const float* p, float (&v)[V]) {
+#pragma unroll
+  for (int g = 0; g < V / 4; ++g) {
+    const f32x4 w = gld<f32x4_a4>(p + 4 * g);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[4 * g + e] = w[e];
+  }
+}
+
+// The first entries a, b of the two chunks of lane c of a row, and whether they are turned (halves).
+__device__ __forceinline__ bool chunks_of(const QkParams& p, int32_t i, int32_t& a, int32_t& b) {
+  if (p.pairs) {
+    a = i;
+    b = p.d / 2 + i;
+    return false;
+  }
+  const int32_t half = p.rot_dim / 2;
+  if (i < half) {
+    a = i;
+    b = half + i;
+    return true;
+  }
+  a = half + i;
+  b = p.rot_dim + (p.d - p.rot_dim) / 2 + (i - half);
+  return false;
+}
+
+// Cosines and sines of the pairs of a lane's chunks: halves: entry e of both chunks; pairs: pair e / 2
+// of chunk A at e / 2, of chunk B at V / 2 + e / 2.  What is not turned (behind the rotated part, or of a
+// padding token: pos < 0) has cosine 1, sine 0, and reads nothing.
+template <int V>
+__device__ __forceinline__ void load_angles(const QkParams& p, int64_t pos, int32_t a, int32_t b,
+                                            bool turned, float (&c)[V], float (&s)[V]) {
+  const int32_t half = p.rot_dim / 2;
+  const float* row = p.rot + pos * p.rot_dim;
+  if (!p.pairs) {
+    if (turned && pos >= 0) {
+      load_floats<V>(row + a, c);
+      load_floats<V>(row + half + a, s);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        c[e] = 1.0f;
+        s[e] = 0.0f;
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const int32_t i = e < V / 2 ? a / 2 + e : b / 2 + e - V / 2;
+    const bool in = i < half && pos >= 0;
+    c[e] = in ? gld<float>(row + i) : 1.0f;
+    s[e] = in ? gld<float>(row + half + i) : 0.0f;
+  }
+}
+// The rotation of a lane's two chunks (the other way where back).
+template <int V>
+__device__ __forceinline__ void turn(bool pairs, bool back, const float (&c)[V], const float (&s)[V],
+                                     float (&x)[V], float (&y)[V]) {
+  const auto one = [&](float& a, float& b, float co, float si) {
+    if (back) si = -si;
+    const float t = a * co - b * si;
+    b = b * co + a * si;
+    a = t;
+  };
+  if (!pairs) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) one(x[e], y[e], c[e], s[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V / 2; ++e) {
+      one(x[2 * e], x[2 * e + 1], c[e], s[e]);
+      one(y[2 * e], y[2 * e + 1], c[V / 2 + e], s[V / 2 + e]);
+    }
+  }
+}
+
+// Whether the rows are whole chunks whose pairs meet in a lane.
+bool chunked(const QkParams& p) {
+  const int32_t two = p.bf16 ? 16 : 8;
+  return p.d % two == 0 && (p.pairs || p.rot_dim % two == 0);
+}
+
+template <bool BF16, int LANES>
+__global__ __launch_bounds__(QT) void qk_chunk_kernel(QkParams p, int32_t rows, int32_t per_token,
+                                                      FastDiv div) {
+  constexpr int V = Chunk<BF16>::V;
+  const int lane = threadIdx.x & 63;
+  const int32_t row = ((int32_t)blockIdx.x * QW + (threadIdx.x >> 6)) * (64 / LANES) + lane / LANES;
+  const int32_t i = (lane % LANES) * V;
+  if (row >= rows) return;   // whole rows: the folds below stay within one
+  const Row r = row_at(p, row, per_token, div);
+  if (!r.out) return;
+  const bool in = i < p.d / 2;   // lanes past the row's chunks repeat its first
+  int32_t a, b;
+  const bool turned = chunks_of(p, in ? i : 0, a, b);
+  const u32x4 wx = load_chunk<BF16>(r.x, r.from + a), wy = load_chunk<BF16>(r.x, r.from + b);
+  if (!r.w) {
+    if (in) {
+      gst<u32x4_a2>(static_cast<char*>(r.out) + (r.to + a) * Chunk<BF16>::ES, wx);
+      gst<u32x4_a2>(static_cast<char*>(r.out) + (r.to + b) * Chunk<BF16>::ES, wy);
+    }
+    return;
+  }
+  float x[V], y[V], c[V], s[V], wa[V], wb[V];
+  load_angles<V>(p, r.pos, a, b, turned, c, s);
+  load_floats<V>(r.w + a, wa);
+  load_floats<V>(r.w + b, wb);
+  widen<BF16>(wx, x);
+  widen<BF16>(wy, y);
+  float sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) sum += x[e] * x[e] + y[e] * y[e];
+  const float rstd = 1.0f / sqrtf(lanes_sum<LANES>(in ? sum : 0.0f) / (float)p.d + p.eps);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    x[e] = r.pos < 0 ? 0.0f : x[e] * rstd * wa[e];
+    y[e] = r.pos < 0 ? 0.0f : y[e] * rstd * wb[e];
+  }
+  turn<V>(p.pairs, false, c, s, x, y);
+  if (in) {
+    store_chunk<BF16>(r.out, r.to + a, x);
+    store_chunk<BF16>(r.out, r.to + b, y);
+  }
+}
+
+// Backward.  Workgroup w of a side (the first nq of the queries, the rest of the keys) takes every n-th
+// set of QW * 64 / LANES rows and keeps its part of the weights' gradient in registers; parts go to
+// `part` (a row of D per workgroup), or straight to dw where a side has one workgroup.
+template <bool BF16, int LANES>
+__global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32_t nq, float* part) {
+  constexpr int V = Chunk<BF16>::V, SLOTS = 64 / LANES;
+  __shared__ float acc[QW][LANES * 2 * V];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool keys = (int32_t)blockIdx.x >= nq;
+  const int32_t wg = blockIdx.x - (keys ? nq : 0), n_wg = keys ? (int32_t)gridDim.x - nq : nq;
+  const QkSide sd = keys ? p.side[1] : p.side[0];
+  const int32_t i = (lane % LANES) * V;
+  const bool in = i < p.d / 2;
+  int32_t a, b;
+  const bool turned = chunks_of(p, in ? i : 0, a, b);
+  float wa[V], wb[V], da[V], db[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) wa[e] = wb[e] = da[e] = db[e] = 0.0f;
+  // this lane's row, stepped without divisions
+  const int64_t first = ((int64_t)wg * QW + wave) * SLOTS + lane / LANES;
+  const int64_t step = (int64_t)n_wg * QW * SLOTS;
+  const int64_t step_t = step / (sd.heads ? sd.heads : 1);
+  const int32_t step_h = (int32_t)(step - step_t * sd.heads);
+  int64_t t = sd.heads ? first / sd.heads : p.tokens;
+  int32_t h = (int32_t)(first - t * sd.heads);
+  if (t < p.tokens) {
+    load_floats<V>(sd.w + a, wa);
+    load_floats<V>(sd.w + b, wb);
+  }
+  while (t < p.tokens) {   // the lanes of a row leave together
+    const int64_t pos = gld<int64_t>(p.pos + t);
+    const bool held = pos >= 0 && pos < p.n_positions;
+    const int64_t hd = (int64_t)h * p.d;
+    const int64_t fx = t * sd.ldx + hd, fg = t * sd.ldg + hd;
+    const u32x4 xw = load_chunk<BF16>(sd.x, fx + a), yw = load_chunk<BF16>(sd.x, fx + b);
+    const u32x4 gw = load_chunk<BF16>(sd.g, fg + a), fw = load_chunk<BF16>(sd.g, fg + b);
+    float x[V], y[V], g[V], f[V], c[V], s[V];
+    load_angles<V>(p, held ? pos : -1, a, b, turned, c, s);
+    widen<BF16>(xw, x);
+    widen<BF16>(yw, y);
+    widen<BF16>(gw, g);
+    widen<BF16>(fw, f);
+    turn<V>(p.pairs, true, c, s, g, f);
+    float xx = 0.0f, ux = 0.0f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      xx += x[e] * x[e] + y[e] * y[e];
+      ux += g[e] * wa[e] * x[e] + f[e] * wb[e] * y[e];
+    }
+    const float r = 1.0f / sqrtf(lanes_sum<LANES>(in ? xx : 0.0f) / (float)p.d + p.eps);
+    const float m = lanes_sum<LANES>(in ? ux : 0.0f) * r / (float)p.d;   // mean(u xn)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float xn = x[e] * r, yn = y[e] * r;
+      if (held) {
+        da[e] += g[e] * xn;
+        db[e] += f[e] * yn;
+      }
+      x[e] = held ? r * (g[e] * wa[e] - xn * m) : 0.0f;
+      y[e] = held ? r * (f[e] * wb[e] - yn * m) : 0.0f;
+    }
+    if (in) {
+      store_chunk<BF16>(sd.out, t * sd.ldo + hd + a, x);
+      store_chunk<BF16>(sd.out, t * sd.ldo + hd + b, y);
+    }
+    t += step_t;
+    h += step_h;
+    if (h >= sd.heads) {
+      h -= sd.heads;
+      ++t;
+    }
+  }
+  // the rows of a wavefront, then the wavefronts, added in a fixed order
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+#pragma unroll
+    for (int d = LANES; d < 64; d *= 2) {
+      da[e] += __shfl_xor(da[e], d, 64);
+      db[e] += __shfl_xor(db[e], d, 64);
+    }
+    if (lane < LANES) {
+      acc[wave][e * LANES + lane] = da[e];
+      acc[wave][(V + e) * LANES + lane] = db[e];
+    }
+  }
+  __syncthreads();
+  for (int32_t j = threadIdx.x; j < LANES * 2 * V; j += QT) {
+    const int32_t ln = j % LANES, e = j / LANES;
+    if (ln * V >= p.d / 2) continue;
+    chunks_of(p, ln * V, a, b);
+    const float v = ((acc[0][j] + acc[1][j]) + acc[2][j]) + acc[3][j];
+    gst<float>((part ? part + (int64_t)blockIdx.x * p.d : sd.dw) + (e < V ? a + e : b + e - V), v);
+  }
+}
+
+// ---- other rows -----------------------------------------------------------------------------------
+constexpr int IN_FLIGHT = 4;   // rows of a wavefront
 
 // Entries of unit u of a row: a pair (a, b) below rot_dim / 2, else the entry a alone (b < 0).
 __device__ __forceinline__ void unit_entries(const QkParams& p, int32_t u, int32_t& a, int32_t& b) {
@@ -49,92 +375,70 @@ __device__ __forceinline__ void unit_entries(const QkParams& p, int32_t u, int32
   }
 }
 
-// First element of head `head` of cache slot `slot` (inside the pools).
-__device__ __forceinline__ int64_t slot_base(const QkParams& p, int64_t slot, int32_t head) {
-  const int64_t page = p.n_slots <= 0x7fffffff ? (int64_t)fdiv((uint32_t)slot, p.page)
-                                               : slot / p.page_size;
-  return page * p.page_stride + (slot - page * p.page_size) * p.pos_stride + head * p.head_stride;
-}
-
 template <int NU>
-__global__ __launch_bounds__(QT) void qk_row_kernel(QkParams p, int64_t rows, int32_t per_token,
-                                                    FastDiv div) {
+__global__ __launch_bounds__(QT) void qk_unit_kernel(QkParams p, int32_t rows, int32_t per_token,
+                                                     FastDiv div) {
   const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (QT / 64) + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const int64_t t = fdiv((uint32_t)row, div);
-  int32_t head = (int32_t)(row - t * per_token);
-  int side = 0;
-  for (; side < 2 && head >= p.side[side].heads; ++side) head -= p.side[side].heads;
-  const int64_t pos = p.pos[t];
-  const bool held = pos >= 0 && pos < p.n_positions;
-  int64_t to = 0;
-  void* out;
-  if (side > 0 && p.slot) {
-    const int64_t slot = p.slot[t];
-    if (!held || slot < 0 || slot >= p.n_slots) return;
-    to = slot_base(p, slot, head);
-    out = side == 1 ? p.kc : p.vc;
-  } else {
-    to = t * p.side[side].ldo + (int64_t)head * p.d;
-    out = p.side[side].out;
-  }
-  if (side == 2) {   // a value head: copied
-    for (int32_t e = lane; e < p.d; e += 64)
-      store_elem(out, to + e, load_elem(p.v, t * p.ldv + (int64_t)head * p.d + e, p.bf16), p.bf16);
-    return;
-  }
-  const QkSide& sd = p.side[side];
-  const int64_t from = t * sd.ldx + (int64_t)head * p.d;
+  const int32_t row0 = ((int32_t)blockIdx.x * QW + (threadIdx.x >> 6)) * IN_FLIGHT;
   const int32_t units = p.d - p.rot_dim / 2;
-  float xa[NU], xb[NU], sum = 0.0f;
+  Row r[IN_FLIGHT];
+  float xa[IN_FLIGHT][NU], xb[IN_FLIGHT][NU];
 #pragma unroll
-  for (int i = 0; i < NU; ++i) {
-    const int32_t u = lane + 64 * i;
-    xa[i] = xb[i] = 0.0f;
-    if (u < units) {
+  for (int k = 0; k < IN_FLIGHT; ++k) {
+    r[k] = row_at(p, row0 + k < rows ? row0 + k : rows - 1, per_token, div);
+    if (row0 + k >= rows) r[k].out = nullptr;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int32_t u = lane + 64 * i;
+      xa[k][i] = xb[k][i] = 0.0f;
+      if (u >= units) continue;
       int32_t a, b;
       unit_entries(p, u, a, b);
-      xa[i] = load_elem(sd.x, from + a, p.bf16);
-      if (b >= 0) xb[i] = load_elem(sd.x, from + b, p.bf16);
+      xa[k][i] = load_elem(r[k].x, r[k].from + a, p.bf16);
+      if (b >= 0) xb[k][i] = load_elem(r[k].x, r[k].from + b, p.bf16);
     }
-    sum += xa[i] * xa[i] + xb[i] * xb[i];
   }
-  const float r = 1.0f / sqrtf(wave_sum(sum) / (float)p.d + p.eps);
 #pragma unroll
-  for (int i = 0; i < NU; ++i) {
-    const int32_t u = lane + 64 * i;
-    if (u >= units) continue;
-    int32_t a, b;
-    unit_entries(p, u, a, b);
-    float ya = 0.0f, yb = 0.0f;
-    if (held) {
-      ya = xa[i] * r * gld<float>(sd.w + a);
-      if (b >= 0) {
-        yb = xb[i] * r * gld<float>(sd.w + b);
-        const float c = gld<float>(p.rot + pos * p.rot_dim + u);
-        const float s = gld<float>(p.rot + pos * p.rot_dim + p.rot_dim / 2 + u);
-        const float ta = ya * c - yb * s;
-        yb = yb * c + ya * s;
-        ya = ta;
+  for (int k = 0; k < IN_FLIGHT; ++k) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) sum += xa[k][i] * xa[k][i] + xb[k][i] * xb[k][i];
+    const float rstd = 1.0f / sqrtf(lanes_sum<64>(sum) / (float)p.d + p.eps);
+    if (!r[k].out) continue;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int32_t u = lane + 64 * i;
+      if (u >= units) continue;
+      int32_t a, b;
+      unit_entries(p, u, a, b);
+      float ya = xa[k][i], yb = xb[k][i];   // a value: copied
+      if (r[k].w) {
+        const bool held = r[k].pos >= 0;
+        ya = held ? ya * rstd * gld<float>(r[k].w + a) : 0.0f;
+        if (b >= 0 && held) {
+          yb = yb * rstd * gld<float>(r[k].w + b);
+          const float c = gld<float>(p.rot + r[k].pos * p.rot_dim + u);
+          const float s = gld<float>(p.rot + r[k].pos * p.rot_dim + p.rot_dim / 2 + u);
+          const float t = ya * c - yb * s;
+          yb = yb * c + ya * s;
+          ya = t;
+        } else {
+          yb = 0.0f;
+        }
       }
+      store_elem(r[k].out, r[k].to + a, ya, p.bf16);
+      if (b >= 0) store_elem(r[k].out, r[k].to + b, yb, p.bf16);
     }
-    store_elem(out, to + a, ya, p.bf16);
-    if (b >= 0) store_elem(out, to + b, yb, p.bf16);
   }
 }
 
-// Backward.  Workgroup w of a side (nq of the queries, the rest of the keys) takes its rows w, w + n,
-// ... and keeps its part of the weights' gradient in registers; parts go to `part` (a row of D per
-// workgroup), or straight to dw where a side has one workgroup.
 template <int NU>
-__global__ __launch_bounds__(QT) void qk_backward_row_kernel(QkParams p, int32_t nq, float* part) {
-  __shared__ float acc[QT / 64][2 * 64 * NU];
+__global__ __launch_bounds__(QT) void qk_backward_unit_kernel(QkParams p, int32_t nq, float* part) {
+  __shared__ float acc[QW][2 * 64 * NU];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int side = (int32_t)blockIdx.x >= nq ? 1 : 0;
-  const int32_t wg = blockIdx.x - (side ? nq : 0);
-  const int32_t n_wg = side ? (int32_t)gridDim.x - nq : nq;
-  const QkSide& sd = p.side[side];
+  const bool keys = (int32_t)blockIdx.x >= nq;
+  const int32_t wg = blockIdx.x - (keys ? nq : 0), n_wg = keys ? (int32_t)gridDim.x - nq : nq;
+  const QkSide sd = keys ? p.side[1] : p.side[0];
   const int64_t rows = p.tokens * sd.heads;
   const int32_t units = p.d - p.rot_dim / 2;
   float wa[NU], wb[NU], da[NU], db[NU];
@@ -148,51 +452,72 @@ __global__ __launch_bounds__(QT) void qk_backward_row_kernel(QkParams p, int32_t
     wa[i] = gld<float>(sd.w + a);
     if (b >= 0) wb[i] = gld<float>(sd.w + b);
   }
-  for (int64_t row = (int64_t)wg * (QT / 64) + wave; row < rows; row += (int64_t)n_wg * (QT / 64)) {
-    const int64_t t = row / sd.heads;
-    const int32_t head = (int32_t)(row - t * sd.heads);
-    const int64_t pos = p.pos[t];
-    const bool held = pos >= 0 && pos < p.n_positions;
-    const int64_t fx = t * sd.ldx + (int64_t)head * p.d, fg = t * sd.ldg + (int64_t)head * p.d,
-                  to = t * sd.ldo + (int64_t)head * p.d;
-    float xa[NU], xb[NU], ga[NU], gb[NU], xx = 0.0f, ux = 0.0f;
+  const int64_t step = (int64_t)n_wg * QW * IN_FLIGHT;
+  for (int64_t row0 = ((int64_t)wg * QW + wave) * IN_FLIGHT; row0 < rows; row0 += step) {
+    float xa[IN_FLIGHT][NU], xb[IN_FLIGHT][NU], ga[IN_FLIGHT][NU], gb[IN_FLIGHT][NU];
+    float c[IN_FLIGHT][NU], s[IN_FLIGHT][NU];
+    int64_t to[IN_FLIGHT];
+    bool held[IN_FLIGHT];
+    // the first row's token by division, the others' by counting on
+    int64_t t = row0 / sd.heads;
+    int32_t head = (int32_t)(row0 - t * sd.heads);
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      const int32_t u = lane + 64 * i;
-      xa[i] = xb[i] = ga[i] = gb[i] = 0.0f;
-      if (u < units && held) {
+    for (int k = 0; k < IN_FLIGHT; ++k) {
+      const bool there = row0 + k < rows;
+      const int64_t pos = there ? gld<int64_t>(p.pos + t) : -1;
+      held[k] = pos >= 0 && pos < p.n_positions;
+      const int64_t hd = (int64_t)head * p.d;
+      to[k] = there ? t * sd.ldo + hd : -1;
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        const int32_t u = lane + 64 * i;
+        xa[k][i] = xb[k][i] = ga[k][i] = gb[k][i] = s[k][i] = 0.0f;
+        c[k][i] = 1.0f;
+        if (u >= units || !held[k]) continue;
         int32_t a, b;
         unit_entries(p, u, a, b);
-        xa[i] = load_elem(sd.x, fx + a, p.bf16);
-        ga[i] = load_elem(sd.g, fg + a, p.bf16);
+        xa[k][i] = load_elem(sd.x, t * sd.ldx + hd + a, p.bf16);
+        ga[k][i] = load_elem(sd.g, t * sd.ldg + hd + a, p.bf16);
         if (b >= 0) {
-          xb[i] = load_elem(sd.x, fx + b, p.bf16);
-          gb[i] = load_elem(sd.g, fg + b, p.bf16);
-          const float c = gld<float>(p.rot + pos * p.rot_dim + u);
-          const float s = gld<float>(p.rot + pos * p.rot_dim + p.rot_dim / 2 + u);
-          const float ta = ga[i] * c + gb[i] * s;
-          gb[i] = gb[i] * c - ga[i] * s;
-          ga[i] = ta;
+          xb[k][i] = load_elem(sd.x, t * sd.ldx + hd + b, p.bf16);
+          gb[k][i] = load_elem(sd.g, t * sd.ldg + hd + b, p.bf16);
+          c[k][i] = gld<float>(p.rot + pos * p.rot_dim + u);
+          s[k][i] = gld<float>(p.rot + pos * p.rot_dim + p.rot_dim / 2 + u);
         }
       }
-      xx += xa[i] * xa[i] + xb[i] * xb[i];
-      ux += ga[i] * wa[i] * xa[i] + gb[i] * wb[i] * xb[i];
-    }
-    const float r = 1.0f / sqrtf(wave_sum(xx) / (float)p.d + p.eps);
-    const float m = wave_sum(ux) * r / (float)p.d;   // mean(u xn)
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      const int32_t u = lane + 64 * i;
-      if (u >= units) continue;
-      int32_t a, b;
-      unit_entries(p, u, a, b);
-      const float na = xa[i] * r, nb = xb[i] * r;
-      if (held) {
-        da[i] += ga[i] * na;
-        db[i] += gb[i] * nb;
+      if (++head == sd.heads) {
+        head = 0;
+        ++t;
       }
-      store_elem(sd.out, to + a, held ? r * (ga[i] * wa[i] - na * m) : 0.0f, p.bf16);
-      if (b >= 0) store_elem(sd.out, to + b, held ? r * (gb[i] * wb[i] - nb * m) : 0.0f, p.bf16);
+    }
+#pragma unroll
+    for (int k = 0; k < IN_FLIGHT; ++k) {
+      float xx = 0.0f, ux = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        const float g = ga[k][i] * c[k][i] + gb[k][i] * s[k][i];
+        gb[k][i] = gb[k][i] * c[k][i] - ga[k][i] * s[k][i];
+        ga[k][i] = g;
+        xx += xa[k][i] * xa[k][i] + xb[k][i] * xb[k][i];
+        ux += ga[k][i] * wa[i] * xa[k][i] + gb[k][i] * wb[i] * xb[k][i];
+      }
+      const float r = 1.0f / sqrtf(lanes_sum<64>(xx) / (float)p.d + p.eps);
+      const float m = lanes_sum<64>(ux) * r / (float)p.d;   // mean(u xn)
+      if (to[k] < 0) continue;
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        const int32_t u = lane + 64 * i;
+        if (u >= units) continue;
+        int32_t a, b;
+        unit_entries(p, u, a, b);
+        const float na = xa[k][i] * r, nb = xb[k][i] * r;
+        if (held[k]) {
+          da[i] += ga[k][i] * na;
+          db[i] += gb[k][i] * nb;
+        }
+        store_elem(sd.out, to[k] + a, held[k] ? r * (ga[k][i] * wa[i] - na * m) : 0.0f, p.bf16);
+        if (b >= 0) store_elem(sd.out, to[k] + b, held[k] ? r * (gb[k][i] * wb[i] - nb * m) : 0.0f, p.bf16);
+      }
     }
   }
   // the four wavefronts' parts, added in order
@@ -214,25 +539,52 @@ __global__ __launch_bounds__(QT) void qk_backward_row_kernel(QkParams p, int32_t
   }
 }
 
-// dw[e] of a side: its workgroups' parts, in order.
-__global__ __launch_bounds__(QT) void qk_fold_kernel(QkParams p, int32_t nq, int32_t nk,
+// dw of a side: its workgroups' parts.  16 wavefronts of a workgroup take every 16th part of 64 entries,
+// 8 in flight, and meet in order.
+constexpr int FT = 1024, FW = FT / 64;
+__global__ __launch_bounds__(FT) void qk_fold_kernel(QkParams p, int32_t nq, int32_t nk,
                                                      const float* part) {
-  const int side = blockIdx.y;
-  const QkSide& sd = p.side[side];
-  const int32_t e = blockIdx.x * QT + threadIdx.x, n = side ? nk : nq;
-  if (e >= p.d || sd.heads == 0) return;
-  const float* from = part + (int64_t)(side ? nq : 0) * p.d + e;
+  __shared__ float acc[FW][64];
+  const bool keys = blockIdx.y != 0;
+  const int32_t heads = keys ? p.side[1].heads : p.side[0].heads;
+  if (heads == 0) return;
+  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t e = blockIdx.x * 64 + lane, n = keys ? nk : nq;
+  const float* from = part + (int64_t)(keys ? nq : 0) * p.d + e;
   float sum = 0.0f;
-  for (int32_t i = 0; i < n; ++i) sum += gld<float>(from + (int64_t)i * p.d);
-  gst<float>(sd.dw + e, sum);
+  for (int32_t i = wave; i < n; i += 8 * FW) {
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      x[u] = e < p.d && i + u * FW < n ? gld<float>(from + (int64_t)(i + u * FW) * p.d) : 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += x[u];
+  }
+  acc[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && e < p.d) {
+#pragma unroll
+    for (int w = 1; w < FW; ++w) sum += acc[w][lane];
+    gst<float>((keys ? p.side[1].dw : p.side[0].dw) + e, sum);
+  }
 }
+
+int lanes_of(const QkParams& p) {
+  const int32_t two = p.bf16 ? 16 : 8;
+  int lanes = 4;
+  while (lanes * two < p.d) lanes *= 2;
+  return lanes;
+}
+
+// Rows that a wavefront takes at once.
+int rows_at_once(const QkParams& p) { return chunked(p) ? 64 / lanes_of(p) : IN_FLIGHT; }
 
 // Workgroups of the two sides in the backward pass: 1024 in all where there are rows for them.
 void backward_groups(const QkParams& p, int32_t& nq, int32_t& nk) {
-  const int32_t heads = p.side[0].heads + p.side[1].heads;
+  const int32_t heads = p.side[0].heads + p.side[1].heads, rows = QW * rows_at_once(p);
   int32_t n[2];
   for (int s = 0; s < 2; ++s) {
-    const int64_t full = (p.tokens * p.side[s].heads + QT / 64 - 1) / (QT / 64);
+    const int64_t full = (p.tokens * p.side[s].heads + rows - 1) / rows;
     const int64_t share = (int64_t)1024 * p.side[s].heads / heads;
     const int64_t most = full < share ? full : share;
     n[s] = p.side[s].heads == 0 ? 0 : most < 1 ? 1 : (int32_t)most;
@@ -249,7 +601,7 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
   const int32_t units = p.d - p.rot_dim / 2;
   const FastDiv div(per);
   // rows count in 32 bits within a launch
-  const int64_t step = 0x7ffffff0 / per;
+  const int64_t step = 0x7fff0000 / per;
   for (int64_t t0 = 0; t0 < p.tokens; t0 += step) {
     QkParams q = p;
     q.tokens = p.tokens - t0 < step ? p.tokens - t0 : step;
@@ -263,14 +615,30 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
       q.slot += t0;
     }
     q.pos += t0;
-    const int64_t rows = q.tokens * per;
-    const dim3 grid((uint32_t)((rows + QT / 64 - 1) / (QT / 64)));
-#define TPP_QK(NU) \
-  hipLaunchKernelGGL((qk_row_kernel<NU>), grid, dim3(QT), 0, stream, q, rows, per, div)
-    if (units <= 64) TPP_QK(1);
-    else if (units <= 128) TPP_QK(2);
-    else if (units <= 256) TPP_QK(4);
-    else TPP_QK(8);
+    const int32_t rows = (int32_t)(q.tokens * per), wg = QW * rows_at_once(p);
+    const dim3 grid((uint32_t)(((int64_t)rows + wg - 1) / wg));
+#define TPP_QK(KERNEL, ...) \
+  hipLaunchKernelGGL((KERNEL<__VA_ARGS__>), grid, dim3(QT), 0, stream, q, rows, per, div)
+#define TPP_QK_LANES(BF16)                                    \
+  switch (lanes_of(p)) {                                      \
+    case 4: TPP_QK(qk_chunk_kernel, BF16, 4); break;          \
+    case 8: TPP_QK(qk_chunk_kernel, BF16, 8); break;          \
+    case 16: TPP_QK(qk_chunk_kernel, BF16, 16); break;        \
+    case 32: TPP_QK(qk_chunk_kernel, BF16, 32); break;        \
+    default: TPP_QK(qk_chunk_kernel, BF16, 64);               \
+  }
+    if (chunked(p)) {
+      if (p.bf16) { TPP_QK_LANES(true) } else { TPP_QK_LANES(false) }
+    } else if (units <= 64) {
+      TPP_QK(qk_unit_kernel, 1);
+    } else if (units <= 128) {
+      TPP_QK(qk_unit_kernel, 2);
+    } else if (units <= 256) {
+      TPP_QK(qk_unit_kernel, 4);
+    } else {
+      TPP_QK(qk_unit_kernel, 8);
+    }
+#undef TPP_QK_LANES
 #undef TPP_QK
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -294,16 +662,31 @@ hipError_t launch_qk_backward(const QkParams& p, float* work, hipStream_t stream
     nk = nk < 1 ? nk : 1;
   }
   const int32_t units = p.d - p.rot_dim / 2;
-#define TPP_QKB(NU)                                                                              \
-  hipLaunchKernelGGL((qk_backward_row_kernel<NU>), dim3(nq + nk), dim3(QT), 0, stream, p, nq, work)
-  if (units <= 64) TPP_QKB(1);
-  else if (units <= 128) TPP_QKB(2);
-  else if (units <= 256) TPP_QKB(4);
-  else TPP_QKB(8);
+#define TPP_QKB(KERNEL, ...)                                                                      \
+  hipLaunchKernelGGL((KERNEL<__VA_ARGS__>), dim3(nq + nk), dim3(QT), 0, stream, p, nq, work)
+#define TPP_QKB_LANES(BF16)                                             \
+  switch (lanes_of(p)) {                                                \
+    case 4: TPP_QKB(qk_backward_chunk_kernel, BF16, 4); break;          \
+    case 8: TPP_QKB(qk_backward_chunk_kernel, BF16, 8); break;          \
+    case 16: TPP_QKB(qk_backward_chunk_kernel, BF16, 16); break;        \
+    case 32: TPP_QKB(qk_backward_chunk_kernel, BF16, 32); break;        \
+    default: TPP_QKB(qk_backward_chunk_kernel, BF16, 64);               \
+  }
+  if (chunked(p)) {
+    if (p.bf16) { TPP_QKB_LANES(true) } else { TPP_QKB_LANES(false) }
+  } else if (units <= 64) {
+    TPP_QKB(qk_backward_unit_kernel, 1);
+  } else if (units <= 128) {
+    TPP_QKB(qk_backward_unit_kernel, 2);
+  } else if (units <= 256) {
+    TPP_QKB(qk_backward_unit_kernel, 4);
+  } else {
+    TPP_QKB(qk_backward_unit_kernel, 8);
+  }
+#undef TPP_QKB_LANES
 #undef TPP_QKB
   if (work)
-    hipLaunchKernelGGL(qk_fold_kernel, dim3((p.d + QT - 1) / QT, 2), dim3(QT), 0, stream, p, nq, nk,
-                       work);
+    hipLaunchKernelGGL(qk_fold_kernel, dim3((p.d + 63) / 64, 2), dim3(FT), 0, stream, p, nq, nk, work);
   return hipGetLastError();
 }
 

@@ -269,6 +269,26 @@ def test_norm_rope_backward_no_tokens_and_in_place(tpp):
         assert torch.equal(dev[s].ravel(), outs[s]) and torch.equal(dw[s], want[s][:64])
 
 
+@pytest.mark.parametrize("form", ["halves", "pairs"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_rope_without_a_table(tpp, form, dtype):
+    """A table of no rows: every token is padding, the table may be NULL."""
+    T, D = 9, 64
+    rot = tpp.TPP_ROT_HALVES if form == "halves" else tpp.TPP_ROT_PAIRS
+    d = tpp.tpp_qk_desc(D, D, rot, 2, 1, code(tpp, dtype), EPS, 0)
+    rng = np.random.default_rng(1)
+    q, k, g = (up(draw(rng, (T, h * D), dtype)) for h in (2, 1, 2))
+    w, pos = torch.ones(D, device="cuda"), torch.zeros(T, dtype=torch.int64, device="cuda")
+    dw = [torch.full((D,), 7.0, device="cuda") for _ in range(2)]
+    out = [torch.full_like(x, 3) for x in (q, k, q, k)]
+    s = tpp.current_stream()
+    tpp.tpp_qk_norm_rope(d, T, q, 2 * D, k, D, w, w, None, pos, out[0], 2 * D, out[1], D, s)
+    tpp.tpp_qk_norm_rope_backward(d, T, q, 2 * D, k, D, w, w, None, pos, g, 2 * D, k, D, out[2], 2 * D,
+                                  out[3], D, dw[0], dw[1], s)
+    torch.cuda.synchronize()
+    assert not any(x.any() for x in out + dw)
+
+
 def test_backward_against_differences(tpp):
     """fp32 gradients against central differences of the GPU's own forward pass, all entries of one
     head moved along a random direction: the sum's curvature bounds the rest."""
