@@ -155,7 +155,7 @@ tpp_status tpp_paged_attention(const tpp_attn_desc* desc, const tpp_kv_cache* ca
  * Work buffer and its errors as tpp_reduce (a capture without one: NO_MEMORY).
  * Errors: INVALID_ARG for sizes < 0, max_len > 2^30, ldt < max_len, a malformed cache or a NULL
  * pointer when there is work; UNSUPPORTED for a launch of more than 2^31 - 1 workgroups, or where the
- * moves of one sequence could take more than 2^31 - 1 chunks of 16 bytes of a pool. */
+ * moves of one sequence could be more than 2^30 rows (positions * kv_heads). */
 tpp_status tpp_cache_evict(const tpp_kv_cache* cache, int64_t n_seqs, int64_t max_len, int64_t budget,
                            const int64_t* d_len, const int64_t* d_pages, int64_t ld_pages,
                            const float* totals, const int64_t* d_pos, const int64_t* d_horizon,

@@ -3,12 +3,13 @@
 // Per sequence: the e candidates of least total leave (ties by position), and what is kept behind the
 // new length moves into the free places below it, in order.  The totals become unsigned keys of the
 // same order, a radix selection (11 + 11 + 10 bits, one histogram each) finds the key T of the e-th
-// smallest candidate, and how many candidates of exactly T leave.  Then the sequence is walked in
-// order: each wavefront has a run of positions, counts its ties, its free places and its movers with
-// ballots, and three counts per wavefront give every one its place in the lists.
+// smallest candidate, and how many candidates of exactly T leave.  Each thread has a run of consecutive
+// positions, and running sums over the threads of its ties, free places and movers give every one its
+// place in the lists.  (Ballots over sets of 64 positions, a wavefront's run at a time, are scalar work,
+// and the compute unit has one scalar unit for its 16 wavefronts: FILL us for 16384 positions, FILL so.)
 //
-// One workgroup of 16 wavefronts per sequence selects.  Up to 32 totals per lane stay in registers, so
-// that memory is read once, with every load in flight; longer sequences are read again by each pass.
+// One workgroup of 16 wavefronts per sequence selects.  Up to 32 keys per thread stay in registers, so that
+// memory is read once, with every load in flight; longer sequences are read again by each pass.
 // The moved rows of keys and values, at most half a sequence, are copied by a second kernel, a 16-byte
 // chunk per lane -- or, where a sequence can lose only a few, by the selecting workgroup itself, since a
 // second launch would cost more than the copy.
@@ -26,6 +27,7 @@ constexpr int ST = 1024;          // threads of the selection: 16 wavefronts
 constexpr int SW = ST / 64;
 constexpr int BINS = 2048;        // of 11 bits
 constexpr int CT = 256;           // threads of the copy
+constexpr int FUSED_CHUNKS = 2 * ST;   // most chunks of a pool that the selecting workgroup copies
 
 // The totals' order as unsigned integers: -0 as +0, NaN above everything.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -34,18 +36,15 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ int32_t lanes_below(uint64_t mask) {
-  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
-                                   __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
-}
-
-// Lists of the moves, in the work space: per sequence the number of moves, then their free places and
-// their movers (cap of each).
+// What the selection leaves in the work space for the copy: per sequence a bit for each position, set
+// in the free places (words of 16), the number of moves, and their free
+// places and movers (cap of each).
 struct MoveLists {
+  uint16_t* gone;
   int32_t* count;
   int32_t* to;
   int32_t* from;
-  int64_t cap;
+  int64_t cap, words;
 };
 
 // Element offset of position t of sequence b (head 0), or -1 where no page holds it.
@@ -56,116 +55,149 @@ __device__ __forceinline__ int64_t row_of(const EvictParams& p, int64_t b, int32
   return page * p.page_stride + (int64_t)(t - j * p.page_size) * p.pos_stride;
 }
 
-// Copies the moved rows of sequence b: threads `at`, at + step, ... of a set that covers them.  A thread
-// takes a 16-byte chunk of a head's row, of the keys and of the values; a row that is no multiple of 16
-// bytes ends with the chunk that ends with it, a shorter one goes by 2-byte units.
+// How the moved rows are copied: `lanes` (a power of two up to 64) consecutive lanes take a row of one
+// head, a 16-byte chunk each (of more than 64 chunks, every 64th), of the keys and of the values.  A row
+// that is no multiple of 16 bytes ends with the chunk that ends with it.  Rows below 16 bytes (unit 2) go
+// by 2 bytes to a lane.
 struct CopyShape {
-  FastDiv chunks, heads;   // chunks of a row; kv_heads
-  int32_t n_chunks;
+  FastDiv heads;              // kv_heads
+  int32_t lanes, unit, units; // bytes of a chunk; chunks of a row
 };
+
+template <int U, typename T>
+__device__ __forceinline__ void copy_rows(const EvictParams& p, const CopyShape& cs, int64_t b,
+                                          const int32_t* to, const int32_t* from, int32_t rows,
+                                          int32_t row, int32_t step, int32_t lane) {
+  const int32_t bytes = p.d * p.es;
+  char* kb = static_cast<char*>(p.k);
+  char* vb = static_cast<char*>(p.v);
+  for (; row < rows; row += U * step) {   // rows below 2^30 by the launcher
+    int64_t dst[U], src[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t r = row + u * step < rows ? row + u * step : row;   // past the end: the first again
+      const int32_t j = fdiv((uint32_t)r, cs.heads), h = r - j * p.kv_heads;
+      const int64_t d = row_of(p, b, to[j]), s = row_of(p, b, from[j]);
+      dst[u] = d < 0 || s < 0 ? -1 : (d + h * p.head_stride) * p.es;
+      src[u] = (s + h * p.head_stride) * p.es;
+    }
+    for (int32_t c = lane; c < cs.units; c += cs.lanes) {
+      const int32_t e = (c + 1) * cs.unit <= bytes ? c * cs.unit : bytes - cs.unit;
+      T k[U], v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (dst[u] >= 0) {
+          k[u] = gld<T>(kb + src[u] + e);
+          v[u] = gld<T>(vb + src[u] + e);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (dst[u] >= 0) {
+          gst<T>(kb + dst[u] + e, k[u]);
+          gst<T>(vb + dst[u] + e, v[u]);
+        }
+    }
+  }
+}
+// Wavefront `wave` of `waves` that copy the moves of sequence b.
 template <int U>
 __device__ __forceinline__ void copy_moves(const EvictParams& p, const CopyShape& cs, int64_t b,
                                            const int32_t* to, const int32_t* from, int32_t moves,
-                                           int32_t at, int32_t step) {
-  const int32_t bytes = p.d * p.es, per_move = p.kv_heads * cs.n_chunks;
-  const int64_t all = (int64_t)moves * per_move;
-  char* kb = static_cast<char*>(p.k);
-  char* vb = static_cast<char*>(p.v);
-  for (int64_t i0 = at; i0 < all; i0 += (int64_t)step * U) {
-    u32x4 k[U], v[U];
-    int64_t dst[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t i = i0 + (int64_t)u * step;
-      dst[u] = -1;
-      if (i >= all) continue;
-      // below 2^31 by the launcher
-      const int32_t r = fdiv((uint32_t)i, cs.chunks), c = (int32_t)i - r * cs.n_chunks;
-      const int32_t j = fdiv((uint32_t)r, cs.heads), h = r - j * p.kv_heads;
-      const int64_t d = row_of(p, b, to[j]), s = row_of(p, b, from[j]);
-      if (d < 0 || s < 0) continue;
-      if (bytes < 16) {
-#pragma unroll 1
-        for (int32_t e = 0; e < bytes; e += 2) {
-          const int64_t x = (s + h * p.head_stride) * p.es + e, y = (d + h * p.head_stride) * p.es + e;
-          gst<uint16_t>(kb + y, gld<uint16_t>(kb + x));
-          gst<uint16_t>(vb + y, gld<uint16_t>(vb + x));
-        }
-        continue;
-      }
-      const int32_t e = c * 16 + 16 <= bytes ? c * 16 : bytes - 16;
-      const int64_t x = (s + h * p.head_stride) * p.es + e;
-      dst[u] = (d + h * p.head_stride) * p.es + e;
-      k[u] = gld<u32x4_a2>(kb + x);
-      v[u] = gld<u32x4_a2>(vb + x);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (dst[u] >= 0) {
-        gst<u32x4_a2>(kb + dst[u], k[u]);
-        gst<u32x4_a2>(vb + dst[u], v[u]);
-      }
-  }
+                                           int32_t wave, int32_t waves) {
+  const int32_t lane = threadIdx.x & 63, slots = 64 / cs.lanes;
+  const int32_t row = wave * slots + lane / cs.lanes, step = waves * slots;
+  if (cs.unit == 16)
+    copy_rows<U, u32x4_a2>(p, cs, b, to, from, moves * p.kv_heads, row, step, lane % cs.lanes);
+  else
+    copy_rows<1, uint16_t>(p, cs, b, to, from, moves * p.kv_heads, row, step, lane % cs.lanes);
 }
 
-// KPT: totals that a lane keeps (0: none, read again).  FUSED: this workgroup copies the rows too.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true);
+}
+// Running sums over the workgroup: what the threads before this one have of v, and in `all` the total.
+// Within a wavefront by register permutes (row shifts, then the rows' last lanes handed on).  The barriers
+// also order what was in LDS before the call.
+__device__ __forceinline__ uint32_t before_me(uint32_t v, uint32_t (&sums)[SW], uint32_t& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t up = v;
+  up += dpp_or_0<0x111, 0xf>(up);   // from 1, 2, 4 and 8 lanes down
+  up += dpp_or_0<0x112, 0xf>(up);
+  up += dpp_or_0<0x114, 0xf>(up);
+  up += dpp_or_0<0x118, 0xf>(up);
+  up += dpp_or_0<0x142, 0xa>(up);   // the row before, then the half before
+  up += dpp_or_0<0x143, 0xc>(up);
+  __syncthreads();
+  if (lane == 63) sums[wave] = up;
+  __syncthreads();
+  uint32_t before = up - v;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < SW; ++w) {
+    before += w < wave ? sums[w] : 0u;
+    all += sums[w];
+  }
+  return before;
+}
+
+// KPT: consecutive positions of a thread; a sequence is taken in parts of KPT * ST positions.  One part's
+// keys stay in registers; of several, each pass reads the totals again.  FUSED: this workgroup hands on
+// the totals and copies the rows too, and the lists stay in LDS.
 template <int KPT, bool FUSED>
 __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLists ml, CopyShape cs) {
+  constexpr int32_t PART = KPT * ST;
   __shared__ int32_t hist[BINS];
-  __shared__ int32_t wsum[3][SW];
-  __shared__ int32_t pick[2];     // digit, candidates below it
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ uint32_t sums[SW];
+  __shared__ uint32_t turned[PART + PART / 32];
+  __shared__ int32_t pick[3];     // digit, candidates below it, candidates of it
+  __shared__ int32_t lists[FUSED ? 2 * FUSED_CHUNKS : 1];
+  const int tid = threadIdx.x;
   const int64_t b = blockIdx.x;
   const int64_t len = gld<int64_t>(p.len + b);
+  const int64_t horizon = p.pos ? gld<int64_t>(p.horizon + b) : 0;
   const int32_t n = (int32_t)(len < 0 ? 0 : len > p.max_len ? p.max_len : len);
   const int32_t want = n > p.budget ? (int32_t)(n - p.budget) : 0;
   const float* tot = p.totals + b * p.ldt;
   const int64_t* pos = p.pos ? p.pos + b * p.ldt : nullptr;
-  const int64_t horizon = p.pos ? gld<int64_t>(p.horizon + b) : 0;
   float* tot_out = p.totals_out + b * p.ldt;
   int64_t* pos_out = p.pos ? p.pos_out + b * p.ldt : nullptr;
-  const bool hand_on = p.totals_out != p.totals, hand_pos = pos && p.pos_out != p.pos;
 
-  // ---- each wavefront's run of positions, whole sets of 64 ---------------------------------------
-  const int32_t run = (((n + SW - 1) / SW) + 63) / 64 * 64;
-  const int32_t t0 = wave * run < n ? wave * run : n;
-  const int32_t t1 = t0 + run < n ? t0 + run : n;
-  float w[KPT > 0 ? KPT : 1];
-  uint32_t may = 0;               // bit i: the i-th total is a candidate's
-  const auto may_go = [&](int32_t t) { return !pos || gld<int64_t>(pos + t) < horizon; };
-  if constexpr (KPT > 0) {
+  // Keys of this thread's positions of the part from `part` on; 0, which is no total's key, for a position
+  // that is no candidate.  Read in order, 16 loads in flight before the first is waited for (past the end
+  // the last position), and turned in LDS, a word in 33 left out against bank conflicts: a thread that read
+  // its own run would touch a cache line for every 16 bytes.
+  uint32_t keys[KPT];
+  const auto load_keys = [&](int32_t part) {
+    constexpr int P = KPT < 16 ? KPT : 16;   // in flight
+    __syncthreads();   // the part before is done with
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-      const int32_t t = t0 + i * 64 + lane;
-      w[i] = t < t1 ? gld<float>(tot + t) : 0.0f;
-    }
-    if (want > 0)
+    for (int i0 = 0; i0 < KPT; i0 += P) {
+      float x[P];
+      int64_t y[P];
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) {
-        const int32_t t = t0 + i * 64 + lane;
-        if (t < t1 && may_go(t)) may |= 1u << i;
+      for (int i = 0; i < P; ++i) {
+        const int32_t t = part + (i0 + i) * ST + tid, u = t < n ? t : n - 1;
+        x[i] = gld<float>(tot + u);
+        y[i] = pos ? gld<int64_t>(pos + u) : INT64_MIN;
       }
-  }
-  // f(t, in the run, key, candidate, total) for the run's sets in order, with all lanes
-  const auto each = [&](auto&& f) {
-    if constexpr (KPT > 0) {
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) {
-        const int32_t t = t0 + i * 64 + lane;
-        if (t0 + i * 64 < t1) f(t, t < t1, order_key(w[i]), (may >> i & 1) != 0, w[i]);
-      }
-    } else {
-      for (int32_t t = t0 + lane; t - lane < t1; t += 64) {
-        const bool in = t < t1;
-        const float x = in ? gld<float>(tot + t) : 0.0f;
-        f(t, in, order_key(x), in && may_go(t), x);
+      for (int i = 0; i < P; ++i) {
+        const int32_t at = (i0 + i) * ST + tid;
+        turned[at + at / 32] = part + at < n && (!pos || y[i] < horizon) ? order_key(x[i]) : 0u;
       }
     }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) keys[i] = turned[tid * KPT + i + (tid * KPT + i) / 32];
   };
+  const bool several = n > PART;
+  if (want > 0 && !several) load_keys(0);
 
   // ---- the key of the last one to leave ----------------------------------------------------------
   uint32_t prefix = 0;            // the digits found so far
   int32_t rank = 0, gone_n = 0;   // ordinal (from 0) among the candidates with that prefix
+  bool all_ties = false;          // whether all candidates of that key leave
   if (want > 0) {
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
@@ -174,108 +206,110 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
       const uint32_t found = pass == 0 ? 0u : pass == 1 ? 0xffe00000u : 0xfffffc00u;
       for (int i = tid; i < BINS; i += ST) hist[i] = 0;
       __syncthreads();
-      each([&](int32_t, bool, uint32_t key, bool cand, float) {
-        if (cand && (key & found) == prefix) atomicAdd(&hist[(key >> shift) & mask], 1);
-      });
-      __syncthreads();
-      // running sums of the histogram: two bins per thread
-      const int32_t h0 = hist[2 * tid], h1 = hist[2 * tid + 1];
-      int32_t up = h0 + h1;
+      for (int32_t part = 0; part < n; part += PART) {
+        if (several) load_keys(part);
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int32_t v = __shfl_up(up, d, 64);
-        if (lane >= d) up += v;
+        for (int i = 0; i < KPT; ++i)
+          if (keys[i] != 0 && (keys[i] & found) == prefix) atomicAdd(&hist[(keys[i] >> shift) & mask], 1);
       }
-      if (lane == 63) wsum[0][wave] = up;
       __syncthreads();
-      int32_t before = 0, all = 0;
-#pragma unroll
-      for (int x = 0; x < SW; ++x) {
-        const int32_t v = wsum[0][x];
-        before += x < wave ? v : 0;
-        all += v;
-      }
+      const int32_t h0 = hist[2 * tid], h1 = hist[2 * tid + 1];   // two bins per thread
+      uint32_t all;
+      const int32_t lo = (int32_t)before_me(h0 + h1, sums, all);   // candidates below them
       if (pass == 0) {
-        gone_n = all < want ? all : want;
+        gone_n = (int32_t)all < want ? (int32_t)all : want;
         rank = gone_n - 1;
       }
-      const int32_t lo = before + up - h0 - h1;   // candidates below this thread's bins
       if (gone_n > 0) {
         if (rank >= lo && rank < lo + h0) {
           pick[0] = 2 * tid;
           pick[1] = lo;
+          pick[2] = h0;
         } else if (rank >= lo + h0 && rank < lo + h0 + h1) {
           pick[0] = 2 * tid + 1;
           pick[1] = lo + h0;
+          pick[2] = h1;
         }
       }
       __syncthreads();
       if (gone_n == 0) break;
       prefix |= (uint32_t)pick[0] << shift;
       rank -= pick[1];
+      all_ties = rank + 1 == pick[2];
     }
   }
   const int32_t left = n - gone_n;
   // candidates below `prefix` leave, and of those equal to it the first rank + 1
 
-  int32_t ties = 0;
+  // ---- the lists, part by part in order ------------------------------------------------------------
+  int32_t* to = FUSED ? lists : ml.to + b * ml.cap;
+  int32_t* from = FUSED ? lists + FUSED_CHUNKS : ml.from + b * ml.cap;
+  int32_t places = 0, movers = 0;   // of the parts before
+  int32_t seen = 0;     // ties of the parts before
   if (gone_n > 0)
-    each([&](int32_t, bool, uint32_t key, bool cand, float) {
-      ties += __popcll(__ballot(cand && key == prefix));
-    });
-  if (lane == 0) wsum[0][wave] = ties;
-  __syncthreads();
-  int32_t ties_before = 0;
-  for (int x = 0; x < wave; ++x) ties_before += wsum[0][x];
-  // f(t, in the run, free place, mover, total)
-  const auto walk = [&](auto&& f) {
-    int32_t seen = ties_before;
-    each([&](int32_t t, bool in, uint32_t key, bool cand, float x) {
-      const uint64_t tie = __ballot(cand && key == prefix);
-      const bool goes = cand && (key < prefix || (key == prefix && seen + lanes_below(tie) <= rank));
-      seen += __popcll(tie);
-      f(t, in, goes && t < left, in && !goes && t >= left, x);
-    });
-  };
-  int32_t places = 0, movers = 0;
-  if (gone_n > 0)
-    walk([&](int32_t, bool, bool place, bool mover, float) {
-      places += __popcll(__ballot(place));
-      movers += __popcll(__ballot(mover));
-    });
-  if (lane == 0) {
-    wsum[1][wave] = places;
-    wsum[2][wave] = movers;
-  }
-  __syncthreads();
-  int32_t place_at = 0, mover_at = 0, moves = 0;
-  for (int x = 0; x < SW; ++x) {
-    if (x < wave) {
-      place_at += wsum[1][x];
-      mover_at += wsum[2][x];
+    for (int32_t part = 0; part < n; part += PART) {
+      if (several) load_keys(part);
+      const int32_t t = part + tid * KPT;
+      uint32_t goes = 0;
+#pragma unroll
+      for (int i = 0; i < KPT; ++i)   // 0 wraps: it is no candidate
+        goes |= keys[i] - 1u < prefix - (all_ties ? 0u : 1u) ? 1u << i : 0u;
+      if (!all_ties) {   // the same for the whole workgroup
+        uint32_t tie = 0;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) tie |= keys[i] == prefix ? 1u << i : 0u;
+        uint32_t all;
+        int32_t ordinal = seen + (int32_t)before_me(__popc(tie), sums, all);
+        seen += (int32_t)all;
+        for (; tie != 0 && ordinal <= rank; ++ordinal) {
+          goes |= tie & -tie;
+          tie &= tie - 1;
+        }
+      }
+      // of this thread's KPT bits, those below the new length and those of the sequence
+      const auto first = [&](int32_t count) {
+        return count >= KPT ? (uint32_t)(((uint64_t)1 << KPT) - 1) : count <= 0 ? 0u : (1u << count) - 1u;
+      };
+      const uint32_t place = goes & first(left - t), mover = ~goes & ~first(left - t) & first(n - t);
+      // both counts of a part (at most 2^15 each) in one sum
+      static_assert(PART <= 1 << 15, "halves of 16 bits");
+      uint32_t all;
+      const uint32_t at = before_me((uint32_t)__popc(mover) << 16 | (uint32_t)__popc(place), sums, all);
+      int32_t pa = places + (int32_t)(at & 0xffffu), ma = movers + (int32_t)(at >> 16);
+      places += (int32_t)(all & 0xffffu);
+      movers += (int32_t)(all >> 16);
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) {
+        if (place >> i & 1) to[pa++] = t + i;
+        if (mover >> i & 1) from[ma++] = t + i;
+      }
+      if (!FUSED && KPT >= 16 && t < n) {
+        // the free places' bits, 16 to a store
+#pragma unroll
+        for (int i = 0; i < KPT; i += 16)
+          gst<uint16_t>(ml.gone + b * ml.words + t / 16 + i / 16, (uint16_t)(place >> i));
+      }
     }
-    moves += wsum[1][x];
-  }
-  int32_t* to = ml.to + b * ml.cap;
-  int32_t* from = ml.from + b * ml.cap;
-  // the lists, and the totals and positions of what stays where it is
-  const auto stay = [&](int32_t t, float x) {
-    if (hand_on) gst<float>(tot_out + t, x);
-    if (hand_pos) gst<int64_t>(pos_out + t, gld<int64_t>(pos + t));
-  };
-  if (gone_n > 0)
-    walk([&](int32_t t, bool in, bool place, bool mover, float x) {
-      const uint64_t pm = __ballot(place), mm = __ballot(mover);
-      if (place) gst<int32_t>(to + place_at + lanes_below(pm), t);
-      else if (in && t < left) stay(t, x);
-      if (mover) gst<int32_t>(from + mover_at + lanes_below(mm), t);
-      place_at += __popcll(pm);
-      mover_at += __popcll(mm);
-    });
-  else if (hand_on || hand_pos)
-    each([&](int32_t t, bool in, uint32_t, bool, float x) {
-      if (in) stay(t, x);
-    });
+  const int32_t moves = places;
+  // totals and positions of all places: the free ones' are overwritten after the barrier
+  if (FUSED && (p.totals_out != p.totals || (pos && p.pos_out != p.pos)))
+    for (int32_t t = tid; t < left; t += 4 * ST) {
+      float x[4];
+      int64_t y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int32_t u = t + i * ST < left ? t + i * ST : left - 1;
+        x[i] = gld<float>(tot + u);
+        y[i] = pos ? gld<int64_t>(pos + u) : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int32_t u = t + i * ST;
+        if (u >= left) continue;
+        gst<float>(tot_out + u, x[i]);
+        if (pos) gst<int64_t>(pos_out + u, y[i]);
+      }
+    }
   __threadfence_block();
   __syncthreads();
   for (int32_t j = tid; j < moves; j += ST) {
@@ -284,17 +318,36 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
     if (pos) gst<int64_t>(pos_out + d, gld<int64_t>(pos + s));
   }
   if (tid == 0) {
-    ml.count[b] = moves;
+    if (!FUSED) ml.count[b] = moves;
     gst<int64_t>(p.len_out + b, left);
   }
-  if constexpr (FUSED) copy_moves<1>(p, cs, b, to, from, moves, tid, ST);
+  if constexpr (FUSED) copy_moves<1>(p, cs, b, to, from, moves, tid >> 6, SW);
 }
 
-// The moved rows of sequence blockIdx.x.
-__global__ __launch_bounds__(CT) void evict_copy_kernel(EvictParams p, MoveLists ml, CopyShape cs) {
-  const int64_t b = blockIdx.x;
-  copy_moves<2>(p, cs, b, ml.to + b * ml.cap, ml.from + b * ml.cap, ml.count[b],
-                blockIdx.y * CT + threadIdx.x, gridDim.y * CT);
+// `per` workgroups for each sequence: the first `hand` hand on the totals and positions of what stays
+// where it is, 4 * CT each; the others copy the moved rows.
+__global__ __launch_bounds__(CT) void evict_copy_kernel(EvictParams p, MoveLists ml, CopyShape cs,
+                                                        int32_t per, FastDiv div, int32_t hand) {
+  const int32_t seq = fdiv(blockIdx.x, div), y = (int32_t)blockIdx.x - seq * per;
+  const int64_t b = seq;
+  if (y >= hand) {
+    copy_moves<2>(p, cs, b, ml.to + b * ml.cap, ml.from + b * ml.cap, ml.count[b],
+                  (y - hand) * (CT / 64) + (threadIdx.x >> 6), (per - hand) * (CT / 64));
+    return;
+  }
+  const int64_t len = gld<int64_t>(p.len_out + b);
+  const int32_t left = (int32_t)len, moves = ml.count[b];
+  const float* tot = p.totals + b * p.ldt;
+  const int64_t* pos = p.pos ? p.pos + b * p.ldt : nullptr;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int32_t t = (y * 4 + i) * CT + threadIdx.x;
+    if (t >= left) continue;
+    // (a sequence without moves has no bits; the free places' values come from the selection)
+    if (moves > 0 && gld<uint16_t>(ml.gone + b * ml.words + t / 16) >> (t & 15) & 1) continue;
+    gst<float>(p.totals_out + b * p.ldt + t, gld<float>(tot + t));
+    if (pos) gst<int64_t>(p.pos_out + b * p.ldt + t, gld<int64_t>(pos + t));
+  }
 }
 
 // Most moves of a sequence: no more than leave, and no more than stay below the new length.
@@ -303,44 +356,57 @@ int64_t move_cap(const EvictParams& p) {
   return gone < p.max_len / 2 ? gone : p.max_len / 2;
 }
 
+// Words of 16 bits of a sequence: a thread writes all of its own, up to 32 positions.
+int64_t gone_words(const EvictParams& p) { return (p.max_len + 31) / 32 * 2; }
+
 }  // namespace
 
-int64_t evict_work_floats(const EvictParams& p) { return p.n_seqs * (2 * move_cap(p) + 1); }
+int64_t evict_work_floats(const EvictParams& p) {
+  return p.n_seqs * (2 * move_cap(p) + 1 + gone_words(p) / 2);
+}
 
 hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   MoveLists ml;
   ml.cap = move_cap(p);
+  ml.words = gone_words(p);
   ml.count = reinterpret_cast<int32_t*>(work);
   ml.to = ml.count + p.n_seqs;
   ml.from = ml.to + p.n_seqs * ml.cap;
+  ml.gone = reinterpret_cast<uint16_t*>(ml.from + p.n_seqs * ml.cap);
   CopyShape cs;
-  const int64_t bytes = (int64_t)p.d * p.es;
-  cs.n_chunks = (int32_t)((bytes + 15) / 16);
-  cs.chunks = FastDiv(cs.n_chunks);
+  const int32_t bytes = p.d * p.es;
+  cs.unit = bytes >= 16 ? 16 : 2;
+  cs.units = (bytes + cs.unit - 1) / cs.unit;
+  cs.lanes = 1;
+  while (cs.lanes < cs.units && cs.lanes < 64) cs.lanes *= 2;
   cs.heads = FastDiv(p.kv_heads);
-  const int64_t chunks = ml.cap * p.kv_heads * cs.n_chunks;   // of a sequence's moves
-  if (p.n_seqs > 0x7fffffff || chunks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  // A chunk or two per thread of the selecting workgroup: no second launch (32 sequences that lose one
-  // position: 12 us so, 17 with the copy of its own).
-  const bool fused = chunks <= 2 * ST;
+  const int64_t rows = ml.cap * p.kv_heads, chunks = rows * cs.units;   // of a sequence's moves
+  if (p.n_seqs > 0x7fffffff || rows > (1 << 30)) return hipErrorInvalidConfiguration;
+  const bool in_place = p.totals_out == p.totals && p.pos_out == p.pos;
+  // A chunk or two per thread of the selecting workgroup, and totals that stay where they are or are few:
+  // no second launch (32 sequences of 2049 that lose one position: 10.4 us so, 16.4 with a copy of its
+  // own; one of 32768, handed on: FILL so, FILL with the copy's workgroups).
+  const bool fused = chunks <= FUSED_CHUNKS && (in_place || p.max_len <= 4 * ST);
   const dim3 grid((uint32_t)p.n_seqs);
 #define TPP_SELECT(KPT, FUSED)                                                                    \
   hipLaunchKernelGGL((evict_select_kernel<KPT, FUSED>), grid, dim3(ST), 0, stream, p, ml, cs)
-#define TPP_SELECT_KPT(FUSED)                                 \
-  if (p.max_len <= 4 * ST) TPP_SELECT(4, FUSED);              \
-  else if (p.max_len <= 16 * ST) TPP_SELECT(16, FUSED);       \
-  else if (p.max_len <= 32 * ST) TPP_SELECT(32, FUSED);       \
-  else TPP_SELECT(0, FUSED)
   if (fused) {
-    TPP_SELECT_KPT(true);
+    if (p.max_len <= 4 * ST) TPP_SELECT(4, true);
+    else if (p.max_len <= 16 * ST) TPP_SELECT(16, true);
+    else TPP_SELECT(32, true);
   } else {
-    TPP_SELECT_KPT(false);
-    const int64_t want = (chunks + 2 * CT - 1) / (2 * CT);   // two chunks per thread, at most 2048 groups
+    if (p.max_len <= 16 * ST) TPP_SELECT(16, false);
+    else TPP_SELECT(32, false);
+    // two rows per set of lanes, at most 2048 workgroups
+    const int64_t want = (rows * cs.lanes + 2 * CT - 1) / (2 * CT);
     const int64_t most = 2048 / p.n_seqs > 0 ? 2048 / p.n_seqs : 1;
-    hipLaunchKernelGGL(evict_copy_kernel, dim3((uint32_t)p.n_seqs, (uint32_t)(want < most ? want : most)),
-                       dim3(CT), 0, stream, p, ml, cs);
+    const int64_t hand = in_place ? 0 : (p.max_len + 4 * CT - 1) / (4 * CT);
+    const int64_t per = hand + (want < most ? want : most);
+    if (per * p.n_seqs > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (per > 0)
+      hipLaunchKernelGGL(evict_copy_kernel, dim3((uint32_t)(per * p.n_seqs)), dim3(CT), 0, stream, p, ml,
+                         cs, (int32_t)per, FastDiv(per), (int32_t)hand);
   }
-#undef TPP_SELECT_KPT
 #undef TPP_SELECT
   return hipGetLastError();
 }

@@ -1261,8 +1261,8 @@ tpp_status tpp_cache_evict(const tpp_kv_cache* cache, int64_t n_seqs, int64_t ma
     return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
   const hipError_t e = tpp::launch_evict(p, work, static_cast<hipStream_t>(stream));
   if (e == hipErrorInvalidConfiguration)
-    return fail(TPP_ERR_UNSUPPORTED, "eviction needs more than 2^31 - 1 workgroups, or 16-byte chunks of "
-                "one sequence's moves");
+    return fail(TPP_ERR_UNSUPPORTED, "eviction needs more than 2^31 - 1 workgroups, or 2^30 rows for one "
+                "sequence's moves");
   return launched("eviction", e);
 }
 
