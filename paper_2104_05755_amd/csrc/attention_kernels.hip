@@ -105,10 +105,12 @@ struct AttnPlan {
   int32_t splits;     // spans of a sequence
   int32_t group;      // query heads of a key head
   int32_t tiles;      // query-head tiles of a key head
-  FastDiv div_splits, div_tiles, div_y;   // splits, tiles, kv_heads * tiles
+  FastDiv div_seqs, div_tiles, div_y;   // n_seqs, tiles, kv_heads * tiles
   // Partial results (null: the workgroup writes the outputs): sums [row][split][D], then maxima and
-  // sums of weights [row][split], row = sequence * q_heads + head; scores [row][max_len] for totals.
+  // sums of weights [row][split], row = sequence * q_heads + head; scores [row][score_ld] for totals, and a row that
+  // takes what no query head's lanes store.
   float *o, *m, *l, *s;
+  int64_t score_ld;   // of a row of scores: max_len in whole tiles
 };
 
 // The kernel's shapes by type: keys of a tile, entries of a key step and of a lane's chunk of it.
@@ -121,8 +123,9 @@ struct Shape {
   static constexpr int VKEYS = 4 * SUB;     // keys whose values a lane loads
 };
 
-// DP: entries of a head the instance covers (D <= DP); TAIL: D < DP; NT: tiles of 16 query heads.
-template <bool BF16, int DP, bool TAIL, int NT>
+// DP: entries of a head the instance covers (D <= DP); TAIL: D < DP; NT: tiles of 16 query heads; TOTALS:
+// the scores are kept.
+template <bool BF16, int DP, bool TAIL, int NT, bool TOTALS>
 __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   using S = Shape<BF16>;
   constexpr int ES = BF16 ? 2 : 4;
@@ -140,8 +143,11 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, grp = lane >> 4;
-  const int32_t by = fdiv(blockIdx.x, pl.div_splits), split = (int32_t)blockIdx.x - by * pl.splits;
-  const int32_t seq = fdiv(by, pl.div_y), y = by - seq * p.kv_heads * pl.tiles;
+  // Heads first, then sequences, spans last: workgroups go to the 8 XCDs in turn, and with the spans first
+  // the XCD of the first ones had work of every sequence, the last one's only of the longest (64 sequences
+  // of 1 to 8192: 293 us).
+  const int32_t by = fdiv(blockIdx.x, pl.div_y), y = (int32_t)blockIdx.x - by * p.kv_heads * pl.tiles;
+  const int32_t split = fdiv(by, pl.div_seqs), seq = by - split * (int32_t)p.n_seqs;
   const int32_t hk = fdiv(y, pl.div_tiles), ht = y - hk * pl.tiles;
   const int64_t b = seq;
   const int32_t D = TAIL ? p.d : DP;
@@ -211,6 +217,131 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   }
   const float sl2 = p.scale * LOG2E;
 
+  // Where this lane's scores go: the row of its query head, or a row of nobody's.  (A branch around the
+  // stores, or around the next loads, would make the waits below wait for everything in flight.)
+  float* score[NT];
+  if constexpr (TOTALS)
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+      const int64_t row = q * 16 + col < nq ? b * p.q_heads + h0 + q * 16 + col : p.n_seqs * p.q_heads;
+      score[q] = pl.s + row * pl.score_ld + grp * 4;
+    }
+
+  // The tile at i0 of the block at t0, whose loads have been issued; MORE: issues the next one's, the keys'
+  // as soon as the first product has read theirs, the values' after the second, so that one of the two is
+  // always in flight.
+  const auto tile = [&](auto more, int32_t t0, int32_t i0, int32_t next) {
+    constexpr bool MORE = decltype(more)::value;
+    float sc[NT][VKEYS];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      f32x4 st[NT];
+#pragma unroll
+      for (int q = 0; q < NT; ++q) st[q] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < NK; ++s) {
+        u32x4 a = kf[u][s];
+        if constexpr (TAIL) {
+          const int32_t e = s * S::STEP + grp * CH, over = e > D - CH ? e - (D - CH) : 0;
+          a = BF16 ? shift_down(a, over < 8 ? over : 8) : shift_dwords(a, over < 4 ? over : 4);
+        }
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+          if constexpr (BF16) {
+            st[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                            __builtin_bit_cast(bf16x8, qf[q][s]),
+                                                            st[q], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              st[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]),
+                                                           __uint_as_float(qf[q][s][e]), st[q], 0, 0, 0);
+          }
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < NT; ++q)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          sc[q][u * 4 + r] = (masks >> (u * 4 + r)) & 1 ? -INFINITY : st[q][r] * sl2;
+    }
+    if constexpr (MORE) load_k(next);   // behind the products that read the registers
+    __builtin_amdgcn_sched_barrier(0);
+
+    if constexpr (TOTALS) {   // the scores
+#pragma unroll
+      for (int q = 0; q < NT; ++q)
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+          gst<f32x4_a4>(score[q] + t0 + i0 + u * 16,
+                        (f32x4){sc[q][4 * u], sc[q][4 * u + 1], sc[q][4 * u + 2], sc[q][4 * u + 3]});
+    }
+    // ---- softmax: the maximum over the tile, the sums so far scaled down to it ------------------
+    u32x4 hi[NT], lw[NT];
+    float pr[NT][VKEYS];
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+      float top = sc[q][0];
+#pragma unroll
+      for (int k = 1; k < VKEYS; ++k) top = fmaxf(top, sc[q][k]);
+      top = fmaxf(m[q], groups_max(top));
+      const float base = top == -INFINITY ? 0.0f : top;
+      const float down = __builtin_amdgcn_exp2f(m[q] - base);
+      m[q] = top;
+      l[q] *= down;
+#pragma unroll
+      for (int k = 0; k < VKEYS; ++k) {
+        pr[q][k] = __builtin_amdgcn_exp2f(sc[q][k] - base);
+        l[q] += pr[q][k];
+      }
+#pragma unroll
+      for (int j = 0; j < NV * VC; ++j) acc[q][j] *= down;
+      if constexpr (BF16) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float a = pr[q][2 * k], c = pr[q][2 * k + 1];
+          const uint32_t h = pack_bf16x2(a, c);
+          hi[q][k] = h;
+          lw[q][k] = pack_bf16x2(a - __uint_as_float(h << 16), c - __uint_as_float(h & 0xffff0000u));
+        }
+      }
+    }
+    // ---- the values -----------------------------------------------------------------------------
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+      if constexpr (BF16) {
+#pragma unroll
+        for (int j = 0; j < VC; ++j) {
+          // entry j of the chunks of 8 keys, two keys a dword
+          u32x4 a;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            a[k] = __builtin_amdgcn_perm(vf[2 * k + 1][c][j / 2], vf[2 * k][c][j / 2],
+                                         j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int q = 0; q < NT; ++q) {
+            f32x4& o = acc[q][c * VC + j];
+            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                        __builtin_bit_cast(bf16x8, hi[q]), o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                        __builtin_bit_cast(bf16x8, lw[q]), o, 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < VC; ++j)
+#pragma unroll
+          for (int k = 0; k < VKEYS; ++k)
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+              acc[q][c * VC + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                  __uint_as_float(vf[k][c][j]), pr[q][k], acc[q][c * VC + j], 0, 0, 0);
+      }
+    }
+    if constexpr (MORE) load_v(next);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
   constexpr int32_t step = AW * KEYS, NONE = 0x7fffffff;
   for (int32_t t0 = c0; t0 < c1; t0 += BLOCK) {
     // ---- addresses of the block's rows --------------------------------------------------------------
@@ -238,125 +369,8 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
     if (i0 < cnt) {
       load_k(i0);
       load_v(i0);
-      for (;;) {
-        const int32_t next = i0 + step < cnt ? i0 + step : -1;   // the same for the whole wavefront
-        float sc[NT][VKEYS];
-#pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-          f32x4 st[NT];
-#pragma unroll
-          for (int q = 0; q < NT; ++q) st[q] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int s = 0; s < NK; ++s) {
-            u32x4 a = kf[u][s];
-            if constexpr (TAIL) {
-              const int32_t e = s * S::STEP + grp * CH, over = e > D - CH ? e - (D - CH) : 0;
-              a = BF16 ? shift_down(a, over < 8 ? over : 8) : shift_dwords(a, over < 4 ? over : 4);
-            }
-#pragma unroll
-            for (int q = 0; q < NT; ++q) {
-              if constexpr (BF16) {
-                st[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                                __builtin_bit_cast(bf16x8, qf[q][s]),
-                                                                st[q], 0, 0, 0);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  st[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]),
-                                                               __uint_as_float(qf[q][s][e]), st[q], 0, 0, 0);
-              }
-            }
-          }
-#pragma unroll
-          for (int q = 0; q < NT; ++q)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              sc[q][u * 4 + r] = (masks >> (u * 4 + r)) & 1 ? -INFINITY : st[q][r] * sl2;
-        }
-        if (next >= 0) load_k(next);   // behind the products that read the registers
-        __builtin_amdgcn_sched_barrier(0);
-
-        if (pl.s) {   // the scores, for the totals
-#pragma unroll
-          for (int q = 0; q < NT; ++q) {
-            const int32_t h = q * 16 + col;
-            if (h < nq) {
-              float* to = pl.s + (b * p.q_heads + h0 + h) * p.max_len;
-#pragma unroll
-              for (int k = 0; k < VKEYS; ++k) {
-                const int32_t t = t0 + i0 + (k >> 2) * 16 + grp * 4 + (k & 3);
-                if (t < n) gst<float>(to + t, sc[q][k]);
-              }
-            }
-          }
-        }
-        // ---- softmax: the maximum over the tile, the sums so far scaled down to it ------------------
-        u32x4 hi[NT], lw[NT];
-        float pr[NT][VKEYS];
-#pragma unroll
-        for (int q = 0; q < NT; ++q) {
-          float top = sc[q][0];
-#pragma unroll
-          for (int k = 1; k < VKEYS; ++k) top = fmaxf(top, sc[q][k]);
-          top = fmaxf(m[q], groups_max(top));
-          const float base = top == -INFINITY ? 0.0f : top;
-          const float down = __builtin_amdgcn_exp2f(m[q] - base);
-          m[q] = top;
-          l[q] *= down;
-#pragma unroll
-          for (int k = 0; k < VKEYS; ++k) {
-            pr[q][k] = __builtin_amdgcn_exp2f(sc[q][k] - base);
-            l[q] += pr[q][k];
-          }
-#pragma unroll
-          for (int j = 0; j < NV * VC; ++j) acc[q][j] *= down;
-          if constexpr (BF16) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float a = pr[q][2 * k], c = pr[q][2 * k + 1];
-              const uint32_t h = pack_bf16x2(a, c);
-              hi[q][k] = h;
-              lw[q][k] = pack_bf16x2(a - __uint_as_float(h << 16), c - __uint_as_float(h & 0xffff0000u));
-            }
-          }
-        }
-        // ---- the values -----------------------------------------------------------------------------
-#pragma unroll
-        for (int c = 0; c < NV; ++c) {
-          if constexpr (BF16) {
-#pragma unroll
-            for (int j = 0; j < VC; ++j) {
-              // entry j of the chunks of 8 keys, two keys a dword
-              u32x4 a;
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                a[k] = __builtin_amdgcn_perm(vf[2 * k + 1][c][j / 2], vf[2 * k][c][j / 2],
-                                             j & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-              for (int q = 0; q < NT; ++q) {
-                f32x4& o = acc[q][c * VC + j];
-                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                            __builtin_bit_cast(bf16x8, hi[q]), o, 0, 0, 0);
-                o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                            __builtin_bit_cast(bf16x8, lw[q]), o, 0, 0, 0);
-              }
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < VC; ++j)
-#pragma unroll
-              for (int k = 0; k < VKEYS; ++k)
-#pragma unroll
-                for (int q = 0; q < NT; ++q)
-                  acc[q][c * VC + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                      __uint_as_float(vf[k][c][j]), pr[q][k], acc[q][c * VC + j], 0, 0, 0);
-          }
-        }
-        if (next < 0) break;
-        load_v(next);
-        __builtin_amdgcn_sched_barrier(0);
-        i0 = next;
-      }
+      for (; i0 + step < cnt; i0 += step) tile(std::true_type(), t0, i0, i0 + step);
+      tile(std::false_type(), t0, i0, 0);
     }
   }
 
@@ -503,7 +517,7 @@ __global__ __launch_bounds__(AT) void attn_join_kernel(AttnParams p, AttnPlan pl
     const int32_t heads = p.q_heads - hb < AT ? p.q_heads - hb : AT;
     if (held)
       for (int32_t h = 0; h < heads; ++h) {
-        const float s = gld<float>(pl.s + (b * p.q_heads + hb + h) * p.max_len + t);
+        const float s = gld<float>(pl.s + (b * p.q_heads + hb + h) * pl.score_ld + t);
         total += __builtin_amdgcn_exp2f(s - lse[h]);
       }
   }
@@ -534,7 +548,8 @@ AttnPlan plan(const AttnParams& p, bool split) {
   if (!split) span = range < step ? step : (range + step - 1) / step * step;
   pl.span = (int32_t)span;
   pl.splits = range > span ? (int32_t)((range + span - 1) / span) : 1;
-  pl.div_splits = FastDiv(pl.splits);
+  pl.score_ld = (p.max_len + 31) / 32 * 32;
+  pl.div_seqs = FastDiv(p.n_seqs);
   pl.div_tiles = FastDiv(pl.tiles);
   pl.div_y = FastDiv((int64_t)p.kv_heads * pl.tiles);
   return pl;
@@ -542,10 +557,16 @@ AttnPlan plan(const AttnParams& p, bool split) {
 
 template <bool BF16, int DP, int NT>
 void launch_tail(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t bytes, hipStream_t stream) {
-  if (p.d < DP)
-    hipLaunchKernelGGL((attn_kernel<BF16, DP, true, NT>), grid, dim3(AT), bytes, stream, p, pl);
-  else
-    hipLaunchKernelGGL((attn_kernel<BF16, DP, false, NT>), grid, dim3(AT), bytes, stream, p, pl);
+#define TPP_ATTN(TAIL, TOTALS) \
+  hipLaunchKernelGGL((attn_kernel<BF16, DP, TAIL, NT, TOTALS>), grid, dim3(AT), bytes, stream, p, pl)
+  if (p.d < DP) {
+    if (pl.s) TPP_ATTN(true, true);
+    else TPP_ATTN(true, false);
+  } else {
+    if (pl.s) TPP_ATTN(false, true);
+    else TPP_ATTN(false, false);
+  }
+#undef TPP_ATTN
 }
 
 template <bool BF16, int NT>
@@ -561,7 +582,7 @@ int64_t attn_work_floats(const AttnParams& p) {
   const AttnPlan pl = plan(p, true);
   if (pl.splits == 1 && !p.totals_out) return 0;
   const int64_t rows = p.n_seqs * p.q_heads;
-  return rows * pl.splits * (p.d + 2) + (p.totals_out ? rows * p.max_len : 0);
+  return rows * pl.splits * (p.d + 2) + (p.totals_out ? (rows + 1) * pl.score_ld : 0);
 }
 
 hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
