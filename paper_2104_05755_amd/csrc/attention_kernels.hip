@@ -105,7 +105,7 @@ struct AttnPlan {
   int32_t splits;     // spans of a sequence
   int32_t group;      // query heads of a key head
   int32_t tiles;      // query-head tiles of a key head
-  FastDiv div_seqs, div_tiles, div_y;   // n_seqs, tiles, kv_heads * tiles
+  FastDiv div_splits, div_seqs, div_tiles, div_y;   // n_seqs, tiles, kv_heads * tiles
   // Partial results (null: the workgroup writes the outputs): sums [row][split][D], then maxima and
   // sums of weights [row][split], row = sequence * q_heads + head; scores [row][score_ld] for totals, and a row that
   // takes what no query head's lanes store.
@@ -132,25 +132,32 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   constexpr int KEYS = S::KEYS, CH = S::CH, SUB = S::SUB, VKEYS = S::VKEYS;
   constexpr int NK = DP / S::STEP;                   // steps of the first product
   constexpr int VC = BF16 && DP > 64 ? 8 : 4;        // entries of a lane's chunk of a value
-  constexpr int NV = DP / (16 * VC);                 // chunks
+  constexpr int NV = (DP + 16 * VC - 1) / (16 * VC); // chunks
+  constexpr bool OVER = TAIL || DP % (16 * VC) != 0; // lanes past the last entry take the last chunk
   typedef typename std::conditional<VC * ES == 16, u32x4, u32x2>::type vchunk;
   typedef typename std::conditional<VC * ES == 16, u32x4_a2, u32x2_a2>::type vchunk_any;
 
   extern __shared__ __align__(16) char lds[];
   int64_t* rows = reinterpret_cast<int64_t*>(lds);   // byte offset of each position, bit 0: masked
+  __shared__ int32_t missing;   // 1 + the first position of the last block that lacks a page
   __shared__ int32_t first_held;
   __shared__ float wave_m[AW][NT * 16], wave_l[AW][NT * 16];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, grp = lane >> 4;
-  // Heads first, then sequences, spans last: workgroups go to the 8 XCDs in turn, and with the spans first
-  // the XCD of the first ones had work of every sequence, the last one's only of the longest (64 sequences
-  // of 1 to 8192: 293 us).
-  const int32_t by = fdiv(blockIdx.x, pl.div_y), y = (int32_t)blockIdx.x - by * p.kv_heads * pl.tiles;
-  const int32_t split = fdiv(by, pl.div_seqs), seq = by - split * (int32_t)p.n_seqs;
+  // Spans first, each sequence's from another one on, then sequences, heads last.  Workgroups go to the 8
+  // XCDs in turn: with every sequence's first span on the same XCD, the others had only the work of long
+  // sequences (64 of 1 to 8192: 293 us so, 234 turned).  With the heads first, which is even too (231), the
+  // interleaved rows of the heads are read at once, at a lower rate (64 of 4096: 211 us, 202 so; 32 of 2049
+  // to 4096 with totals 114 and 109).
+  const int32_t ys = fdiv(blockIdx.x, pl.div_splits), sp = (int32_t)blockIdx.x - ys * pl.splits;
+  const int32_t y = fdiv(ys, pl.div_seqs), seq = ys - y * (int32_t)p.n_seqs;
+  const int32_t from = seq - fdiv(seq, pl.div_splits) * pl.splits;
+  const int32_t split = sp + from >= pl.splits ? sp + from - pl.splits : sp + from;
   const int32_t hk = fdiv(y, pl.div_tiles), ht = y - hk * pl.tiles;
   const int64_t b = seq;
   const int32_t D = TAIL ? p.d : DP;
+  if (tid == 0) missing = 0;
   const int32_t n = length_of(p, b);
   const int32_t lo = window_start(p, n);
   const int32_t c0 = lo / KEYS * KEYS + split * pl.span;   // this span: [c0, c1)
@@ -201,7 +208,7 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 #pragma unroll
       for (int c = 0; c < NV; ++c) {
         const int32_t e = (c * 16 + col) * VC;
-        vf[k][c] = gld<vchunk_any>(vb + (row & ~int64_t(1)) + (TAIL && e > D - VC ? D - VC : e) * ES);
+        vf[k][c] = gld<vchunk_any>(vb + (row & ~int64_t(1)) + (OVER && e > D - VC ? D - VC : e) * ES);
       }
     }
   };
@@ -345,24 +352,32 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   constexpr int32_t step = AW * KEYS, NONE = 0x7fffffff;
   for (int32_t t0 = c0; t0 < c1; t0 += BLOCK) {
     // ---- addresses of the block's rows --------------------------------------------------------------
+    // A position outside the span's or the window's gets the row of the nearest one inside, masked.  Where
+    // pages hold nothing, the first position that is held stands in for those that are not.
     const int32_t cnt = c1 - t0 < BLOCK ? (c1 - t0 + KEYS - 1) / KEYS * KEYS : BLOCK;
     __syncthreads();   // the block before is done with
-    if (tid == 0) first_held = NONE;
-    __syncthreads();
-    int32_t mine = NONE;
     for (int32_t i = tid; i < cnt; i += AT) {
-      const int32_t t = t0 + i;
-      const int64_t row = t >= lo && t < c1 ? row_of(p, b, t) : -1;
-      if (row >= 0 && mine == NONE) mine = i;
-      rows[i] = row < 0 ? -1 : row * ES;
+      const int32_t t = t0 + i, in = t < lo ? lo : t < c1 ? t : c1 - 1;
+      const int64_t row = row_of(p, b, in);
+      if (row < 0) missing = t0 + 1;
+      rows[i] = row < 0 ? -1 : row * ES | (in != t);
     }
-    if (mine != NONE) atomicMin(&first_held, mine);
     __syncthreads();
-    if (first_held == NONE) continue;   // the same for the whole workgroup
-    const int64_t safe = rows[first_held] | 1;
-    for (int32_t i = tid; i < cnt; i += AT)
-      if (rows[i] < 0) rows[i] = safe;
-    __syncthreads();
+    if (missing == t0 + 1) {   // the same for the whole workgroup
+      if (tid == 0) first_held = NONE;
+      __syncthreads();
+      int32_t mine = NONE;
+      for (int32_t i = tid; i < cnt && mine == NONE; i += AT)
+        if (rows[i] >= 0) mine = i;
+      if (mine != NONE) atomicMin(&first_held, mine);
+      __syncthreads();
+      if (first_held == NONE) continue;   // the same for the whole workgroup
+      const int64_t safe = rows[first_held] | 1;
+      __syncthreads();
+      for (int32_t i = tid; i < cnt; i += AT)
+        if (rows[i] < 0) rows[i] = safe;
+      __syncthreads();
+    }
 
     // ---- its tiles ----------------------------------------------------------------------------------
     int32_t i0 = wave * KEYS;
@@ -400,7 +415,7 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int32_t e = (c * 16 + grp * 4 + r) * VC;
-          float* to = part + (wave * ng + h) * D + (TAIL && e > D - VC ? D - VC : e);
+          float* to = part + (wave * ng + h) * D + (OVER && e > D - VC ? D - VC : e);
 #pragma unroll
           for (int j = 0; j < VC; ++j) to[j] = acc[q][c * VC + j][r] * down;
         }
@@ -435,13 +450,13 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 }
 
 // The spans' partial results joined: the first `rows` workgroups a (sequence, query head) each, whose
-// wavefronts take the spans in turn; the others, with totals, 256 positions of a sequence each.
-// NE: entries of a lane.
-template <int NE>
-__global__ __launch_bounds__(AT) void attn_join_kernel(AttnParams p, AttnPlan pl, int32_t rows,
+// wavefronts take the spans in turn; the others, with totals, a position of a sequence to a thread.
+// NE: entries of a lane; JW: wavefronts.
+template <int NE, int JW>
+__global__ __launch_bounds__(JW * 64) void attn_join_kernel(AttnParams p, AttnPlan pl, int32_t rows,
                                                        int32_t blocks, int32_t keys) {
-  __shared__ float lse[AT];
-  __shared__ float part[AW][NE * 64];
+  __shared__ float lse[JW * 64];
+  __shared__ float part[JW][NE * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if ((int32_t)blockIdx.x < rows) {
     const int64_t row = blockIdx.x;
@@ -461,18 +476,18 @@ __global__ __launch_bounds__(AT) void attn_join_kernel(AttnParams p, AttnPlan pl
       const float f = s0 + lane < used ? share(gld<float>(mm + s0 + lane), top) : 0.0f;
       if (s0 + lane < used) sum += gld<float>(ll + s0 + lane) * f;
       const int32_t end = used - s0 < 64 ? used - s0 : 64;
-      for (int32_t s = wave; s < end; s += JOINED * AW) {   // JOINED spans' rows in flight
+      for (int32_t s = wave; s < end; s += JOINED * JW) {   // JOINED spans' rows in flight
         float x[JOINED][NE];
 #pragma unroll
         for (int u = 0; u < JOINED; ++u)
 #pragma unroll
           for (int i = 0; i < NE; ++i)
-            x[u][i] = s + u * AW < end && lane + 64 * i < p.d
-                          ? gld<float>(pl.o + (row * pl.splits + s0 + s + u * AW) * p.d + lane + 64 * i)
+            x[u][i] = s + u * JW < end && lane + 64 * i < p.d
+                          ? gld<float>(pl.o + (row * pl.splits + s0 + s + u * JW) * p.d + lane + 64 * i)
                           : 0.0f;
 #pragma unroll
         for (int u = 0; u < JOINED; ++u) {
-          const float fs = __shfl(f, (s + u * AW) & 63, 64);   // 0 past the last span
+          const float fs = __shfl(f, (s + u * JW) & 63, 64);   // 0 past the last span
 #pragma unroll
           for (int i = 0; i < NE; ++i) o[i] += x[u][i] * fs;
         }
@@ -484,7 +499,9 @@ __global__ __launch_bounds__(AT) void attn_join_kernel(AttnParams p, AttnPlan pl
     for (int i = 0; i < NE; ++i) part[wave][lane + 64 * i] = o[i];
     __syncthreads();
     if (tid < p.d) {
-      const float v = ((part[0][tid] + part[1][tid]) + part[2][tid]) + part[3][tid];
+      float v = part[0][tid];
+#pragma unroll
+      for (int w = 1; w < JW; ++w) v += part[w][tid];
       store_elem(p.out, b * p.ldo + (int64_t)h * p.d + tid, sum == 0.0f ? 0.0f : v / sum, p.out_bf16);
     }
     if (tid == 0 && p.lse)
@@ -495,12 +512,12 @@ __global__ __launch_bounds__(AT) void attn_join_kernel(AttnParams p, AttnPlan pl
   const int32_t w = (int32_t)blockIdx.x - rows;
   const int64_t b = w / blocks;
   const int32_t n = length_of(p, b), start = window_start(p, n), lo = start / keys * keys;
-  const int32_t t = (w - (int32_t)b * blocks) * AT + tid;
+  const int32_t t = (w - (int32_t)b * blocks) * JW * 64 + tid;
   if (t - tid >= n) return;
   const int32_t used = n > lo ? (n - lo + pl.span - 1) / pl.span : 0;
   const bool held = t < n && t >= start && row_of(p, b, t) >= 0;
   float total = 0.0f;
-  for (int32_t hb = 0; hb < p.q_heads; hb += AT) {
+  for (int32_t hb = 0; hb < p.q_heads; hb += JW * 64) {
     __syncthreads();
     if (hb + tid < p.q_heads) {
       const int64_t at = (b * p.q_heads + hb + tid) * pl.splits;
@@ -514,7 +531,7 @@ __global__ __launch_bounds__(AT) void attn_join_kernel(AttnParams p, AttnPlan pl
       lse[tid] = top + __builtin_amdgcn_logf(sum);
     }
     __syncthreads();
-    const int32_t heads = p.q_heads - hb < AT ? p.q_heads - hb : AT;
+    const int32_t heads = p.q_heads - hb < JW * 64 ? p.q_heads - hb : JW * 64;
     if (held)
       for (int32_t h = 0; h < heads; ++h) {
         const float s = gld<float>(pl.s + (b * p.q_heads + hb + h) * pl.score_ld + t);
@@ -542,14 +559,19 @@ AttnPlan plan(const AttnParams& p, bool split) {
   // positions of a sequence that can count, from a tile's first one on
   const int64_t range = p.window > 0 && p.window < p.max_len ? p.window + keys : p.max_len;
   const int64_t units = p.n_seqs * p.kv_heads * pl.tiles;
-  int64_t span = (range * units / 1024 + step - 1) / step * step;
+  int64_t span = (range * units / 512 + step - 1) / step * step;
   if (span < step) span = step;
   if (span > BLOCK) span = BLOCK;
-  if (!split) span = range < step ? step : (range + step - 1) / step * step;
+  // Few tiles to a sequence: their workgroup is done sooner than a second kernel has joined parts (one
+  // sequence of 512, 8 key heads of 128 bf16: 9.0 us either way, of 256 7.0 and 9.5; fp32 256 10.0 whole and
+  // 9.7; 16 sequences of 1024 bf16 16.1 and 17.8, of 512 fp32 16.3 and 19.3).
+  const bool few = range <= keys * (units >= 128 ? 32 : p.bf16 ? 16 : 8);
+  if (!split || few) span = range < step ? step : (range + step - 1) / step * step;
   pl.span = (int32_t)span;
   pl.splits = range > span ? (int32_t)((range + span - 1) / span) : 1;
   pl.score_ld = (p.max_len + 31) / 32 * 32;
   pl.div_seqs = FastDiv(p.n_seqs);
+  pl.div_splits = FastDiv(pl.splits);
   pl.div_tiles = FastDiv(pl.tiles);
   pl.div_y = FastDiv((int64_t)p.kv_heads * pl.tiles);
   return pl;
@@ -572,7 +594,9 @@ void launch_tail(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t byte
 template <bool BF16, int NT>
 void launch_dim(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t bytes, hipStream_t stream) {
   if (p.d <= 64) launch_tail<BF16, 64, NT>(p, pl, grid, bytes, stream);
+  else if (NT == 1 && p.d <= 96) launch_tail<BF16, 96, 1>(p, pl, grid, bytes, stream);
   else if (NT == 2 || p.d <= 128) launch_tail<BF16, 128, NT>(p, pl, grid, bytes, stream);
+  else if (p.d <= 192) launch_tail<BF16, 192, 1>(p, pl, grid, bytes, stream);
   else launch_tail<BF16, 256, 1>(p, pl, grid, bytes, stream);
 }
 
@@ -588,7 +612,8 @@ int64_t attn_work_floats(const AttnParams& p) {
 hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
   AttnPlan pl = plan(p, work != nullptr);
   const int64_t rows = p.n_seqs * p.q_heads;
-  const int64_t blocks = work && p.totals_out ? (p.max_len + AT - 1) / AT : 0;
+  const int jt = pl.splits > 16 ? 1024 : AT;   // more wavefronts where there are many spans to join
+  const int64_t blocks = work && p.totals_out ? (p.max_len + jt - 1) / jt : 0;
   const int64_t wgs = (int64_t)pl.splits * p.kv_heads * pl.tiles * p.n_seqs;
   const int64_t joins = rows + blocks * p.n_seqs;
   if (p.n_seqs > 0x7fffffff || wgs > 0x7fffffff || joins > 0x7fffffff)
@@ -612,12 +637,16 @@ hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
   if (work) {
     const dim3 jgrid((uint32_t)joins);
     const int32_t keys = p.bf16 ? 32 : 16;
-#define TPP_JOIN(NE)                                                                              \
-  hipLaunchKernelGGL((attn_join_kernel<NE>), jgrid, dim3(AT), 0, stream, p, pl, (int32_t)rows,    \
+#define TPP_JOIN_WAVES(NE, JW)                                                                    \
+  hipLaunchKernelGGL((attn_join_kernel<NE, JW>), jgrid, dim3(JW * 64), 0, stream, p, pl, (int32_t)rows, \
                      (int32_t)blocks, keys)
-    if (p.d <= 64) TPP_JOIN(1);
-    else if (p.d <= 128) TPP_JOIN(2);
-    else TPP_JOIN(4);
+#define TPP_JOIN(NE)                          \
+  if (jt == 1024) TPP_JOIN_WAVES(NE, 16);     \
+  else TPP_JOIN_WAVES(NE, AW)
+    if (p.d <= 64) { TPP_JOIN(1); }
+    else if (p.d <= 128) { TPP_JOIN(2); }
+    else { TPP_JOIN(4); }
+#undef TPP_JOIN_WAVES
 #undef TPP_JOIN
   }
   return hipGetLastError();
