@@ -544,22 +544,32 @@ __global__ __launch_bounds__(JW * 64) void attn_join_kernel(AttnParams p, AttnPl
   }
 }
 
-// Tiles of 16 query heads per workgroup: two read the keys and values once for twice the heads, and have
-// the registers for it up to 128 entries a head.
-int32_t head_tiles(const AttnParams& p) { return p.q_heads / p.kv_heads > 16 && p.d <= 128 ? 2 : 1; }
+// Positions of a sequence that can count, from a tile's first one on.
+int64_t range_of(const AttnParams& p) {
+  return p.window > 0 && p.window < p.max_len ? p.window + (p.bf16 ? 32 : 16) : p.max_len;
+}
 
-// Spans of at most a block where that gives the 256 compute units four workgroups each, down to one tile
-// per wavefront; `split` false: the whole sequence.
+// Tiles of 16 query heads per workgroup.  Two read the keys and values once for twice the heads, and have
+// the registers for it up to 128 entries a head, but one wavefront per SIMD: for more than 16 heads to a
+// key head and 32 MB of cache on (64 heads to one, 64 sequences of 8192: 136 us, 179 with one tile; 16 of
+// 4096 22.2 and 23.2; one sequence of 300, 24 heads to one 12.7 and 9.4).
+int32_t head_tiles(const AttnParams& p) {
+  const int64_t bytes = range_of(p) * p.n_seqs * p.kv_heads * p.d * (p.bf16 ? 4 : 8);
+  return p.q_heads / p.kv_heads > 16 && p.d <= 128 && bytes >= int64_t(32) << 20 ? 2 : 1;
+}
+
+// Spans that give the 256 compute units two workgroups each, as many as have the registers at once (one
+// of two head tiles), between a tile per wavefront and a block; `split` false: the whole sequence.  (Four
+// each: the odd fp32 case 28 us, 22.7 so; spans of two blocks: 64 sequences of 1 to 8192 261 us, 234 so.)
 AttnPlan plan(const AttnParams& p, bool split) {
   AttnPlan pl = {};
   pl.group = p.q_heads / p.kv_heads;
   const int32_t nt = head_tiles(p);
   pl.tiles = (pl.group + 16 * nt - 1) / (16 * nt);
   const int32_t keys = p.bf16 ? 32 : 16, step = AW * keys;
-  // positions of a sequence that can count, from a tile's first one on
-  const int64_t range = p.window > 0 && p.window < p.max_len ? p.window + keys : p.max_len;
+  const int64_t range = range_of(p);
   const int64_t units = p.n_seqs * p.kv_heads * pl.tiles;
-  int64_t span = (range * units / 512 + step - 1) / step * step;
+  int64_t span = (range * units / (nt == 2 ? 256 : 512) + step - 1) / step * step;
   if (span < step) span = step;
   if (span > BLOCK) span = BLOCK;
   // Few tiles to a sequence: their workgroup is done sooner than a second kernel has joined parts (one
