@@ -449,6 +449,9 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   }
 }
 
+// (A join by the last workgroup to finish, with a counter per unit, saves this launch; the releases of its
+// writes to the device cost every workgroup a write-back of its L2: 64 sequences of 1 to 8192 1032 us, 224
+// so, one of 1024 14.3 us and 10.6.)
 // The spans' partial results joined: the first `rows` workgroups a (sequence, query head) each, whose
 // wavefronts take the spans in turn; the others, with totals, a position of a sequence to a thread.
 // NE: entries of a lane; JW: wavefronts.

@@ -6,11 +6,12 @@
 // over its entries and one pass; the backward pass turns the gradient back (the rotation's transpose),
 // u = g w, and needs one more sum, of u xn.  8 (16) operations per entry of 2 or 4 bytes: bound by HBM.
 //
-// Rows of whole 16-byte chunks: a lane has two chunks of a row, placed so that what the rotation turns
-// together is in one lane -- chunks at i and i + rot_dim / 2 in the halves form (behind the rotated part
-// at i and half of the rest on), any two in the pairs form -- and the sums fold over the 4 to 64 lanes
-// of the row by register permutes.  A wavefront has 64 / lanes rows.  Other rows: one per wavefront, a
-// rotated pair or an entry behind the rotated part to a lane, four rows in flight.
+// A lane has two 16-byte chunks of a row, placed so that what the rotation turns together is in one lane --
+// chunks at i and i + rot_dim / 2 in the halves form (behind the rotated part any two), any two in the pairs
+// form -- and the sums fold over the 4 to 64 lanes of the row by register permutes.  A wavefront has
+// 64 / lanes rows.  A part that is no multiple of a chunk ends with the chunk that ends with it, whose first
+// entries another lane counts and stores.  Rows that are too short for that: one per wavefront, a rotated
+// pair or an entry behind the rotated part to a lane, four rows in flight.
 #include <hip/hip_runtime.h>
 
 #include "brgemm_device.h"
@@ -147,22 +148,51 @@ __device__ __forceinline__ void load_floats(const float* p, float (&v)[V]) {
   }
 }
 
-// The first entries a, b of the two chunks of lane c of a row, and whether they are turned (halves).
-__device__ __forceinline__ bool chunks_of(const QkParams& p, int32_t i, int32_t& a, int32_t& b) {
-  if (p.pairs) {
-    a = i;
-    b = p.d / 2 + i;
-    return false;
+// The two chunks of lane c of a row: their first entries, and how many entries of each belong to another
+// lane's chunk as well (a part that is no multiple of V ends with the chunk that ends with it).  `turned`:
+// entry e of one goes with entry e of the other (halves).
+struct Chunks {
+  int32_t a, b, dup_a, dup_b;
+  bool turned;
+};
+// Chunk c of the n >= V entries from `first` on; a chunk past the last is the last again, all of it another's.
+template <int V>
+__device__ __forceinline__ int32_t chunk_at(int32_t first, int32_t n, int32_t c, int32_t& dup) {
+  const int32_t at = c * V < n - V ? c * V : n - V;
+  dup = c * V - at < V ? c * V - at : V;
+  return first + at;
+}
+template <int V, bool WHOLE>
+__device__ __forceinline__ Chunks chunks_of(const QkParams& p, int32_t c) {
+  Chunks k;
+  const int32_t half = p.rot_dim / 2, rest = p.d - p.rot_dim;
+  if constexpr (WHOLE) {
+    const int32_t i = c * V;
+    k.dup_a = k.dup_b = 0;
+    k.turned = !p.pairs && i < half;
+    k.a = p.pairs ? i : k.turned ? i : half + i;
+    k.b = p.pairs ? p.d / 2 + i : k.turned ? half + i : p.rot_dim + rest / 2 + (i - half);
+    return k;
   }
-  const int32_t half = p.rot_dim / 2;
-  if (i < half) {
-    a = i;
-    b = half + i;
-    return true;
+  const int32_t lanes = p.pairs ? 0 : (half + V - 1) / V;   // of the rotated part
+  k.turned = c < lanes;
+  if (k.turned) {
+    k.a = chunk_at<V>(0, half, c, k.dup_a);
+    k.b = half + k.a;
+    k.dup_b = k.dup_a;
+  } else {
+    // two chunks of the rest (pairs: of the row); a rest below V is the end of the row's last chunk
+    const int32_t first = p.pairs ? 0 : p.rot_dim, n = p.d - first, j = 2 * (c - lanes);
+    if (n < V) {
+      k.a = k.b = p.d - V;
+      k.dup_a = V - n;
+      k.dup_b = V;
+    } else {
+      k.a = chunk_at<V>(first, n, j, k.dup_a);
+      k.b = chunk_at<V>(first, n, j + 1, k.dup_b);
+    }
   }
-  a = half + i;
-  b = p.rot_dim + (p.d - p.rot_dim) / 2 + (i - half);
-  return false;
+  return k;
 }
 
 // Cosines and sines of the pairs of a lane's chunks: halves: entry e of both chunks; pairs: pair e / 2
@@ -216,42 +246,73 @@ __device__ __forceinline__ void turn(bool pairs, bool back, const float (&c)[V],
   }
 }
 
-// Whether the rows are whole chunks whose pairs meet in a lane.
-bool chunked(const QkParams& p) {
+// Whether the rows are whole chunks whose pairs meet in a lane, and whether they go by chunks at all: both
+// halves of the rotated part hold one, no pair lies across the border of the last (odd) one, and the chunks
+// fit a wavefront.
+bool whole_chunks(const QkParams& p) {
   const int32_t two = p.bf16 ? 16 : 8;
   return p.d % two == 0 && (p.pairs || p.rot_dim % two == 0);
 }
+// Lanes with chunks of a row.
+int32_t chunk_lanes(const QkParams& p) {
+  const int32_t v = p.bf16 ? 8 : 4;
+  if (whole_chunks(p)) return p.d / (2 * v);
+  const int32_t half = p.pairs ? 0 : p.rot_dim / 2, rest = p.d - 2 * half;
+  return (half + v - 1) / v + ((rest + v - 1) / v + 1) / 2;
+}
+bool chunked(const QkParams& p) {
+  const int32_t v = p.bf16 ? 8 : 4;
+  if (p.d < v || chunk_lanes(p) > 64) return false;
+  return p.pairs ? p.d % 2 == 0 || p.rot_dim <= p.d - v : p.rot_dim == 0 || p.rot_dim >= 2 * v;
+}
 
-template <bool BF16, int LANES>
+template <int V>
+__device__ __forceinline__ float squares(const float (&x)[V], int32_t dup) {
+  float sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) sum += e >= dup ? x[e] * x[e] : 0.0f;
+  return sum;
+}
+// A chunk's entries but those that another lane stores.
+template <bool BF16, bool WHOLE>
+__device__ __forceinline__ void store_own(void* p, int64_t at, const float (&v)[Chunk<BF16>::V], int32_t dup) {
+  if (WHOLE || dup == 0) {
+    store_chunk<BF16>(p, at, v);
+  } else {
+#pragma unroll
+    for (int e = 1; e < Chunk<BF16>::V; ++e)
+      if (e >= dup) store_elem(p, at + e, v[e], BF16);
+  }
+}
+
+template <bool BF16, bool WHOLE, int LANES>
 __global__ __launch_bounds__(QT) void qk_chunk_kernel(QkParams p, int32_t rows, int32_t per_token,
-                                                      FastDiv div) {
+                                                      FastDiv div, int32_t used) {
   constexpr int V = Chunk<BF16>::V;
   const int lane = threadIdx.x & 63;
   const int32_t row = ((int32_t)blockIdx.x * QW + (threadIdx.x >> 6)) * (64 / LANES) + lane / LANES;
-  const int32_t i = (lane % LANES) * V;
+  const int32_t i = lane % LANES;
   if (row >= rows) return;   // whole rows: the folds below stay within one
   const Row r = row_at(p, row, per_token, div);
   if (!r.out) return;
-  const bool in = i < p.d / 2;   // lanes past the row's chunks repeat its first
-  int32_t a, b;
-  const bool turned = chunks_of(p, in ? i : 0, a, b);
+  const bool in = i < used;   // lanes past the row's chunks repeat its first
+  const Chunks k = chunks_of<V, WHOLE>(p, in ? i : 0);
+  const int32_t a = k.a, b = k.b;
   const u32x4 wx = load_chunk<BF16>(r.x, r.from + a), wy = load_chunk<BF16>(r.x, r.from + b);
   if (!r.w) {
-    if (in) {
+    if (in) {   // what two lanes store is the same
       gst<u32x4_a2>(static_cast<char*>(r.out) + (r.to + a) * Chunk<BF16>::ES, wx);
       gst<u32x4_a2>(static_cast<char*>(r.out) + (r.to + b) * Chunk<BF16>::ES, wy);
     }
     return;
   }
   float x[V], y[V], c[V], s[V], wa[V], wb[V];
-  load_angles<V>(p, r.pos, a, b, turned, c, s);
+  load_angles<V>(p, r.pos, a, b, k.turned, c, s);
   load_floats<V>(r.w + a, wa);
   load_floats<V>(r.w + b, wb);
   widen<BF16>(wx, x);
   widen<BF16>(wy, y);
-  float sum = 0.0f;
-#pragma unroll
-  for (int e = 0; e < V; ++e) sum += x[e] * x[e] + y[e] * y[e];
+  const float sum = squares<V>(x, k.dup_a) + squares<V>(y, k.dup_b);
   const float rstd = 1.0f / sqrtf(lanes_sum<LANES>(in ? sum : 0.0f) / (float)p.d + p.eps);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
@@ -260,26 +321,26 @@ __global__ __launch_bounds__(QT) void qk_chunk_kernel(QkParams p, int32_t rows, 
   }
   turn<V>(p.pairs, false, c, s, x, y);
   if (in) {
-    store_chunk<BF16>(r.out, r.to + a, x);
-    store_chunk<BF16>(r.out, r.to + b, y);
+    store_own<BF16, WHOLE>(r.out, r.to + a, x, k.dup_a);
+    store_own<BF16, WHOLE>(r.out, r.to + b, y, k.dup_b);
   }
 }
 
 // Backward.  Workgroup w of a side (the first nq of the queries, the rest of the keys) takes every n-th
 // set of QW * 64 / LANES rows and keeps its part of the weights' gradient in registers; parts go to
 // `part` (a row of D per workgroup), or straight to dw where a side has one workgroup.
-template <bool BF16, int LANES>
-__global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32_t nq, float* part) {
+template <bool BF16, bool WHOLE, int LANES>
+__global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32_t nq, float* part,
+                                                               int32_t used) {
   constexpr int V = Chunk<BF16>::V, SLOTS = 64 / LANES;
   __shared__ float acc[QW][LANES * 2 * V];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool keys = (int32_t)blockIdx.x >= nq;
   const int32_t wg = blockIdx.x - (keys ? nq : 0), n_wg = keys ? (int32_t)gridDim.x - nq : nq;
   const QkSide sd = keys ? p.side[1] : p.side[0];
-  const int32_t i = (lane % LANES) * V;
-  const bool in = i < p.d / 2;
-  int32_t a, b;
-  const bool turned = chunks_of(p, in ? i : 0, a, b);
+  const bool in = lane % LANES < used;
+  const Chunks k = chunks_of<V, WHOLE>(p, in ? lane % LANES : 0);
+  const int32_t a = k.a, b = k.b;
   float wa[V], wb[V], da[V], db[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) wa[e] = wb[e] = da[e] = db[e] = 0.0f;
@@ -302,17 +363,18 @@ __global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32
     const u32x4 xw = load_chunk<BF16>(sd.x, fx + a), yw = load_chunk<BF16>(sd.x, fx + b);
     const u32x4 gw = load_chunk<BF16>(sd.g, fg + a), fw = load_chunk<BF16>(sd.g, fg + b);
     float x[V], y[V], g[V], f[V], c[V], s[V];
-    load_angles<V>(p, held ? pos : -1, a, b, turned, c, s);
+    load_angles<V>(p, held ? pos : -1, a, b, k.turned, c, s);
     widen<BF16>(xw, x);
     widen<BF16>(yw, y);
     widen<BF16>(gw, g);
     widen<BF16>(fw, f);
     turn<V>(p.pairs, true, c, s, g, f);
-    float xx = 0.0f, ux = 0.0f;
+    const float xx = squares<V>(x, k.dup_a) + squares<V>(y, k.dup_b);
+    float ux = 0.0f;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      xx += x[e] * x[e] + y[e] * y[e];
-      ux += g[e] * wa[e] * x[e] + f[e] * wb[e] * y[e];
+      ux += e >= k.dup_a ? g[e] * wa[e] * x[e] : 0.0f;
+      ux += e >= k.dup_b ? f[e] * wb[e] * y[e] : 0.0f;
     }
     const float r = 1.0f / sqrtf(lanes_sum<LANES>(in ? xx : 0.0f) / (float)p.d + p.eps);
     const float m = lanes_sum<LANES>(in ? ux : 0.0f) * r / (float)p.d;   // mean(u xn)
@@ -327,8 +389,8 @@ __global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32
       y[e] = held ? r * (f[e] * wb[e] - yn * m) : 0.0f;
     }
     if (in) {
-      store_chunk<BF16>(sd.out, t * sd.ldo + hd + a, x);
-      store_chunk<BF16>(sd.out, t * sd.ldo + hd + b, y);
+      store_own<BF16, WHOLE>(sd.out, t * sd.ldo + hd + a, x, k.dup_a);
+      store_own<BF16, WHOLE>(sd.out, t * sd.ldo + hd + b, y, k.dup_b);
     }
     t += step_t;
     h += step_h;
@@ -353,10 +415,11 @@ __global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32
   __syncthreads();
   for (int32_t j = threadIdx.x; j < LANES * 2 * V; j += QT) {
     const int32_t ln = j % LANES, e = j / LANES;
-    if (ln * V >= p.d / 2) continue;
-    chunks_of(p, ln * V, a, b);
+    if (ln >= used) continue;
+    const Chunks o = chunks_of<V, WHOLE>(p, ln);
+    if (e < V ? e < o.dup_a : e - V < o.dup_b) continue;
     const float v = ((acc[0][j] + acc[1][j]) + acc[2][j]) + acc[3][j];
-    gst<float>((part ? part + (int64_t)blockIdx.x * p.d : sd.dw) + (e < V ? a + e : b + e - V), v);
+    gst<float>((part ? part + (int64_t)blockIdx.x * p.d : sd.dw) + (e < V ? o.a + e : o.b + e - V), v);
   }
 }
 
@@ -539,40 +602,40 @@ __global__ __launch_bounds__(QT) void qk_backward_unit_kernel(QkParams p, int32_
   }
 }
 
-// dw of a side: its workgroups' parts.  16 wavefronts of a workgroup take every 16th part of 64 entries,
+// dw of a side: its workgroups' parts.  A workgroup has 16 entries; 64 sets of 16 lanes take every 64th part,
 // 8 in flight, and meet in order.
-constexpr int FT = 1024, FW = FT / 64;
+constexpr int FT = 1024, FE = 16, FS = FT / FE;
 __global__ __launch_bounds__(FT) void qk_fold_kernel(QkParams p, int32_t nq, int32_t nk,
                                                      const float* part) {
-  __shared__ float acc[FW][64];
+  __shared__ float acc[FS][FE];
   const bool keys = blockIdx.y != 0;
   const int32_t heads = keys ? p.side[1].heads : p.side[0].heads;
   if (heads == 0) return;
-  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int32_t e = blockIdx.x * 64 + lane, n = keys ? nk : nq;
+  const int32_t set = threadIdx.x / FE, lane = threadIdx.x % FE;
+  const int32_t e = blockIdx.x * FE + lane, n = keys ? nk : nq;
   const float* from = part + (int64_t)(keys ? nq : 0) * p.d + e;
   float sum = 0.0f;
-  for (int32_t i = wave; i < n; i += 8 * FW) {
+  for (int32_t i = set; i < n; i += 8 * FS) {
     float x[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      x[u] = e < p.d && i + u * FW < n ? gld<float>(from + (int64_t)(i + u * FW) * p.d) : 0.0f;
+      x[u] = e < p.d && i + u * FS < n ? gld<float>(from + (int64_t)(i + u * FS) * p.d) : 0.0f;
 #pragma unroll
     for (int u = 0; u < 8; ++u) sum += x[u];
   }
-  acc[wave][lane] = sum;
+  acc[set][lane] = sum;
   __syncthreads();
-  if (wave == 0 && e < p.d) {
 #pragma unroll
-    for (int w = 1; w < FW; ++w) sum += acc[w][lane];
-    gst<float>((keys ? p.side[1].dw : p.side[0].dw) + e, sum);
+  for (int h = FS / 2; h > 0; h /= 2) {
+    if (set < h) acc[set][lane] += acc[set + h][lane];
+    __syncthreads();
   }
+  if (set == 0 && e < p.d) gst<float>((keys ? p.side[1].dw : p.side[0].dw) + e, acc[0][lane]);
 }
 
 int lanes_of(const QkParams& p) {
-  const int32_t two = p.bf16 ? 16 : 8;
   int lanes = 4;
-  while (lanes * two < p.d) lanes *= 2;
+  while (lanes < chunk_lanes(p)) lanes *= 2;
   return lanes;
 }
 
@@ -617,27 +680,35 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
     q.pos += t0;
     const int32_t rows = (int32_t)(q.tokens * per), wg = QW * rows_at_once(p);
     const dim3 grid((uint32_t)(((int64_t)rows + wg - 1) / wg));
-#define TPP_QK(KERNEL, ...) \
-  hipLaunchKernelGGL((KERNEL<__VA_ARGS__>), grid, dim3(QT), 0, stream, q, rows, per, div)
-#define TPP_QK_LANES(BF16)                                    \
-  switch (lanes_of(p)) {                                      \
-    case 4: TPP_QK(qk_chunk_kernel, BF16, 4); break;          \
-    case 8: TPP_QK(qk_chunk_kernel, BF16, 8); break;          \
-    case 16: TPP_QK(qk_chunk_kernel, BF16, 16); break;        \
-    case 32: TPP_QK(qk_chunk_kernel, BF16, 32); break;        \
-    default: TPP_QK(qk_chunk_kernel, BF16, 64);               \
+#define TPP_QK(LANES, BF16, WHOLE)                                                                  \
+  case LANES:                                                                                       \
+    hipLaunchKernelGGL((qk_chunk_kernel<BF16, WHOLE, LANES>), grid, dim3(QT), 0, stream, q, rows, per, \
+                       div, chunk_lanes(p));                                                        \
+    break
+#define TPP_QK_LANES(BF16, WHOLE)                                                                   \
+  switch (lanes_of(p)) {                                                                            \
+    TPP_QK(4, BF16, WHOLE);                                                                         \
+    TPP_QK(8, BF16, WHOLE);                                                                         \
+    TPP_QK(16, BF16, WHOLE);                                                                        \
+    TPP_QK(32, BF16, WHOLE);                                                                        \
+    TPP_QK(64, BF16, WHOLE);                                                                        \
   }
-    if (chunked(p)) {
-      if (p.bf16) { TPP_QK_LANES(true) } else { TPP_QK_LANES(false) }
+#define TPP_QK_UNITS(NU) \
+  hipLaunchKernelGGL((qk_unit_kernel<NU>), grid, dim3(QT), 0, stream, q, rows, per, div)
+    if (whole_chunks(p)) {
+      if (p.bf16) { TPP_QK_LANES(true, true) } else { TPP_QK_LANES(false, true) }
+    } else if (chunked(p)) {
+      if (p.bf16) { TPP_QK_LANES(true, false) } else { TPP_QK_LANES(false, false) }
     } else if (units <= 64) {
-      TPP_QK(qk_unit_kernel, 1);
+      TPP_QK_UNITS(1);
     } else if (units <= 128) {
-      TPP_QK(qk_unit_kernel, 2);
+      TPP_QK_UNITS(2);
     } else if (units <= 256) {
-      TPP_QK(qk_unit_kernel, 4);
+      TPP_QK_UNITS(4);
     } else {
-      TPP_QK(qk_unit_kernel, 8);
+      TPP_QK_UNITS(8);
     }
+#undef TPP_QK_UNITS
 #undef TPP_QK_LANES
 #undef TPP_QK
     const hipError_t e = hipGetLastError();
@@ -662,31 +733,39 @@ hipError_t launch_qk_backward(const QkParams& p, float* work, hipStream_t stream
     nk = nk < 1 ? nk : 1;
   }
   const int32_t units = p.d - p.rot_dim / 2;
-#define TPP_QKB(KERNEL, ...)                                                                      \
-  hipLaunchKernelGGL((KERNEL<__VA_ARGS__>), dim3(nq + nk), dim3(QT), 0, stream, p, nq, work)
-#define TPP_QKB_LANES(BF16)                                             \
-  switch (lanes_of(p)) {                                                \
-    case 4: TPP_QKB(qk_backward_chunk_kernel, BF16, 4); break;          \
-    case 8: TPP_QKB(qk_backward_chunk_kernel, BF16, 8); break;          \
-    case 16: TPP_QKB(qk_backward_chunk_kernel, BF16, 16); break;        \
-    case 32: TPP_QKB(qk_backward_chunk_kernel, BF16, 32); break;        \
-    default: TPP_QKB(qk_backward_chunk_kernel, BF16, 64);               \
+#define TPP_QKB(LANES, BF16, WHOLE)                                                                 \
+  case LANES:                                                                                       \
+    hipLaunchKernelGGL((qk_backward_chunk_kernel<BF16, WHOLE, LANES>), dim3(nq + nk), dim3(QT), 0,  \
+                       stream, p, nq, work, chunk_lanes(p));                                        \
+    break
+#define TPP_QKB_LANES(BF16, WHOLE)                                                                  \
+  switch (lanes_of(p)) {                                                                            \
+    TPP_QKB(4, BF16, WHOLE);                                                                        \
+    TPP_QKB(8, BF16, WHOLE);                                                                        \
+    TPP_QKB(16, BF16, WHOLE);                                                                       \
+    TPP_QKB(32, BF16, WHOLE);                                                                       \
+    TPP_QKB(64, BF16, WHOLE);                                                                       \
   }
-  if (chunked(p)) {
-    if (p.bf16) { TPP_QKB_LANES(true) } else { TPP_QKB_LANES(false) }
+#define TPP_QKB_UNITS(NU) \
+  hipLaunchKernelGGL((qk_backward_unit_kernel<NU>), dim3(nq + nk), dim3(QT), 0, stream, p, nq, work)
+  if (whole_chunks(p)) {
+    if (p.bf16) { TPP_QKB_LANES(true, true) } else { TPP_QKB_LANES(false, true) }
+  } else if (chunked(p)) {
+    if (p.bf16) { TPP_QKB_LANES(true, false) } else { TPP_QKB_LANES(false, false) }
   } else if (units <= 64) {
-    TPP_QKB(qk_backward_unit_kernel, 1);
+    TPP_QKB_UNITS(1);
   } else if (units <= 128) {
-    TPP_QKB(qk_backward_unit_kernel, 2);
+    TPP_QKB_UNITS(2);
   } else if (units <= 256) {
-    TPP_QKB(qk_backward_unit_kernel, 4);
+    TPP_QKB_UNITS(4);
   } else {
-    TPP_QKB(qk_backward_unit_kernel, 8);
+    TPP_QKB_UNITS(8);
   }
+#undef TPP_QKB_UNITS
 #undef TPP_QKB_LANES
 #undef TPP_QKB
   if (work)
-    hipLaunchKernelGGL(qk_fold_kernel, dim3((p.d + 63) / 64, 2), dim3(FT), 0, stream, p, nq, nk, work);
+    hipLaunchKernelGGL(qk_fold_kernel, dim3((p.d + FE - 1) / FE, 2), dim3(FT), 0, stream, p, nq, nk, work);
   return hipGetLastError();
 }
 

@@ -85,6 +85,21 @@ ROPE = [  # tokens, q heads, k heads, D, rot_dim, form, dtype, extra ld, first e
     (65, 4, 0, 64, 0, "halves", "f32", 0, 0),        # the norm alone
     (300, 2, 2, 72, 48, "halves", "bf16", 0, 0),
     (300, 2, 2, 112, 56, "pairs", "bf16", 0, 0),
+    # parts that are no whole chunks: the halves, the rest, both; a rest below a chunk; odd rows
+    (70, 3, 2, 80, 40, "halves", "bf16", 0, 0),
+    (70, 3, 2, 72, 72, "halves", "bf16", 1, 1),
+    (70, 3, 2, 72, 36, "halves", "f32", 0, 0),
+    (70, 3, 2, 77, 38, "halves", "bf16", 0, 1),
+    (70, 3, 2, 77, 76, "halves", "f32", 1, 0),
+    (70, 3, 2, 77, 0, "halves", "bf16", 0, 0),
+    (70, 3, 2, 77, 76, "pairs", "f32", 0, 0),
+    (70, 3, 2, 77, 68, "pairs", "bf16", 0, 0),
+    (70, 3, 2, 78, 78, "pairs", "bf16", 0, 1),
+    (70, 3, 2, 9, 0, "pairs", "bf16", 0, 0),
+    (70, 3, 2, 17, 16, "halves", "bf16", 0, 0),
+    (9, 2, 1, 511, 10, "halves", "f32", 0, 0),           # one lane too many for a wavefront
+    (9, 2, 1, 511, 8, "halves", "f32", 0, 0),
+    (9, 2, 1, 511, 500, "halves", "bf16", 0, 0),
 ]
 ROPE_IDS = [f"T{c[0]}-{c[1]}x{c[2]}-D{c[3]}-R{c[4]}-{c[5]}-{c[6]}-{c[7]}-{c[8]}" for c in ROPE]
 EPS = 1e-5
