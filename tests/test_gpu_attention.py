@@ -691,6 +691,13 @@ def test_decode_step(tpp):
             assert np.array_equal(got, before[x][pg[k // ev.page], k % ev.page])
 
 
+def test_current_stream_is_torchs(tpp):
+    assert tpp.current_stream() == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(torch.cuda.Stream()):
+        assert tpp.current_stream() == torch.cuda.current_stream().cuda_stream != 0
+    assert tpp.current_stream() == torch.cuda.current_stream().cuda_stream
+
+
 def test_side_stream(tpp):
     """All calls on a stream that is not torch's current one, beside work on that one."""
     pc = Paged([3000, 700], 128, 2, 16, "bf16", seed=1)
