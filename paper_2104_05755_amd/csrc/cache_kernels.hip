@@ -27,6 +27,7 @@ constexpr int ST = 1024;          // threads of the selection: 16 wavefronts
 constexpr int SW = ST / 64;
 constexpr int BINS = 2048;        // of 11 bits
 constexpr int CT = 256;           // threads of the copy
+constexpr int FEW = 4;            // positions that leave one by one rather than by selection
 constexpr int FUSED_CHUNKS = 2 * ST;   // most chunks of a pool that the selecting workgroup copies
 
 // The totals' order as unsigned integers: -0 as +0, NaN above everything.
@@ -116,6 +117,20 @@ template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true);
 }
+// The least of a wavefront's values, in every lane.
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) {
+  const auto dpp = [](uint32_t x, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, decltype(ctrl)::value, 0xf, 0xf, false);
+  };
+  v = min(v, dpp(v, IntC<0xB1>()));    // lane ^ 1, lane ^ 2, the other quad of 8, the other 8 of 16
+  v = min(v, dpp(v, IntC<0x4E>()));
+  v = min(v, dpp(v, IntC<0x141>()));
+  v = min(v, dpp(v, IntC<0x140>()));
+  auto w = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = min(w[0], w[1]);
+  w = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return min(w[0], w[1]);
+}
 // Running sums over the workgroup: what the threads before this one have of v, and in `all` the total.
 // Within a wavefront by register permutes (row shifts, then the rows' last lanes handed on).  The barriers
 // also order what was in LDS before the call.
@@ -149,14 +164,17 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
   constexpr int32_t PART = KPT * ST;
   __shared__ int32_t hist[BINS];
   __shared__ uint32_t sums[SW];
-  __shared__ uint32_t turned[PART + PART / 32];
+  __shared__ uint32_t turned[KPT == 4 ? 1 : PART + PART / 32];
   __shared__ int32_t pick[3];     // digit, candidates below it, candidates of it
+  __shared__ uint32_t best[2][SW];
+  __shared__ int32_t best_t[2][SW];
   __shared__ int32_t lists[FUSED ? 2 * FUSED_CHUNKS : 1];
   const int tid = threadIdx.x;
   const int64_t b = blockIdx.x;
   const int64_t len = gld<int64_t>(p.len + b);
   const int64_t horizon = p.pos ? gld<int64_t>(p.horizon + b) : 0;
-  const int32_t n = (int32_t)(len < 0 ? 0 : len > p.max_len ? p.max_len : len);
+  const int32_t n =
+      __builtin_amdgcn_readfirstlane((int32_t)(len < 0 ? 0 : len > p.max_len ? p.max_len : len));
   const int32_t want = n > p.budget ? (int32_t)(n - p.budget) : 0;
   const float* tot = p.totals + b * p.ldt;
   const int64_t* pos = p.pos ? p.pos + b * p.ldt : nullptr;
@@ -167,8 +185,33 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
   // that is no candidate.  Read in order, 16 loads in flight before the first is waited for (past the end
   // the last position), and turned in LDS, a word in 33 left out against bank conflicts: a thread that read
   // its own run would touch a cache line for every 16 bytes.
+  // (Four positions of a thread are 16 consecutive bytes: read where they belong, before the length is known.)
   uint32_t keys[KPT];
+  f32x4 x4 = {0.0f, 0.0f, 0.0f, 0.0f};
+  int64_t y4[4] = {0, 0, 0, 0};
+  if constexpr (KPT == 4) {
+    const int32_t t = tid * 4;
+    if (t + 4 <= p.max_len) {
+      x4 = gld<f32x4_a4>(tot + t);
+      if (pos)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y4[i] = gld<int64_t>(pos + t + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t + i < p.max_len) {
+          x4[i] = gld<float>(tot + t + i);
+          if (pos) y4[i] = gld<int64_t>(pos + t + i);
+        }
+    }
+  }
   const auto load_keys = [&](int32_t part) {
+    if constexpr (KPT == 4) {   // one part
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        keys[i] = tid * 4 + i < n && (!pos || y4[i] < horizon) ? order_key(x4[i]) : 0u;
+      return;
+    }
     constexpr int P = KPT < 16 ? KPT : 16;   // in flight
     __syncthreads();   // the part before is done with
 #pragma unroll
@@ -198,7 +241,48 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
   uint32_t prefix = 0;            // the digits found so far
   int32_t rank = 0, gone_n = 0;   // ordinal (from 0) among the candidates with that prefix
   bool all_ties = false;          // whether all candidates of that key leave
-  if (want > 0) {
+  int32_t cut = -1;               // or those of them up to this position
+  if (want > 0 && want <= FEW && !several) {
+    // A few leave: the least candidate behind the last one, by (key, position), as many times.  A wavefront's
+    // is the first lane of its least key; the wavefronts meet in LDS.
+    uint32_t last = 0;       // key and position of the last one
+    int32_t last_t = -1;
+    for (; gone_n < want; ++gone_n) {
+      uint32_t key = ~0u;
+      int32_t at = n;
+#pragma unroll
+      for (int i = KPT - 1; i >= 0; --i) {
+        const int32_t t = tid * KPT + i;
+        const bool after = keys[i] > last || (keys[i] == last && t > last_t);
+        if (keys[i] != 0 && after && keys[i] <= key) {
+          key = keys[i];
+          at = t;
+        }
+      }
+      const uint32_t least = wave_min(at < n ? key : ~0u);
+      const uint64_t has = __ballot(at < n && key == least);
+      const int first = has ? __builtin_ctzll(has) : 0;
+      const int32_t t = __builtin_amdgcn_readlane(at, first);   // n where the wavefront has none
+      if ((tid & 63) == 0) {
+        best[gone_n & 1][tid >> 6] = least;
+        best_t[gone_n & 1][tid >> 6] = has ? t : n;
+      }
+      __syncthreads();
+      uint32_t k = ~0u;
+      int32_t kt = n;
+#pragma unroll
+      for (int w = SW - 1; w >= 0; --w)
+        if (best_t[gone_n & 1][w] < n && best[gone_n & 1][w] <= k) {
+          k = best[gone_n & 1][w];
+          kt = best_t[gone_n & 1][w];
+        }
+      if (kt == n) break;   // no candidate is left
+      last = k;
+      last_t = kt;
+    }
+    prefix = last;
+    cut = last_t;
+  } else if (want > 0) {
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t mask = pass == 2 ? 1023u : 2047u;
@@ -254,7 +338,10 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
 #pragma unroll
       for (int i = 0; i < KPT; ++i)   // 0 wraps: it is no candidate
         goes |= keys[i] - 1u < prefix - (all_ties ? 0u : 1u) ? 1u << i : 0u;
-      if (!all_ties) {   // the same for the whole workgroup
+      if (cut >= 0) {   // the same for the whole workgroup
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) goes |= keys[i] == prefix && t + i <= cut ? 1u << i : 0u;
+      } else if (!all_ties) {
         uint32_t tie = 0;
 #pragma unroll
         for (int i = 0; i < KPT; ++i) tie |= keys[i] == prefix ? 1u << i : 0u;
