@@ -6,7 +6,7 @@
 // smallest candidate, and how many candidates of exactly T leave.  Each thread has a run of consecutive
 // positions, and running sums over the threads of its ties, free places and movers give every one its
 // place in the lists.  (Ballots over sets of 64 positions, a wavefront's run at a time, are scalar work,
-// and the compute unit has one scalar unit for its 16 wavefronts: FILL us for 16384 positions, FILL so.)
+// and the compute unit has one scalar unit for its 16 wavefronts: 27 us for 16384 positions, 20.4 so.)
 //
 // One workgroup of 16 wavefronts per sequence selects.  Up to 32 keys per thread stay in registers, so that
 // memory is read once, with every load in flight; longer sequences are read again by each pass.
@@ -65,52 +65,40 @@ struct CopyShape {
   int32_t lanes, unit, units; // bytes of a chunk; chunks of a row
 };
 
-template <int U, typename T>
+template <typename T>
 __device__ __forceinline__ void copy_rows(const EvictParams& p, const CopyShape& cs, int64_t b,
                                           const int32_t* to, const int32_t* from, int32_t rows,
                                           int32_t row, int32_t step, int32_t lane) {
   const int32_t bytes = p.d * p.es;
   char* kb = static_cast<char*>(p.k);
   char* vb = static_cast<char*>(p.v);
-  for (; row < rows; row += U * step) {   // rows below 2^30 by the launcher
-    int64_t dst[U], src[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int32_t r = row + u * step < rows ? row + u * step : row;   // past the end: the first again
-      const int32_t j = fdiv((uint32_t)r, cs.heads), h = r - j * p.kv_heads;
-      const int64_t d = row_of(p, b, to[j]), s = row_of(p, b, from[j]);
-      dst[u] = d < 0 || s < 0 ? -1 : (d + h * p.head_stride) * p.es;
-      src[u] = (s + h * p.head_stride) * p.es;
-    }
+  for (; row < rows; row += step) {   // rows below 2^30 by the launcher
+    const int32_t j = fdiv((uint32_t)row, cs.heads), h = row - j * p.kv_heads;
+    const int64_t d = row_of(p, b, to[j]), s = row_of(p, b, from[j]);
+    const int64_t dst = d < 0 || s < 0 ? -1 : (d + h * p.head_stride) * p.es;
+    const int64_t src = (s + h * p.head_stride) * p.es;
     for (int32_t c = lane; c < cs.units; c += cs.lanes) {
       const int32_t e = (c + 1) * cs.unit <= bytes ? c * cs.unit : bytes - cs.unit;
-      T k[U], v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (dst[u] >= 0) {
-          k[u] = gld<T>(kb + src[u] + e);
-          v[u] = gld<T>(vb + src[u] + e);
-        }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (dst[u] >= 0) {
-          gst<T>(kb + dst[u] + e, k[u]);
-          gst<T>(vb + dst[u] + e, v[u]);
-        }
+      T k, v;
+      if (dst >= 0) {
+        k = gld<T>(kb + src + e);
+        v = gld<T>(vb + src + e);
+        gst<T>(kb + dst + e, k);
+        gst<T>(vb + dst + e, v);
+      }
     }
   }
 }
 // Wavefront `wave` of `waves` that copy the moves of sequence b.
-template <int U>
 __device__ __forceinline__ void copy_moves(const EvictParams& p, const CopyShape& cs, int64_t b,
                                            const int32_t* to, const int32_t* from, int32_t moves,
                                            int32_t wave, int32_t waves) {
   const int32_t lane = threadIdx.x & 63, slots = 64 / cs.lanes;
   const int32_t row = wave * slots + lane / cs.lanes, step = waves * slots;
   if (cs.unit == 16)
-    copy_rows<U, u32x4_a2>(p, cs, b, to, from, moves * p.kv_heads, row, step, lane % cs.lanes);
+    copy_rows<u32x4_a2>(p, cs, b, to, from, moves * p.kv_heads, row, step, lane % cs.lanes);
   else
-    copy_rows<1, uint16_t>(p, cs, b, to, from, moves * p.kv_heads, row, step, lane % cs.lanes);
+    copy_rows<uint16_t>(p, cs, b, to, from, moves * p.kv_heads, row, step, lane % cs.lanes);
 }
 
 template <int CTRL, int ROWS>
@@ -408,7 +396,7 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
     if (!FUSED) ml.count[b] = moves;
     gst<int64_t>(p.len_out + b, left);
   }
-  if constexpr (FUSED) copy_moves<1>(p, cs, b, to, from, moves, tid >> 6, SW);
+  if constexpr (FUSED) copy_moves(p, cs, b, to, from, moves, tid >> 6, SW);
 }
 
 // `per` workgroups for each sequence: the first `hand` hand on the totals and positions of what stays
@@ -418,8 +406,8 @@ __global__ __launch_bounds__(CT) void evict_copy_kernel(EvictParams p, MoveLists
   const int32_t seq = fdiv(blockIdx.x, div), y = (int32_t)blockIdx.x - seq * per;
   const int64_t b = seq;
   if (y >= hand) {
-    copy_moves<2>(p, cs, b, ml.to + b * ml.cap, ml.from + b * ml.cap, ml.count[b],
-                  (y - hand) * (CT / 64) + (threadIdx.x >> 6), (per - hand) * (CT / 64));
+    copy_moves(p, cs, b, ml.to + b * ml.cap, ml.from + b * ml.cap, ml.count[b],
+               (y - hand) * (CT / 64) + (threadIdx.x >> 6), (per - hand) * (CT / 64));
     return;
   }
   const int64_t len = gld<int64_t>(p.len_out + b);
@@ -471,8 +459,8 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   if (p.n_seqs > 0x7fffffff || rows > (1 << 30)) return hipErrorInvalidConfiguration;
   const bool in_place = p.totals_out == p.totals && p.pos_out == p.pos;
   // A chunk or two per thread of the selecting workgroup, and totals that stay where they are or are few:
-  // no second launch (32 sequences of 2049 that lose one position: 10.4 us so, 16.4 with a copy of its
-  // own; one of 32768, handed on: FILL so, FILL with the copy's workgroups).
+  // no second launch (32 sequences of 2049 that lose one position: 10.9 us so, 16.4 with a copy of its own;
+  // one of 32768 that loses one and is handed on: 28.1 us so, 21.4 with the copy's workgroups).
   const bool fused = chunks <= FUSED_CHUNKS && (in_place || p.max_len <= 4 * ST);
   const dim3 grid((uint32_t)p.n_seqs);
 #define TPP_SELECT(KPT, FUSED)                                                                    \
@@ -484,9 +472,9 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   } else {
     if (p.max_len <= 16 * ST) TPP_SELECT(16, false);
     else TPP_SELECT(32, false);
-    // two rows per set of lanes, at most 2048 workgroups
+    // two rows per set of lanes, at most 8192 workgroups (2048: 66.6 us for 8 x 16384 cut to 4096, 64.1 so)
     const int64_t want = (rows * cs.lanes + 2 * CT - 1) / (2 * CT);
-    const int64_t most = 2048 / p.n_seqs > 0 ? 2048 / p.n_seqs : 1;
+    const int64_t most = 8192 / p.n_seqs > 0 ? 8192 / p.n_seqs : 1;
     const int64_t hand = in_place ? 0 : (p.max_len + 4 * CT - 1) / (4 * CT);
     const int64_t per = hand + (want < most ? want : most);
     if (per * p.n_seqs > 0x7fffffff) return hipErrorInvalidConfiguration;
