@@ -133,6 +133,10 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   constexpr int NK = DP / S::STEP;                   // steps of the first product
   constexpr int VC = BF16 && DP > 64 ? 8 : 4;        // entries of a lane's chunk of a value
   constexpr int NV = (DP + 16 * VC - 1) / (16 * VC); // chunks
+  // Values are read once, whole lines by one load: past the caches' replacement (64 sequences of 4096: 199 us
+  // without, 181 so; a sequence of 131072 107 and 97).  The keys' lines take two loads, which would then both
+  // go to memory (64 of 1 to 8192 215 us, 234 so), and rows that are no whole lines share some with the next.
+  constexpr bool STREAM = !TAIL && DP * ES % 128 == 0;
   constexpr bool OVER = TAIL || DP % (16 * VC) != 0; // lanes past the last entry take the last chunk
   typedef typename std::conditional<VC * ES == 16, u32x4, u32x2>::type vchunk;
   typedef typename std::conditional<VC * ES == 16, u32x4_a2, u32x2_a2>::type vchunk_any;
@@ -208,7 +212,9 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 #pragma unroll
       for (int c = 0; c < NV; ++c) {
         const int32_t e = (c * 16 + col) * VC;
-        vf[k][c] = gld<vchunk_any>(vb + (row & ~int64_t(1)) + (OVER && e > D - VC ? D - VC : e) * ES);
+        const GLOBAL_AS vchunk_any* at =
+            (const GLOBAL_AS vchunk_any*)(vb + (row & ~int64_t(1)) + (OVER && e > D - VC ? D - VC : e) * ES);
+        vf[k][c] = STREAM ? (vchunk)__builtin_nontemporal_load(at) : (vchunk)*at;
       }
     }
   };
