@@ -112,9 +112,17 @@ struct Chunk {
   static constexpr int V = BF16 ? 8 : 4;
   static constexpr int ES = BF16 ? 2 : 4;
 };
-template <bool BF16>
+// How rows go through the caches.  What is read or written once only displaces what may be read again, from
+// the 32 MB of the L2s and the 256 MB behind them: outputs beyond the former are stored past their replacement
+// (4096 tokens of 32 + 8 heads of 128 bf16 23.4 us, 17.5 so), and where inputs and outputs pass half of the
+// latter, inputs are loaded so too, if every load takes whole lines (8192 tokens 37.3 us and 32.9, the
+// backward pass 56.0 and 51.2; 4096 tokens 25.4; rows of 160 bytes 15.4 and 18.1).
+enum { CACHED, STREAM_OUT, STREAM };
+template <bool BF16, int HOW>
 __device__ __forceinline__ u32x4 load_chunk(const void* p, int64_t at) {
-  return gld<u32x4_a2>(static_cast<const char*>(p) + at * Chunk<BF16>::ES);
+  const GLOBAL_AS u32x4_a2* from =
+      (const GLOBAL_AS u32x4_a2*)(static_cast<const char*>(p) + at * Chunk<BF16>::ES);
+  return HOW == STREAM ? (u32x4)__builtin_nontemporal_load(from) : (u32x4)*from;
 }
 template <bool BF16>
 __device__ __forceinline__ void widen(u32x4 w, float (&x)[Chunk<BF16>::V]) {
@@ -128,7 +136,7 @@ __device__ __forceinline__ void widen(u32x4 w, float (&x)[Chunk<BF16>::V]) {
     }
   }
 }
-template <bool BF16>
+template <bool BF16, int HOW>
 __device__ __forceinline__ void store_chunk(void* p, int64_t at, const float (&v)[Chunk<BF16>::V]) {
   u32x4 w;
 #pragma unroll
@@ -136,7 +144,9 @@ __device__ __forceinline__ void store_chunk(void* p, int64_t at, const float (&v
     if constexpr (BF16) w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
     else w[e] = __float_as_uint(v[e]);
   }
-  gst<u32x4_a2>(static_cast<char*>(p) + at * Chunk<BF16>::ES, w);
+  GLOBAL_AS u32x4_a2* to = (GLOBAL_AS u32x4_a2*)(static_cast<char*>(p) + at * Chunk<BF16>::ES);
+  if constexpr (HOW != CACHED) __builtin_nontemporal_store((u32x4_a2)w, to);
+  else *to = w;
 }
 template <int V>
 __device__ __forceinline__ void load_floats(const float* p, float (&v)[V]) {
@@ -274,10 +284,10 @@ __device__ __forceinline__ float squares(const float (&x)[V], int32_t dup) {
   return sum;
 }
 // A chunk's entries but those that another lane stores.
-template <bool BF16, bool WHOLE>
+template <bool BF16, bool WHOLE, int HOW>
 __device__ __forceinline__ void store_own(void* p, int64_t at, const float (&v)[Chunk<BF16>::V], int32_t dup) {
   if (WHOLE || dup == 0) {
-    store_chunk<BF16>(p, at, v);
+    store_chunk<BF16, HOW>(p, at, v);
   } else {
 #pragma unroll
     for (int e = 1; e < Chunk<BF16>::V; ++e)
@@ -285,7 +295,7 @@ __device__ __forceinline__ void store_own(void* p, int64_t at, const float (&v)[
   }
 }
 
-template <bool BF16, bool WHOLE, int LANES>
+template <bool BF16, bool WHOLE, int LANES, int HOW>
 __global__ __launch_bounds__(QT) void qk_chunk_kernel(QkParams p, int32_t rows, int32_t per_token,
                                                       FastDiv div, int32_t used) {
   constexpr int V = Chunk<BF16>::V;
@@ -298,7 +308,7 @@ __global__ __launch_bounds__(QT) void qk_chunk_kernel(QkParams p, int32_t rows, 
   const bool in = i < used;   // lanes past the row's chunks repeat its first
   const Chunks k = chunks_of<V, WHOLE>(p, in ? i : 0);
   const int32_t a = k.a, b = k.b;
-  const u32x4 wx = load_chunk<BF16>(r.x, r.from + a), wy = load_chunk<BF16>(r.x, r.from + b);
+  const u32x4 wx = load_chunk<BF16, HOW>(r.x, r.from + a), wy = load_chunk<BF16, HOW>(r.x, r.from + b);
   if (!r.w) {
     if (in) {   // what two lanes store is the same
       gst<u32x4_a2>(static_cast<char*>(r.out) + (r.to + a) * Chunk<BF16>::ES, wx);
@@ -321,15 +331,15 @@ __global__ __launch_bounds__(QT) void qk_chunk_kernel(QkParams p, int32_t rows, 
   }
   turn<V>(p.pairs, false, c, s, x, y);
   if (in) {
-    store_own<BF16, WHOLE>(r.out, r.to + a, x, k.dup_a);
-    store_own<BF16, WHOLE>(r.out, r.to + b, y, k.dup_b);
+    store_own<BF16, WHOLE, HOW>(r.out, r.to + a, x, k.dup_a);
+    store_own<BF16, WHOLE, HOW>(r.out, r.to + b, y, k.dup_b);
   }
 }
 
 // Backward.  Workgroup w of a side (the first nq of the queries, the rest of the keys) takes every n-th
 // set of QW * 64 / LANES rows and keeps its part of the weights' gradient in registers; parts go to
 // `part` (a row of D per workgroup), or straight to dw where a side has one workgroup.
-template <bool BF16, bool WHOLE, int LANES>
+template <bool BF16, bool WHOLE, int LANES, int HOW>
 __global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32_t nq, float* part,
                                                                int32_t used) {
   constexpr int V = Chunk<BF16>::V, SLOTS = 64 / LANES;
@@ -360,8 +370,8 @@ __global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32
     const bool held = pos >= 0 && pos < p.n_positions;
     const int64_t hd = (int64_t)h * p.d;
     const int64_t fx = t * sd.ldx + hd, fg = t * sd.ldg + hd;
-    const u32x4 xw = load_chunk<BF16>(sd.x, fx + a), yw = load_chunk<BF16>(sd.x, fx + b);
-    const u32x4 gw = load_chunk<BF16>(sd.g, fg + a), fw = load_chunk<BF16>(sd.g, fg + b);
+    const u32x4 xw = load_chunk<BF16, HOW>(sd.x, fx + a), yw = load_chunk<BF16, HOW>(sd.x, fx + b);
+    const u32x4 gw = load_chunk<BF16, HOW>(sd.g, fg + a), fw = load_chunk<BF16, HOW>(sd.g, fg + b);
     float x[V], y[V], g[V], f[V], c[V], s[V];
     load_angles<V>(p, held ? pos : -1, a, b, k.turned, c, s);
     widen<BF16>(xw, x);
@@ -389,8 +399,8 @@ __global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32
       y[e] = held ? r * (f[e] * wb[e] - yn * m) : 0.0f;
     }
     if (in) {
-      store_own<BF16, WHOLE>(sd.out, t * sd.ldo + hd + a, x, k.dup_a);
-      store_own<BF16, WHOLE>(sd.out, t * sd.ldo + hd + b, y, k.dup_b);
+      store_own<BF16, WHOLE, HOW>(sd.out, t * sd.ldo + hd + a, x, k.dup_a);
+      store_own<BF16, WHOLE, HOW>(sd.out, t * sd.ldo + hd + b, y, k.dup_b);
     }
     t += step_t;
     h += step_h;
@@ -642,6 +652,20 @@ int lanes_of(const QkParams& p) {
 // Rows that a wavefront takes at once.
 int rows_at_once(const QkParams& p) { return chunked(p) ? 64 / lanes_of(p) : IN_FLIGHT; }
 
+// How a pass goes through the caches, by what it moves (see above).
+int cache_use(const QkParams& p, bool backward) {
+  if (p.slot || !whole_chunks(p)) return CACHED;   // keys and queries on their way to attention
+  const int64_t es = p.bf16 ? 2 : 4;
+  const int64_t out = p.tokens * (p.side[0].heads + p.side[1].heads) * p.d * es;
+  if (out <= int64_t(32) << 20) return CACHED;
+  bool lines = p.d * es % 128 == 0;
+  for (const QkSide& s : p.side)
+    if (s.heads > 0)
+      lines = lines && s.ldx * es % 128 == 0 && (reinterpret_cast<uintptr_t>(s.x) & 127) == 0 &&
+              (!backward || (s.ldg * es % 128 == 0 && (reinterpret_cast<uintptr_t>(s.g) & 127) == 0));
+  return lines && out * (backward ? 3 : 2) > int64_t(128) << 20 ? STREAM : STREAM_OUT;
+}
+
 // Workgroups of the two sides in the backward pass: 1024 in all where there are rows for them.
 void backward_groups(const QkParams& p, int32_t& nq, int32_t& nk) {
   const int32_t heads = p.side[0].heads + p.side[1].heads, rows = QW * rows_at_once(p);
@@ -680,25 +704,30 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
     q.pos += t0;
     const int32_t rows = (int32_t)(q.tokens * per), wg = QW * rows_at_once(p);
     const dim3 grid((uint32_t)(((int64_t)rows + wg - 1) / wg));
-#define TPP_QK(LANES, BF16, WHOLE)                                                                  \
+#define TPP_QK(LANES, BF16, WHOLE, HOW)                                                             \
   case LANES:                                                                                       \
-    hipLaunchKernelGGL((qk_chunk_kernel<BF16, WHOLE, LANES>), grid, dim3(QT), 0, stream, q, rows, per, \
-                       div, chunk_lanes(p));                                                        \
+    hipLaunchKernelGGL((qk_chunk_kernel<BF16, WHOLE, LANES, HOW>), grid, dim3(QT), 0, stream, q,    \
+                       rows, per, div, chunk_lanes(p));                                             \
     break
-#define TPP_QK_LANES(BF16, WHOLE)                                                                   \
+#define TPP_QK_LANES(BF16, WHOLE, HOW)                                                              \
   switch (lanes_of(p)) {                                                                            \
-    TPP_QK(4, BF16, WHOLE);                                                                         \
-    TPP_QK(8, BF16, WHOLE);                                                                         \
-    TPP_QK(16, BF16, WHOLE);                                                                        \
-    TPP_QK(32, BF16, WHOLE);                                                                        \
-    TPP_QK(64, BF16, WHOLE);                                                                        \
+    TPP_QK(4, BF16, WHOLE, HOW);                                                                    \
+    TPP_QK(8, BF16, WHOLE, HOW);                                                                    \
+    TPP_QK(16, BF16, WHOLE, HOW);                                                                   \
+    TPP_QK(32, BF16, WHOLE, HOW);                                                                   \
+    TPP_QK(64, BF16, WHOLE, HOW);                                                                   \
   }
+#define TPP_QK_TYPE(WHOLE, HOW) \
+  if (p.bf16) { TPP_QK_LANES(true, WHOLE, HOW) } else { TPP_QK_LANES(false, WHOLE, HOW) }
 #define TPP_QK_UNITS(NU) \
   hipLaunchKernelGGL((qk_unit_kernel<NU>), grid, dim3(QT), 0, stream, q, rows, per, div)
     if (whole_chunks(p)) {
-      if (p.bf16) { TPP_QK_LANES(true, true) } else { TPP_QK_LANES(false, true) }
+      const int how = cache_use(p, false);
+      if (how == STREAM) { TPP_QK_TYPE(true, STREAM) }
+      else if (how == STREAM_OUT) { TPP_QK_TYPE(true, STREAM_OUT) }
+      else { TPP_QK_TYPE(true, CACHED) }
     } else if (chunked(p)) {
-      if (p.bf16) { TPP_QK_LANES(true, false) } else { TPP_QK_LANES(false, false) }
+      TPP_QK_TYPE(false, CACHED)
     } else if (units <= 64) {
       TPP_QK_UNITS(1);
     } else if (units <= 128) {
@@ -709,6 +738,7 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
       TPP_QK_UNITS(8);
     }
 #undef TPP_QK_UNITS
+#undef TPP_QK_TYPE
 #undef TPP_QK_LANES
 #undef TPP_QK
     const hipError_t e = hipGetLastError();
@@ -733,25 +763,30 @@ hipError_t launch_qk_backward(const QkParams& p, float* work, hipStream_t stream
     nk = nk < 1 ? nk : 1;
   }
   const int32_t units = p.d - p.rot_dim / 2;
-#define TPP_QKB(LANES, BF16, WHOLE)                                                                 \
+#define TPP_QKB(LANES, BF16, WHOLE, HOW)                                                            \
   case LANES:                                                                                       \
-    hipLaunchKernelGGL((qk_backward_chunk_kernel<BF16, WHOLE, LANES>), dim3(nq + nk), dim3(QT), 0,  \
+    hipLaunchKernelGGL((qk_backward_chunk_kernel<BF16, WHOLE, LANES, HOW>), dim3(nq + nk), dim3(QT), 0, \
                        stream, p, nq, work, chunk_lanes(p));                                        \
     break
-#define TPP_QKB_LANES(BF16, WHOLE)                                                                  \
+#define TPP_QKB_LANES(BF16, WHOLE, HOW)                                                             \
   switch (lanes_of(p)) {                                                                            \
-    TPP_QKB(4, BF16, WHOLE);                                                                        \
-    TPP_QKB(8, BF16, WHOLE);                                                                        \
-    TPP_QKB(16, BF16, WHOLE);                                                                       \
-    TPP_QKB(32, BF16, WHOLE);                                                                       \
-    TPP_QKB(64, BF16, WHOLE);                                                                       \
+    TPP_QKB(4, BF16, WHOLE, HOW);                                                                   \
+    TPP_QKB(8, BF16, WHOLE, HOW);                                                                   \
+    TPP_QKB(16, BF16, WHOLE, HOW);                                                                  \
+    TPP_QKB(32, BF16, WHOLE, HOW);                                                                  \
+    TPP_QKB(64, BF16, WHOLE, HOW);                                                                  \
   }
+#define TPP_QKB_TYPE(WHOLE, HOW) \
+  if (p.bf16) { TPP_QKB_LANES(true, WHOLE, HOW) } else { TPP_QKB_LANES(false, WHOLE, HOW) }
 #define TPP_QKB_UNITS(NU) \
   hipLaunchKernelGGL((qk_backward_unit_kernel<NU>), dim3(nq + nk), dim3(QT), 0, stream, p, nq, work)
   if (whole_chunks(p)) {
-    if (p.bf16) { TPP_QKB_LANES(true, true) } else { TPP_QKB_LANES(false, true) }
+    const int how = cache_use(p, true);
+    if (how == STREAM) { TPP_QKB_TYPE(true, STREAM) }
+    else if (how == STREAM_OUT) { TPP_QKB_TYPE(true, STREAM_OUT) }
+    else { TPP_QKB_TYPE(true, CACHED) }
   } else if (chunked(p)) {
-    if (p.bf16) { TPP_QKB_LANES(true, false) } else { TPP_QKB_LANES(false, false) }
+    TPP_QKB_TYPE(false, CACHED)
   } else if (units <= 64) {
     TPP_QKB_UNITS(1);
   } else if (units <= 128) {
@@ -762,6 +797,7 @@ hipError_t launch_qk_backward(const QkParams& p, float* work, hipStream_t stream
     TPP_QKB_UNITS(8);
   }
 #undef TPP_QKB_UNITS
+#undef TPP_QKB_TYPE
 #undef TPP_QKB_LANES
 #undef TPP_QKB
   if (work)
