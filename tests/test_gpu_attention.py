@@ -304,6 +304,74 @@ def test_norm_rope_without_a_table(tpp, form, dtype):
     assert not any(x.any() for x in out + dw)
 
 
+@pytest.mark.parametrize("dtype,D,form,T", [("bf16", 128, "halves", 8300), ("bf16", 80, "pairs", 7001),
+                                            ("f32", 64, "halves", 5000), ("bf16", 128, "pairs", 4000)])
+def test_norm_rope_large(tpp, dtype, D, form, T):
+    """Passes large enough to go past the caches give the bits that the same tokens give in small ones."""
+    hq, hk, part = 32, 8, 100
+    g = torch.Generator(device="cuda")
+    g.manual_seed(D)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x, gy = (torch.randn(T, (hq + hk) * D, generator=g, device="cuda").to(dt) for _ in range(2))
+    ang = torch.rand(64, D // 2, generator=g, device="cuda") * 6
+    rot = torch.cat([ang.cos(), ang.sin()], 1).contiguous()
+    pos = torch.arange(T, device="cuda") % 66 - 1        # padding tokens among them
+    w = [1 + 0.1 * torch.randn(D, generator=g, device="cuda") for _ in range(2)]
+    desc = tpp.tpp_qk_desc(D, D, tpp.TPP_ROT_HALVES if form == "halves" else tpp.TPP_ROT_PAIRS, hq, hk,
+                           code(tpp, dtype), EPS, 64)
+    ld, s, es = (hq + hk) * D, tpp.current_stream(), x.element_size()
+
+    def run(t0, n):
+        at = lambda a: (a.data_ptr() + t0 * ld * es, a.data_ptr() + (t0 * ld + hq * D) * es)
+        y, dx = torch.zeros(n, ld, dtype=dt, device="cuda"), torch.zeros(n, ld, dtype=dt, device="cuda")
+        o = lambda a: (a.data_ptr(), a.data_ptr() + hq * D * es)
+        dw = [torch.zeros(D, device="cuda") for _ in range(2)]
+        p = pos[t0:t0 + n].contiguous()
+        (q, k), (gq, gk), (yq, yk), (dq, dk) = at(x), at(gy), o(y), o(dx)
+        tpp.tpp_qk_norm_rope(desc, n, q, ld, k, ld, w[0], w[1], rot, p, yq, ld, yk, ld, s)
+        tpp.tpp_qk_norm_rope_backward(desc, n, q, ld, k, ld, w[0], w[1], rot, p, gq, ld, gk, ld, dq, ld, dk,
+                                      ld, dw[0], dw[1], s)
+        torch.cuda.synchronize()
+        return y, dx, dw
+
+    y, dx, dw = run(0, T)
+    for t0 in (0, 1234, T - part):
+        yp, dxp, _ = run(t0, part)
+        assert torch.equal(y[t0:t0 + part], yp) and torch.equal(dx[t0:t0 + part], dxp)
+    halves = [run(0, T // 2), run(T // 2, T - T // 2)]
+    for side in range(2):
+        # both are within (64 + rows) u of the sum of |g xn|, below rows * 64 for these normals
+        both = halves[0][2][side].double() + halves[1][2][side].double()
+        rows = T * (hq, hk)[side]
+        assert (dw[side].double() - both).abs().max() <= 2 * (64 + rows ** 0.5) * U * rows * 2
+        assert dw[side].abs().max() > 0
+
+
+def test_norm_rope_past_32_bits(tpp):
+    """Tokens more than 2^32 bytes apart."""
+    D, ld, T = 64, (1 << 31) + 72, 3
+    big = torch.zeros(ld * (T - 1) + 3 * D, dtype=torch.bfloat16, device="cuda")
+    small = torch.randn(T, 3 * D, device="cuda").bfloat16()
+    for t in range(T):
+        big[t * ld:t * ld + 3 * D] = small[t]
+    rot = torch.rand(8, D, device="cuda")
+    pos, w = torch.tensor([1, 7, 3], device="cuda"), torch.ones(D, device="cuda")
+    desc, s, res = tpp.tpp_qk_desc(D, D, tpp.TPP_ROT_HALVES, 2, 1, tpp.TPP_DT_BF16, EPS, 8), tpp.current_stream(), []
+    for x, l in ((small.clone(), 3 * D), (big, ld)):
+        p = x.data_ptr()
+        dw = torch.zeros(2, D, device="cuda")
+        g = small.flip(0).contiguous()
+        dx = torch.zeros_like(g)
+        tpp.tpp_qk_norm_rope_backward(desc, T, p, l, p + 4 * D, l, w, w, rot, pos, g, 3 * D, g.data_ptr() + 4 * D,
+                                      3 * D, dx, 3 * D, dx.data_ptr() + 4 * D, 3 * D, dw[0], dw[1], s)
+        tpp.tpp_qk_norm_rope(desc, T, p, l, p + 4 * D, l, w, w, rot, pos, p, l, p + 4 * D, l, s)   # in place
+        torch.cuda.synchronize()
+        y = torch.stack([x.reshape(-1)[t * l:t * l + 3 * D] for t in range(T)])
+        res.append((y, dx, dw))
+    for a, b in zip(*res):
+        assert torch.equal(a, b) and a.any()
+
+
 def test_backward_against_differences(tpp):
     """fp32 gradients against central differences of the GPU's own forward pass, all entries of one
     head moved along a random direction: the sum's curvature bounds the rest."""
@@ -513,6 +581,18 @@ def test_attention_long(tpp, n, L, D, hq, hk, dtype):
     check_attention(tpp, pc, hq, "bf16", max_len=L + 3000)
 
 
+def test_attention_nan_in_what_is_held_shows(tpp):
+    """A NaN among the held keys reaches the heads that read it, one among the values its entry alone."""
+    pc = Paged([70, 300], 64, 2, 16, "bf16", seed=4)
+    hold = lambda b, t, h: pc.row(b, t) + h * pc.strides[2]
+    pc.dev[0][hold(0, 33, 1)] = int(NAN["bf16"])
+    pc.dev[1][hold(1, 299, 0) + 5] = int(NAN["bf16"])
+    out, lse, _ = attend(tpp, pc, draw(pc.rng, (2, 4 * 64), "bf16"), 4, "f32", 0.125)
+    bad = np.isnan(out.reshape(2, 4, 64))
+    assert bad[0, 2:].all() and not bad[0, :2].any() and np.isnan(lse[0, 2:]).all()
+    assert bad[1, :2, 5].all() and bad[1].sum() == 2 and not np.isnan(lse[1]).any()
+
+
 def test_attention_past_32_bits(tpp):
     """Pages more than 2^32 bytes apart."""
     D, page, stride = 64, 16, (1 << 31) + 64
@@ -573,6 +653,13 @@ EVICT = [  # lens, budget, D, heads, page, dtype, kind of totals, positions
     ([3000, 1], 2999, 40, 1, 16, "bf16", "odd", None),
     ([5000, 4097, 2222], 1111, 16, 2, 32, "f32", "ties", 700),
     ([70, 80], 10, 64, 1, 16, "bf16", "random", 75),       # more protected than the budget holds
+    ([20000, 4097], 19999, 8, 1, 64, "bf16", "ties", 50),  # one leaves of more than 16 positions a thread
+    ([32768, 20001], 19000, 8, 1, 64, "bf16", "random", 50),
+    ([70000, 32769], 69990, 8, 1, 64, "bf16", "ties", 500),    # several parts
+    ([33000, 40000], 30000, 8, 1, 64, "f32", "odd", 3000),
+    ([2000, 1999], 1996, 64, 8, 16, "bf16", "equal", 100),     # a few leave, one by one
+    ([2000, 1999], 1997, 64, 8, 16, "bf16", "odd", None),
+    ([30, 29, 28], 26, 32, 2, 16, "bf16", "odd", 28),          # fewer candidates than have to leave
 ]
 
 
