@@ -623,8 +623,11 @@ void launch_dim(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t bytes
 
 int64_t attn_work_floats(const AttnParams& p) {
   const AttnPlan pl = plan(p, true);
+  // every grid below is in bounds before anything is multiplied further
+  const int64_t rows = p.n_seqs * p.q_heads, most = 0x7fffffff;
+  const int64_t units = (int64_t)p.kv_heads * pl.tiles * p.n_seqs, blocks = (p.max_len + AT - 1) / AT;
+  if (p.n_seqs > most || rows > most || units > most / pl.splits || rows + blocks * p.n_seqs > most) return -1;
   if (pl.splits == 1 && !p.totals_out) return 0;
-  const int64_t rows = p.n_seqs * p.q_heads;
   return rows * pl.splits * (p.d + 2) + (p.totals_out ? (rows + 1) * pl.score_ld : 0);
 }
 
@@ -635,8 +638,7 @@ hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
   const int64_t blocks = work && p.totals_out ? (p.max_len + jt - 1) / jt : 0;
   const int64_t wgs = (int64_t)pl.splits * p.kv_heads * pl.tiles * p.n_seqs;
   const int64_t joins = rows + blocks * p.n_seqs;
-  if (p.n_seqs > 0x7fffffff || wgs > 0x7fffffff || joins > 0x7fffffff)
-    return hipErrorInvalidConfiguration;
+  if (attn_work_floats(p) < 0 || wgs > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidConfiguration;
   if (work) {
     pl.o = work;
     pl.m = pl.o + rows * pl.splits * p.d;

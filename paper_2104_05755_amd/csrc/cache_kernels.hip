@@ -445,6 +445,7 @@ int64_t gone_words(const EvictParams& p) { return (p.max_len + 31) / 32 * 2; }
 }  // namespace
 
 int64_t evict_work_floats(const EvictParams& p) {
+  if (p.n_seqs > 0x7fffffff || move_cap(p) > (1 << 30) / p.kv_heads) return -1;
   return p.n_seqs * (2 * move_cap(p) + 1 + gone_words(p) / 2);
 }
 
@@ -464,7 +465,7 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   while (cs.lanes < cs.units && cs.lanes < 64) cs.lanes *= 2;
   cs.heads = FastDiv(p.kv_heads);
   const int64_t rows = ml.cap * p.kv_heads, chunks = rows * cs.units;   // of a sequence's moves
-  if (p.n_seqs > 0x7fffffff || rows > (1 << 30)) return hipErrorInvalidConfiguration;
+  if (evict_work_floats(p) < 0) return hipErrorInvalidConfiguration;
   const bool in_place = p.totals_out == p.totals && p.pos_out == p.pos;
   // A chunk or two per thread of the selecting workgroup, and totals that stay where they are or are few:
   // no second launch (32 sequences of 2049 that lose one position: 10.9 us so, 16.4 with a copy of its own;

@@ -317,6 +317,8 @@ struct AttnParams {
   int32_t page_size, q_heads, kv_heads, d, bf16, out_bf16;
   float scale;
 };
+// Floats of work space (-1: a launch would need more than 2^31 - 1 workgroups).  Without work space (null)
+// the launch is unsplit; one with totals has to have it.
 int64_t attn_work_floats(const AttnParams& p);
 hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream);
 
@@ -336,6 +338,7 @@ struct EvictParams {
   float* totals_out;
   int64_t* pos_out;
 };
+// Floats of work space (-1: more than the launches count).
 int64_t evict_work_floats(const EvictParams& p);
 hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream);
 

@@ -1206,6 +1206,7 @@ tpp_status tpp_paged_attention(const tpp_attn_desc* desc, const tpp_kv_cache* ca
   float* work = nullptr;
   std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
   const int64_t need = tpp::attn_work_floats(p);
+  if (need < 0) return fail(TPP_ERR_UNSUPPORTED, "attention needs more than 2^31 - 1 workgroups");
   if (tpp_status s = call_work(WORK_ATTENTION, stream, need, &work, hold)) return s;
   if (need > 0 && !work && totals_out)
     return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
@@ -1256,13 +1257,14 @@ tpp_status tpp_cache_evict(const tpp_kv_cache* cache, int64_t n_seqs, int64_t ma
   float* work = nullptr;
   std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
   const int64_t need = tpp::evict_work_floats(p);
+  const char* too_many = "eviction needs more than 2^31 - 1 workgroups, or 2^30 rows for one sequence's moves";
+  if (need < 0) return fail(TPP_ERR_UNSUPPORTED, "%s", too_many);
   if (tpp_status s = call_work(WORK_EVICT, stream, need, &work, hold)) return s;
   if (need > 0 && !work)
     return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
   const hipError_t e = tpp::launch_evict(p, work, static_cast<hipStream_t>(stream));
   if (e == hipErrorInvalidConfiguration)
-    return fail(TPP_ERR_UNSUPPORTED, "eviction needs more than 2^31 - 1 workgroups, or 2^30 rows for one "
-                "sequence's moves");
+    return fail(TPP_ERR_UNSUPPORTED, "%s", too_many);
   return launched("eviction", e);
 }
 

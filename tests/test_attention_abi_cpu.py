@@ -123,7 +123,8 @@ def test_append_refuses(tpp):
     (INV, {}, dict(ldq=255)), (INV, {}, dict(ldo=255)), (INV, {}, dict(ld_pages=2)),
     (INV, {}, dict(q=None)), (INV, {}, dict(out=None)), (INV, {}, dict(lens=None)),
     (INV, {}, dict(pages=None)), (INV, {}, dict(totals_in=P, ldt=40)),
-    (INV, {}, dict(totals_out=P, ldt=39))], ids=str)
+    (INV, {}, dict(totals_out=P, ldt=39)), (UNS, {}, dict(n=1 << 40)), (UNS, {}, dict(n=1 << 30)),
+    (UNS, dict(kv_heads=1), dict(q_heads=1 << 20, n=1 << 20))], ids=str)
 def test_attention_refuses(tpp, status, ckw, kw):
     refused(tpp, status, lambda: attend(tpp, cache(tpp, **ckw), **kw))
 
@@ -134,6 +135,12 @@ def test_attention_refuses(tpp, status, ckw, kw):
     dict(len_out=None), dict(pos=None), dict(horizon=None), dict(pos_out=None)], ids=str)
 def test_evict_refuses(tpp, kw):
     refused(tpp, INV, lambda: evict(tpp, cache(tpp), **kw))
+
+
+def test_evict_refuses_more_than_a_grid(tpp):
+    refused(tpp, UNS, lambda: evict(tpp, cache(tpp), n=1 << 40))
+    refused(tpp, UNS, lambda: evict(tpp, cache(tpp, kv_heads=64, page_size=1 << 28), max_len=1 << 30, ldt=1 << 30,
+                                    ld_pages=4))
 
 
 def test_nothing_to_do(tpp):
