@@ -105,7 +105,7 @@ struct AttnPlan {
   int32_t splits;     // spans of a sequence
   int32_t group;      // query heads of a key head
   int32_t tiles;      // query-head tiles of a key head
-  FastDiv div_splits, div_seqs, div_tiles, div_y;   // n_seqs, tiles, kv_heads * tiles
+  FastDiv div_splits, div_seqs, div_tiles;
   // Partial results (null: the workgroup writes the outputs): sums [row][split][D], then maxima and
   // sums of weights [row][split], row = sequence * q_heads + head; scores [row][score_ld] for totals, and a row that
   // takes what no query head's lanes store.
@@ -151,9 +151,9 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   const int col = lane & 15, grp = lane >> 4;
   // Spans first, each sequence's from another one on, then sequences, heads last.  Workgroups go to the 8
   // XCDs in turn: with every sequence's first span on the same XCD, the others had only the work of long
-  // sequences (64 of 1 to 8192: 293 us so, 234 turned).  With the heads first, which is even too (231), the
-  // interleaved rows of the heads are read at once, at a lower rate (64 of 4096: 211 us, 202 so; 32 of 2049
-  // to 4096 with totals 114 and 109).
+  // sequences (64 of 1 to 8192: 244 us so, 215 turned).  With the heads first, which is even too, the
+  // interleaved rows of the heads are read at once, at a lower rate (223 us; 64 of 4096 189, 180 so; 32 of
+  // 2049 to 4096 with totals 107 and 103).
   const int32_t ys = fdiv(blockIdx.x, pl.div_splits), sp = (int32_t)blockIdx.x - ys * pl.splits;
   const int32_t y = fdiv(ys, pl.div_seqs), seq = ys - y * (int32_t)p.n_seqs;
   const int32_t from = seq - fdiv(seq, pl.div_splits) * pl.splits;
@@ -560,8 +560,8 @@ int64_t range_of(const AttnParams& p) {
 
 // Tiles of 16 query heads per workgroup.  Two read the keys and values once for twice the heads, and have
 // the registers for it up to 128 entries a head, but one wavefront per SIMD: for more than 16 heads to a
-// key head and 32 MB of cache on (64 heads to one, 64 sequences of 8192: 136 us, 179 with one tile; 16 of
-// 4096 22.2 and 23.2; one sequence of 300, 24 heads to one 12.7 and 9.4).
+// key head and 32 MB of cache on (64 heads to one, 64 sequences of 8192: 81 us, 173 with one tile; 16 of
+// 4096 23.4 and 24.9; one sequence of 300, 24 heads to one 12.7 and 9.5).
 int32_t head_tiles(const AttnParams& p) {
   const int64_t bytes = range_of(p) * p.n_seqs * p.kv_heads * p.d * (p.bf16 ? 4 : 8);
   return p.q_heads / p.kv_heads > 16 && p.d <= 128 && bytes >= int64_t(32) << 20 ? 2 : 1;
@@ -569,7 +569,10 @@ int32_t head_tiles(const AttnParams& p) {
 
 // Spans that give the 256 compute units two workgroups each, as many as have the registers at once (one
 // of two head tiles), between a tile per wavefront and a block; `split` false: the whole sequence.  (Four
-// each: the odd fp32 case 28 us, 22.7 so; spans of two blocks: 64 sequences of 1 to 8192 261 us, 234 so.)
+// each: the odd fp32 case 26.4 us, 21.7 so; spans of two blocks: 64 sequences of 1 to 8192 235 us, 215 so.)
+// Two head tiles leave twice the partial results a span, and the start of a workgroup alone on its compute
+// unit is covered by nothing: up to four blocks (64 heads to one, 64 sequences of 8192 128 us with one, 81
+// so; 24 to one, 256 of 2000 to 4096 118 and 82; 32 heads of 64 to one, 64 of 1 to 8192 29 and 31).
 AttnPlan plan(const AttnParams& p, bool split) {
   AttnPlan pl = {};
   pl.group = p.q_heads / p.kv_heads;
@@ -580,10 +583,11 @@ AttnPlan plan(const AttnParams& p, bool split) {
   const int64_t units = p.n_seqs * p.kv_heads * pl.tiles;
   int64_t span = (range * units / (nt == 2 ? 256 : 512) + step - 1) / step * step;
   if (span < step) span = step;
-  if (span > BLOCK) span = BLOCK;
+  const int64_t most = (nt == 2 ? 4 : 1) * BLOCK;
+  if (span > most) span = most;
   // Few tiles to a sequence: their workgroup is done sooner than a second kernel has joined parts (one
-  // sequence of 512, 8 key heads of 128 bf16: 9.0 us either way, of 256 7.0 and 9.5; fp32 256 10.0 whole and
-  // 9.7; 16 sequences of 1024 bf16 16.1 and 17.8, of 512 fp32 16.3 and 19.3).
+  // sequence of 512, 8 key heads of 128 bf16: 9.3 us whole and 9.1, of 256 6.4 and 8.9; fp32 256 10.0 whole and
+  // 9.6; 16 sequences of 1024 bf16 18.3 and 18.9, of 512 fp32 17.2 and 20.0).
   const bool few = range <= keys * (units >= 128 ? 32 : p.bf16 ? 16 : 8);
   if (!split || few) span = range < step ? step : (range + step - 1) / step * step;
   pl.span = (int32_t)span;
@@ -592,7 +596,6 @@ AttnPlan plan(const AttnParams& p, bool split) {
   pl.div_seqs = FastDiv(p.n_seqs);
   pl.div_splits = FastDiv(pl.splits);
   pl.div_tiles = FastDiv(pl.tiles);
-  pl.div_y = FastDiv((int64_t)p.kv_heads * pl.tiles);
   return pl;
 }
 

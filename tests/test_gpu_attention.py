@@ -472,7 +472,7 @@ def check_attention(tpp, pc, hq, out_type, window=0, with_totals=False, max_len=
     q = draw(pc.rng, (n, hq * D + pad), dt, std)
     scale = D ** -0.5 if scale is None else scale
     cut = np.clip(pc.lens, 0, max_len) if max_len is not None else np.clip(pc.lens, 0, None)
-    ldt = int(max(1, cut.max(initial=0))) + 3
+    ldt = int(max(1, cut.max(initial=0), max_len or 0)) + 3
     totals = pc.rng.random((n, ldt)).astype(np.float32) if with_totals else None
     k, v = pc.host()
     args = (dt, D, pc.hk, pc.page, pc.n_pages, pc.strides, pc.pages, q, q.shape[1], hq, cut)
@@ -579,6 +579,18 @@ def test_attention_long(tpp, n, L, D, hq, hk, dtype):
     pc = Paged(lens, D, hk, 16, dtype, seed=L, room=3000)
     check_attention(tpp, pc, hq, "f32", with_totals=True)
     check_attention(tpp, pc, hq, "bf16", max_len=L + 3000)
+
+
+@pytest.mark.parametrize("D,hq,hk,page,dtype", [(128, 24, 1, 16, "bf16"), (128, 64, 1, 64, "f32"),
+                                                (77, 70, 2, 7, "bf16"), (64, 35, 1, 16, "f32")])
+def test_attention_two_head_tiles(tpp, D, hq, hk, page, dtype):
+    """Room for 8192 positions in 40 sequences: two tiles of query heads to a workgroup, whose span is of
+    more positions than it looks up at a time; some of those blocks hold nothing, some a single page."""
+    lens = [2700, 1500, 1025, 0, 1024, 2100] + list(range(34))
+    holes = [(0, j) for j in range(1030 // page, 2100 // page)] + [(5, j) for j in range(1024 // page + 1)]
+    pc = Paged(lens, D, hk, page, dtype, seed=hq, holes=holes, room=8192)
+    check_attention(tpp, pc, hq, "f32", max_len=8192, with_totals=True)
+    check_attention(tpp, pc, hq, "bf16", max_len=8192, window=5000)
 
 
 def test_attention_nan_in_what_is_held_shows(tpp):
