@@ -95,7 +95,7 @@ __device__ __forceinline__ float share(float m, float top) {
   return m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
 }
 
-constexpr int32_t BLOCK = 1024;   // positions whose addresses are in LDS at a time
+constexpr int32_t BLOCK = 1024;   // most positions whose addresses are in LDS at a time
 constexpr int JOINED = 4;         // partial results that a lane of the joining kernel has in flight
 constexpr int32_t MEET = 8;       // query heads whose sums are in LDS at a time
 
@@ -107,10 +107,11 @@ struct AttnPlan {
   int32_t tiles;      // query-head tiles of a key head
   FastDiv div_splits, div_seqs, div_tiles;
   // Partial results (null: the workgroup writes the outputs): sums [row][split][D], then maxima and
-  // sums of weights [row][split], row = sequence * q_heads + head; scores [row][score_ld] for totals, and a row that
-  // takes what no query head's lanes store.
+  // sums of weights [row][split], row = sequence * q_heads + head; scores [row][score_ld] for totals.
   float *o, *m, *l, *s;
-  int64_t score_ld;   // of a row of scores: max_len in whole tiles
+  int64_t score_ld;   // of a row of scores: max_len in an odd number of 256-byte lines
+  int32_t block;      // positions whose addresses, and with totals whose scores, are in LDS at a time
+  int32_t stage_ld;   // of a head's scores in LDS
 };
 
 // The kernel's shapes by type: keys of a tile, entries of a key step and of a lane's chunk of it.
@@ -143,6 +144,7 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 
   extern __shared__ __align__(16) char lds[];
   int64_t* rows = reinterpret_cast<int64_t*>(lds);   // byte offset of each position, bit 0: masked
+  float* stage = reinterpret_cast<float*>(rows + pl.block);   // scores [query head][stage_ld]
   __shared__ int32_t missing;   // 1 + the first position of the last block that lacks a page
   __shared__ int32_t first_held;
   __shared__ float wave_m[AW][NT * 16], wave_l[AW][NT * 16];
@@ -230,20 +232,10 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   }
   const float sl2 = p.scale * LOG2E;
 
-  // Where this lane's scores go: the row of its query head, or a row of nobody's.  (A branch around the
-  // stores, or around the next loads, would make the waits below wait for everything in flight.)
-  float* score[NT];
-  if constexpr (TOTALS)
-#pragma unroll
-    for (int q = 0; q < NT; ++q) {
-      const int64_t row = q * 16 + col < nq ? b * p.q_heads + h0 + q * 16 + col : p.n_seqs * p.q_heads;
-      score[q] = pl.s + row * pl.score_ld + grp * 4;
-    }
-
-  // The tile at i0 of the block at t0, whose loads have been issued; MORE: issues the next one's, the keys'
+  // The tile at i0 of a block, whose loads have been issued; MORE: issues the next one's, the keys'
   // as soon as the first product has read theirs, the values' after the second, so that one of the two is
   // always in flight.
-  const auto tile = [&](auto more, int32_t t0, int32_t i0, int32_t next) {
+  const auto tile = [&](auto more, int32_t i0, int32_t next) {
     constexpr bool MORE = decltype(more)::value;
     float sc[NT][VKEYS];
 #pragma unroll
@@ -281,13 +273,14 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
     if constexpr (MORE) load_k(next);   // behind the products that read the registers
     __builtin_amdgcn_sched_barrier(0);
 
-    if constexpr (TOTALS) {   // the scores
+    if constexpr (TOTALS) {   // the scores of the columns that are a query head's
 #pragma unroll
       for (int q = 0; q < NT; ++q)
+        if (q * 16 + col < nq)
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-          gst<f32x4_a4>(score[q] + t0 + i0 + u * 16,
-                        (f32x4){sc[q][4 * u], sc[q][4 * u + 1], sc[q][4 * u + 2], sc[q][4 * u + 3]});
+          for (int u = 0; u < SUB; ++u)
+            *reinterpret_cast<f32x4*>(stage + (q * 16 + col) * pl.stage_ld + i0 + u * 16 + grp * 4) =
+                (f32x4){sc[q][4 * u], sc[q][4 * u + 1], sc[q][4 * u + 2], sc[q][4 * u + 3]};
     }
     // ---- softmax: the maximum over the tile, the sums so far scaled down to it ------------------
     u32x4 hi[NT], lw[NT];
@@ -356,11 +349,11 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   };
 
   constexpr int32_t step = AW * KEYS, NONE = 0x7fffffff;
-  for (int32_t t0 = c0; t0 < c1; t0 += BLOCK) {
+  for (int32_t t0 = c0; t0 < c1; t0 += pl.block) {
     // ---- addresses of the block's rows --------------------------------------------------------------
     // A position outside the span's or the window's gets the row of the nearest one inside, masked.  Where
     // pages hold nothing, the first position that is held stands in for those that are not.
-    const int32_t cnt = c1 - t0 < BLOCK ? (c1 - t0 + KEYS - 1) / KEYS * KEYS : BLOCK;
+    const int32_t cnt = c1 - t0 < pl.block ? (c1 - t0 + KEYS - 1) / KEYS * KEYS : pl.block;
     __syncthreads();   // the block before is done with
     for (int32_t i = tid; i < cnt; i += AT) {
       const int32_t t = t0 + i, in = t < lo ? lo : t < c1 ? t : c1 - 1;
@@ -390,8 +383,18 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
     if (i0 < cnt) {
       load_k(i0);
       load_v(i0);
-      for (; i0 + step < cnt; i0 += step) tile(std::true_type(), t0, i0, i0 + step);
-      tile(std::false_type(), t0, i0, 0);
+      for (; i0 + step < cnt; i0 += step) tile(std::true_type(), i0, i0 + step);
+      tile(std::false_type(), i0, 0);
+    }
+    // ---- its scores: a query head's row to a wavefront ------------------------------------------------
+    // (Stored by each tile, 64 bytes of a head at a time: 32 sequences of 2049 to 4096 103 us, 95 so.)
+    if constexpr (TOTALS) {
+      __syncthreads();
+      for (int32_t h = wave; h < nq; h += AW) {
+        float* to = pl.s + (b * p.q_heads + h0 + h) * pl.score_ld + t0;
+        for (int32_t i = lane * 4; i < cnt; i += 256)
+          gst<f32x4_a4>(to + i, *reinterpret_cast<const f32x4*>(stage + h * pl.stage_ld + i));
+      }
     }
   }
 
@@ -592,7 +595,12 @@ AttnPlan plan(const AttnParams& p, bool split) {
   if (!split || few) span = range < step ? step : (range + step - 1) / step * step;
   pl.span = (int32_t)span;
   pl.splits = range > span ? (int32_t)((range + span - 1) / span) : 1;
-  pl.score_ld = (p.max_len + 31) / 32 * 32;
+  pl.score_ld = ((p.max_len + 63) / 64 | 1) * 64;
+  const int32_t heads = pl.group < 16 * nt ? pl.group : 16 * nt;
+  // at most 32 KB of scores, so that as many workgroups have room as have registers
+  pl.block = !p.totals_out || heads <= 8 ? BLOCK : heads <= 16 ? BLOCK / 2 : BLOCK / 4;
+  if (pl.block > span) pl.block = (int32_t)span;
+  pl.stage_ld = pl.block + 16;   // four heads' chunks at once to different banks
   pl.div_seqs = FastDiv(p.n_seqs);
   pl.div_splits = FastDiv(pl.splits);
   pl.div_tiles = FastDiv(pl.tiles);
@@ -631,7 +639,7 @@ int64_t attn_work_floats(const AttnParams& p) {
   const int64_t units = (int64_t)p.kv_heads * pl.tiles * p.n_seqs, blocks = (p.max_len + AT - 1) / AT;
   if (p.n_seqs > most || rows > most || units > most / pl.splits || rows + blocks * p.n_seqs > most) return -1;
   if (pl.splits == 1 && !p.totals_out) return 0;
-  return rows * pl.splits * (p.d + 2) + (p.totals_out ? (rows + 1) * pl.score_ld : 0);
+  return rows * pl.splits * (p.d + 2) + (p.totals_out ? 64 + rows * pl.score_ld : 0);
 }
 
 hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
@@ -646,11 +654,12 @@ hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
     pl.o = work;
     pl.m = pl.o + rows * pl.splits * p.d;
     pl.l = pl.m + rows * pl.splits;
-    pl.s = p.totals_out ? pl.l + rows * pl.splits : nullptr;
+    pl.s = p.totals_out ? work + (rows * pl.splits * (p.d + 2) + 63) / 64 * 64 : nullptr;   // whole lines
   }
   const int32_t nt = head_tiles(p), meet = pl.group < MEET ? pl.group : MEET;
-  const size_t addr = (size_t)(pl.span < BLOCK ? pl.span : BLOCK) * 8, part = (size_t)AW * meet * p.d * 4;
-  const size_t bytes = addr > part ? addr : part;
+  const int32_t heads = pl.group < 16 * nt ? pl.group : 16 * nt;
+  const size_t block = (size_t)pl.block * 8 + (pl.s ? (size_t)heads * pl.stage_ld * 4 : 0);
+  const size_t part = (size_t)AW * meet * p.d * 4, bytes = block > part ? block : part;
   const dim3 grid((uint32_t)wgs);
   if (p.bf16)
     nt == 1 ? launch_dim<true, 1>(p, pl, grid, bytes, stream)
