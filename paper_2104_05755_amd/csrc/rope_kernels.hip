@@ -12,6 +12,11 @@
 // 64 / lanes rows.  A part that is no multiple of a chunk ends with the chunk that ends with it, whose first
 // entries another lane counts and stores.  Rows that are too short for that: one per wavefront, a rotated
 // pair or an entry behind the rotated part to a lane, four rows in flight.
+//
+// 32 + 8 heads of 128 bf16, 8192 tokens: forward 33.0 us, 5.2 TB/s; backward 51.1 us with the fold of the
+// norm weights' gradients, 5.0 TB/s.  2048 tokens into a cache 10.8 us, 4.7 TB/s; one token 5.8 us from
+// call to call, 3.0 of them the kernel.  1533 tokens of 21 + 7 fp32 heads of 77, backward: 15.5 us, 2.6
+// TB/s: 20 chunks a row leave 12 of the 32 places of its lanes empty, and the fold is 4 us.
 #include <hip/hip_runtime.h>
 
 #include "brgemm_device.h"
