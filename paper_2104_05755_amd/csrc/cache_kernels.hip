@@ -14,7 +14,7 @@
 // chunk per lane -- or, where a sequence can lose only a few, by the selecting workgroup itself, since a
 // second launch would cost more than the copy.
 //
-// 8 key heads of 128 bf16: 8 sequences of 9001 to 16384 cut to 4096 55 us, of them 20 the selection, whose
+// 8 key heads of 128 bf16: 8 sequences of 9001 to 16384 cut to 4096 53 us, of them 18 the selection, whose
 // passes wait for each other, and 35 the copy, 5.3 TB/s; 32 of 2049 that lose one 7.5 us.
 #include <hip/hip_runtime.h>
 
@@ -41,7 +41,7 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 
 // What the selection leaves in the work space for the copy: per sequence a bit for each position, set
-// in the free places (words of 16), the number of moves, and their free
+// in the free places (words of 16; null where nothing is handed on), the number of moves, and their free
 // places and movers (cap of each).
 struct MoveLists {
   uint16_t* gone;
@@ -282,13 +282,13 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
     prefix = last;
     cut = last_t;
   } else if (want > 0) {
+    hist[2 * tid] = hist[2 * tid + 1] = 0;
+    __syncthreads();
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t mask = pass == 2 ? 1023u : 2047u;
       // the bits above the digit, which have to be those found
       const uint32_t found = pass == 0 ? 0u : pass == 1 ? 0xffe00000u : 0xfffffc00u;
-      for (int i = tid; i < BINS; i += ST) hist[i] = 0;
-      __syncthreads();
       for (int32_t part = 0; part < n; part += PART) {
         if (several) load_keys(part);
 #pragma unroll
@@ -297,6 +297,7 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
       }
       __syncthreads();
       const int32_t h0 = hist[2 * tid], h1 = hist[2 * tid + 1];   // two bins per thread
+      hist[2 * tid] = hist[2 * tid + 1] = 0;                      // for the next pass
       uint32_t all;
       const int32_t lo = (int32_t)before_me(h0 + h1, sums, all);   // candidates below them
       if (pass == 0) {
@@ -319,6 +320,10 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
       prefix |= (uint32_t)pick[0] << shift;
       rank -= pick[1];
       all_ties = rank + 1 == pick[2];
+      if (all_ties) {   // all of this prefix leave, whatever their other bits
+        prefix |= (1u << shift) - 1;
+        break;
+      }
     }
   }
   const int32_t left = n - gone_n;
@@ -369,11 +374,17 @@ __global__ __launch_bounds__(ST) void evict_select_kernel(EvictParams p, MoveLis
         if (place >> i & 1) to[pa++] = t + i;
         if (mover >> i & 1) from[ma++] = t + i;
       }
-      if (!FUSED && KPT >= 16 && t < n) {
-        // the free places' bits, 16 to a store
+      if (!FUSED && ml.gone) {   // the free places' bits, 16 to a store
+        if constexpr (KPT == 4) {
+          uint32_t w = place << 4 * (tid & 3);
+          w |= dpp_or_0<0xB1, 0xf>(w);   // lane ^ 1, lane ^ 2
+          w |= dpp_or_0<0x4E, 0xf>(w);
+          if (t < n && (tid & 3) == 0) gst<uint16_t>(ml.gone + b * ml.words + t / 16, (uint16_t)w);
+        } else if (t < n) {
 #pragma unroll
-        for (int i = 0; i < KPT; i += 16)
-          gst<uint16_t>(ml.gone + b * ml.words + t / 16 + i / 16, (uint16_t)(place >> i));
+          for (int i = 0; i < KPT; i += 16)
+            gst<uint16_t>(ml.gone + b * ml.words + t / 16 + i / 16, (uint16_t)(place >> i));
+        }
       }
     }
   const int32_t moves = places;
@@ -459,7 +470,8 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   ml.count = reinterpret_cast<int32_t*>(work);
   ml.to = ml.count + p.n_seqs;
   ml.from = ml.to + p.n_seqs * ml.cap;
-  ml.gone = reinterpret_cast<uint16_t*>(ml.from + p.n_seqs * ml.cap);
+  const bool in_place = p.totals_out == p.totals && p.pos_out == p.pos;
+  ml.gone = in_place ? nullptr : reinterpret_cast<uint16_t*>(ml.from + p.n_seqs * ml.cap);
   CopyShape cs;
   const int32_t bytes = p.d * p.es;
   cs.unit = bytes >= 16 ? 16 : 2;
@@ -469,7 +481,6 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   cs.heads = FastDiv(p.kv_heads);
   const int64_t rows = ml.cap * p.kv_heads, chunks = rows * cs.units;   // of a sequence's moves
   if (evict_work_floats(p) < 0) return hipErrorInvalidConfiguration;
-  const bool in_place = p.totals_out == p.totals && p.pos_out == p.pos;
   // A chunk or two per thread of the selecting workgroup, and totals that stay where they are or are few:
   // no second launch (32 sequences of 2049 that lose one position: 10.9 us so, 16.4 with a copy of its own;
   // one of 32768 that loses one and is handed on: 28.1 us so, 21.4 with the copy's workgroups).
@@ -482,7 +493,10 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
     else if (p.max_len <= 16 * ST) TPP_SELECT(16, true);
     else TPP_SELECT(32, true);
   } else {
-    if (p.max_len <= 16 * ST) TPP_SELECT(16, false);
+    // as few positions to a thread as do: with 16, the fewest that were turned in LDS, one sequence of 3082
+    // cut to 1541 18.3 us, 11.3 so
+    if (p.max_len <= 4 * ST) TPP_SELECT(4, false);
+    else if (p.max_len <= 16 * ST) TPP_SELECT(16, false);
     else TPP_SELECT(32, false);
     // two rows per set of lanes, at most 8192 workgroups (2048: 66.6 us for 8 x 16384 cut to 4096, 64.1 so)
     const int64_t want = (rows * cs.lanes + 2 * CT - 1) / (2 * CT);
