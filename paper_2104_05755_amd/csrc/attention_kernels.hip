@@ -156,14 +156,14 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, grp = lane >> 4;
-  // Spans first, each sequence's from another one on, then sequences, heads last.  Workgroups go to the 8
-  // XCDs in turn: with every sequence's first span on the same XCD, the others had only the work of long
-  // sequences (64 of 1 to 8192: 244 us so, 215 turned).  With the heads first, which is even too, the
-  // interleaved rows of the heads are read at once, at a lower rate (223 us; 64 of 4096 189, 180 so; 32 of
-  // 2049 to 4096 with totals 107 and 103).
+  // Spans first, those of each sequence and head from another one on, then sequences, heads last.
+  // Workgroups go to the 8 XCDs in turn: with every sequence's first span on the same XCD, the others had
+  // only the work of long sequences (64 of 1 to 8192: 244 us so, 215 turned by the sequence, which is as
+  // uneven for each head, 192 by both).  With the heads first the interleaved rows of the heads are read at
+  // once, at a lower rate (223 us; 64 of 4096 189, 180 so; 32 of 2049 to 4096 with totals 107 and 103).
   const int32_t ys = fdiv(blockIdx.x, pl.div_splits), sp = (int32_t)blockIdx.x - ys * pl.splits;
   const int32_t y = fdiv(ys, pl.div_seqs), seq = ys - y * (int32_t)p.n_seqs;
-  const int32_t from = seq - fdiv(seq, pl.div_splits) * pl.splits;
+  const int32_t from = seq + y - fdiv(seq + y, pl.div_splits) * pl.splits;
   const int32_t split = sp + from >= pl.splits ? sp + from - pl.splits : sp + from;
   const int32_t hk = fdiv(y, pl.div_tiles), ht = y - hk * pl.tiles;
   const int64_t b = seq;
@@ -581,6 +581,9 @@ int32_t head_tiles(const AttnParams& p) {
 // Two head tiles leave twice the partial results a span, and the start of a workgroup alone on its compute
 // unit is covered by nothing: up to four blocks (64 heads to one, 64 sequences of 8192 128 us with one, 81
 // so; 24 to one, 256 of 2000 to 4096 118 and 82; 32 heads of 64 to one, 64 of 1 to 8192 29 and 31).
+// Where blocks would make less than two rounds of workgroups, sequences of several lengths leave compute
+// units idle: half a block (22 of 0 to 1760, 16 heads to 16 of 64 30.0 us with a block, 25.6 so; 52 of 0 to
+// 8745, 8 heads to 2 of 32 34.2 and 29.3; of 96 39.3 and 40.0).
 AttnPlan plan(const AttnParams& p, bool split) {
   AttnPlan pl = {};
   pl.group = p.q_heads / p.kv_heads;
@@ -591,7 +594,7 @@ AttnPlan plan(const AttnParams& p, bool split) {
   const int64_t units = p.n_seqs * p.kv_heads * pl.tiles;
   int64_t span = (range * units / (nt == 2 ? 256 : 512) + step - 1) / step * step;
   if (span < step) span = step;
-  const int64_t most = (nt == 2 ? 4 : 1) * BLOCK;
+  const int64_t most = nt == 2 ? 4 * BLOCK : p.n_seqs > 1 && range * units < 1024 * BLOCK ? BLOCK / 2 : BLOCK;
   if (span > most) span = most;
   // Few tiles to a sequence: their workgroup is done sooner than a second kernel has joined parts (one
   // sequence of 512, 8 key heads of 128 bf16: 9.3 us whole and 9.1, of 256 6.4 and 8.9; fp32 256 10.0 whole and
