@@ -111,6 +111,8 @@ struct AttnPlan {
   int32_t group;      // query heads of a key head
   int32_t tiles;      // query-head tiles of a key head
   FastDiv div_splits, div_seqs, div_tiles;
+  int32_t round;      // workgroups of 8 spans of all key heads, where those go together, or 0
+  FastDiv div_round;
   // Partial results (null: the workgroup writes the outputs): sums [row][split][D], then maxima and
   // sums of weights [row][split], row = sequence * q_heads + head; scores [row][score_ld] for totals.
   float *o, *m, *l, *s;
@@ -161,9 +163,25 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   // only the work of long sequences (64 of 1 to 8192: 244 us so, 215 turned by the sequence, which is as
   // uneven for each head, 192 by both).  With the heads first the interleaved rows of the heads are read at
   // once, at a lower rate (223 us; 64 of 4096 189, 180 so; 32 of 2049 to 4096 with totals 107 and 103).
-  const int32_t ys = fdiv(blockIdx.x, pl.div_splits), sp = (int32_t)blockIdx.x - ys * pl.splits;
-  const int32_t y = fdiv(ys, pl.div_seqs), seq = ys - y * (int32_t)p.n_seqs;
-  const int32_t from = seq + y - fdiv(seq + y, pl.div_splits) * pl.splits;
+  // Where rows share lines with other heads' (plan()), all heads of a span follow each other on one XCD,
+  // whose L2 has what they share.
+  int32_t seq, sp, y, turn;
+  if (pl.round) {
+    const int32_t r = fdiv(blockIdx.x, pl.div_round), in = (int32_t)blockIdx.x - r * pl.round;
+    const int32_t u = r * 8 + (in & 7);
+    y = in >> 3;
+    seq = fdiv(u, pl.div_splits);
+    sp = u - seq * pl.splits;
+    if (seq >= p.n_seqs) return;   // of the last round
+    turn = seq;
+  } else {
+    const int32_t ys = fdiv(blockIdx.x, pl.div_splits);
+    sp = (int32_t)blockIdx.x - ys * pl.splits;
+    y = fdiv(ys, pl.div_seqs);
+    seq = ys - y * (int32_t)p.n_seqs;
+    turn = seq + y;
+  }
+  const int32_t from = turn - fdiv(turn, pl.div_splits) * pl.splits;
   const int32_t split = sp + from >= pl.splits ? sp + from - pl.splits : sp + from;
   const int32_t hk = fdiv(y, pl.div_tiles), ht = y - hk * pl.tiles;
   const int64_t b = seq;
@@ -612,6 +630,18 @@ AttnPlan plan(const AttnParams& p, bool split) {
   pl.div_seqs = FastDiv(p.n_seqs);
   pl.div_splits = FastDiv(pl.splits);
   pl.div_tiles = FastDiv(pl.tiles);
+  // Heads side by side in the cache whose rows are no whole lines: two workgroups read a line, and the bytes
+  // past L2 are those of whole lines unless they do so on one XCD.  With fewer workgroups than run at once
+  // all of a sequence's on one XCD would leave others idle.  (32 heads to 8, 64 sequences: of 96 bf16, 4096
+  // 171 us apart, 151 together; of 77, 1 to 8192 211 and 185; the odd fp32 case 21.6 and 20.8; 16 heads to
+  // 16 of 77, 22 of 0 to 1760 51.0 and 51.7.)
+  const int64_t lines = p.head_stride % 128 * (p.bf16 ? 2 : 4) % 128, spans = p.n_seqs * pl.splits;
+  const int64_t round = 8 * (int64_t)p.kv_heads * pl.tiles;
+  if (lines != 0 && p.kv_heads > 1 && p.head_stride < p.pos_stride && units * pl.splits >= 512 &&
+      (spans + 7) / 8 <= 0x7fffffff / round) {
+    pl.round = (int32_t)round;
+    pl.div_round = FastDiv(round);
+  }
   return pl;
 }
 
@@ -641,11 +671,13 @@ void launch_dim(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t bytes
 }  // namespace
 
 int64_t attn_work_floats(const AttnParams& p) {
-  const AttnPlan pl = plan(p, true);
   // every grid below is in bounds before anything is multiplied further
-  const int64_t rows = p.n_seqs * p.q_heads, most = 0x7fffffff;
+  const int64_t most = 0x7fffffff;
+  if (p.n_seqs > most || p.n_seqs * p.q_heads > most) return -1;
+  const AttnPlan pl = plan(p, true);
+  const int64_t rows = p.n_seqs * p.q_heads;
   const int64_t units = (int64_t)p.kv_heads * pl.tiles * p.n_seqs, blocks = (p.max_len + AT - 1) / AT;
-  if (p.n_seqs > most || rows > most || units > most / pl.splits || rows + blocks * p.n_seqs > most) return -1;
+  if (units > most / pl.splits || rows + blocks * p.n_seqs > most) return -1;
   if (pl.splits == 1 && !p.totals_out) return 0;
   return rows * pl.splits * (p.d + 2) + (p.totals_out ? 64 + rows * pl.score_ld : 0);
 }
@@ -655,7 +687,8 @@ hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
   const int64_t rows = p.n_seqs * p.q_heads;
   const int jt = pl.splits > 16 ? 1024 : AT;   // more wavefronts where there are many spans to join
   const int64_t blocks = work && p.totals_out ? (p.max_len + jt - 1) / jt : 0;
-  const int64_t wgs = (int64_t)pl.splits * p.kv_heads * pl.tiles * p.n_seqs;
+  const int64_t wgs = pl.round ? (p.n_seqs * pl.splits + 7) / 8 * pl.round
+                               : (int64_t)pl.splits * p.kv_heads * pl.tiles * p.n_seqs;
   const int64_t joins = rows + blocks * p.n_seqs;
   if (attn_work_floats(p) < 0 || wgs > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidConfiguration;
   if (work) {
