@@ -102,6 +102,7 @@ __device__ __forceinline__ float share(float m, float top) {
 
 constexpr int32_t BLOCK = 1024;   // most positions whose addresses are in LDS at a time
 constexpr int JOINED = 4;         // partial results that a lane of the joining kernel has in flight
+constexpr int SCORES = 16;        // heads whose scores of a position a lane has in flight
 constexpr int32_t MEET = 8;       // query heads whose sums are in LDS at a time
 
 // What one launch needs beside AttnParams.
@@ -551,6 +552,7 @@ __global__ __launch_bounds__(JW * 64) void attn_join_kernel(AttnParams p, AttnPl
   if (t - tid >= n) return;
   const int32_t used = n > lo ? (n - lo + pl.span - 1) / pl.span : 0;
   const bool held = t < n && t >= start && row_of(p, b, t) >= 0;
+  const float was = t < n && p.totals_in ? gld<float>(p.totals_in + b * p.ldt + t) : 0.0f;
   float total = 0.0f;
   for (int32_t hb = 0; hb < p.q_heads; hb += JW * 64) {
     __syncthreads();
@@ -568,15 +570,20 @@ __global__ __launch_bounds__(JW * 64) void attn_join_kernel(AttnParams p, AttnPl
     __syncthreads();
     const int32_t heads = p.q_heads - hb < JW * 64 ? p.q_heads - hb : JW * 64;
     if (held)
-      for (int32_t h = 0; h < heads; ++h) {
-        const float s = gld<float>(pl.s + (b * p.q_heads + hb + h) * pl.score_ld + t);
-        total += __builtin_amdgcn_exp2f(s - lse[h]);
+      // (one by one: 64 heads, 22 sequences of 0 to 54 15.1 us, 13.6 so)
+      for (int32_t h = 0; h < heads; h += SCORES) {
+        float s[SCORES];
+#pragma unroll
+        for (int u = 0; u < SCORES; ++u) {
+          const int32_t hu = h + u < heads ? h + u : heads - 1;
+          s[u] = gld<float>(pl.s + (b * p.q_heads + hb + hu) * pl.score_ld + t) - lse[hu];
+        }
+#pragma unroll
+        for (int u = 0; u < SCORES; ++u)
+          if (h + u < heads) total += __builtin_amdgcn_exp2f(s[u]);
       }
   }
-  if (t < n) {
-    const int64_t at = b * p.ldt + t;
-    gst<float>(p.totals_out + at, (p.totals_in ? gld<float>(p.totals_in + at) : 0.0f) + total);
-  }
+  if (t < n) gst<float>(p.totals_out + b * p.ldt + t, was + total);
 }
 
 // Positions of a sequence that can count, from a tile's first one on.
