@@ -26,8 +26,8 @@
 // but held positions is ever read.
 //
 // Bound by HBM where the cache is large.  32 heads to 8 of 128 bf16: 64 sequences of 4096 180 us, 6.0 TB/s;
-// 64 of 1 to 8192 214 us, 5.0 TB/s, 8 of them the join; one of 131072 97 us, 5.5 TB/s; 32 of 2049 to 4096
-// with totals 95 us, 4.3 TB/s.  One of 100 positions 5.4 us from call to call, 4.4 of them the kernel: the
+// 64 of 1 to 8192 192 us, 5.6 TB/s, 7 of them the join; one of 131072 97 us, 5.5 TB/s; 32 of 2049 to 4096
+// with totals 92 us, 4.4 TB/s.  One of 100 positions 5.4 us from call to call, 4.4 of them the kernel: the
 // loads of length, page, keys and values wait for each other.
 #include <hip/hip_runtime.h>
 
@@ -602,7 +602,7 @@ int32_t head_tiles(const AttnParams& p) {
 
 // Spans that give the 256 compute units two workgroups each, as many as have the registers at once (one
 // of two head tiles), between a tile per wavefront and a block; `split` false: the whole sequence.  (Four
-// each: the odd fp32 case 26.4 us, 21.7 so; spans of two blocks: 64 sequences of 1 to 8192 235 us, 215 so.)
+// each: the odd fp32 case 26.4 us, 21.7 so; spans of two blocks: 64 sequences of 1 to 8192 235 us, 215 with one.)
 // Two head tiles leave twice the partial results a span, and the start of a workgroup alone on its compute
 // unit is covered by nothing: up to four blocks (64 heads to one, 64 sequences of 8192 128 us with one, 81
 // so; 24 to one, 256 of 2000 to 4096 118 and 82; 32 heads of 64 to one, 64 of 1 to 8192 29 and 31).
@@ -640,8 +640,8 @@ AttnPlan plan(const AttnParams& p, bool split) {
   // Heads side by side in the cache whose rows are no whole lines: two workgroups read a line, and the bytes
   // past L2 are those of whole lines unless they do so on one XCD.  With fewer workgroups than run at once
   // all of a sequence's on one XCD would leave others idle.  (32 heads to 8, 64 sequences: of 96 bf16, 4096
-  // 171 us apart, 151 together; of 77, 1 to 8192 211 and 185; the odd fp32 case 21.6 and 20.8; 16 heads to
-  // 16 of 77, 22 of 0 to 1760 51.0 and 51.7.)
+  // 171 us apart, 151 together; of 77, 1 to 8192 211 and 185; 16 of 3000, of 80, 38.5 and 34.6; the odd
+  // fp32 case 21.8 and 21.1; but 16 heads to 16 of 77, 22 of 0 to 1760, 50.5 and 54.5.)
   const int64_t lines = p.head_stride % 128 * (p.bf16 ? 2 : 4) % 128, spans = p.n_seqs * pl.splits;
   const int64_t round = 8 * (int64_t)p.kv_heads * pl.tiles;
   if (lines != 0 && p.kv_heads > 1 && p.head_stride < p.pos_stride && units * pl.splits >= 512 &&
