@@ -483,8 +483,8 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   if (evict_work_floats(p) < 0) return hipErrorInvalidConfiguration;
   // A chunk or two per thread of the selecting workgroup, and totals that stay where they are or are few:
   // no second launch (32 sequences of 2049 that lose one position: 10.9 us so, 16.4 with a copy of its own;
-  // one of 32768 that loses one and is handed on: 28.1 us so, 21.4 with the copy's workgroups).
-  const bool fused = chunks <= FUSED_CHUNKS && (in_place || p.max_len <= 4 * ST);
+  // handed on and losing one: 4 of 8000 14.0 us so, 15.2 with the copy's workgroups, 4 of 16000 16.7 and 15.5).
+  const bool fused = chunks <= FUSED_CHUNKS && (in_place || p.max_len <= 8 * ST);
   const dim3 grid((uint32_t)p.n_seqs);
 #define TPP_SELECT(KPT, FUSED)                                                                    \
   hipLaunchKernelGGL((evict_select_kernel<KPT, FUSED>), grid, dim3(ST), 0, stream, p, ml, cs)

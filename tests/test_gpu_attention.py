@@ -672,6 +672,8 @@ EVICT = [  # lens, budget, D, heads, page, dtype, kind of totals, positions
     ([2000, 1999], 1996, 64, 8, 16, "bf16", "equal", 100),     # a few leave, one by one
     ([2000, 1999], 1997, 64, 8, 16, "bf16", "odd", None),
     ([30, 29, 28], 26, 32, 2, 16, "bf16", "odd", 28),          # fewer candidates than have to leave
+    ([8192, 4097, 20, 8191], 8189, 64, 2, 16, "bf16", "random", 90),   # one launch of several positions a thread
+    ([6000, 5901, 4500], 5900, 8, 2, 7, "f32", "ties", 300),
 ]
 
 
