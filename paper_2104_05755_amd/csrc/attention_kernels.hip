@@ -15,11 +15,12 @@
 // The order of the entries in the first product and of the keys in the second is free, which is what
 // lets both operands of each fit the layouts: no lane exchanges anything but the maximum.
 //   bf16: 32 keys a tile, v_mfma_f32_16x16x32_bf16; a lane loads whole chunks of V of 8 keys and turns
-//         them with byte permutes.  The weights enter as two bf16 parts, hi + lo, since one would cost
-//         an fp32 output 2^-9 of its value; the matrix instructions are far from being the bound.
+//         them with byte permutes.  The weights enter as three bf16 parts whose sum is the fp32 weight
+//         (8 bits of its 24 each); one would cost an fp32 output 2^-9 of its value, two 2^-17.
 //   fp32: 16 keys a tile, v_mfma_f32_16x16x4_f32, whose operands are single entries: nothing to turn.
 // Fewer queries than 16 leave columns of the instructions idle, which costs nothing: a tile of 16 KB
-// (128 entries a head) takes about 600 cycles of a SIMD's matrix unit, and 5000 of its share of HBM.
+// (128 entries a head) takes 512 cycles of a SIMD's matrix unit in bf16 (two parts of the weights 384, with
+// the same time of every call to 2%), 2048 in fp32, and 5000 or more of its share of HBM.
 //
 // The rows' addresses are looked up once per span and kept in LDS.  A position that is not held gets the
 // address of one that is, and a mark that sets its score to -inf: loads need no branches, and nothing
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
                 (f32x4){sc[q][4 * u], sc[q][4 * u + 1], sc[q][4 * u + 2], sc[q][4 * u + 3]};
     }
     // ---- softmax: the maximum over the tile, the sums so far scaled down to it ------------------
-    u32x4 hi[NT], lw[NT];
+    u32x4 parts[3][NT];
     float pr[NT][VKEYS];
 #pragma unroll
     for (int q = 0; q < NT; ++q) {
@@ -329,10 +330,14 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
       if constexpr (BF16) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float a = pr[q][2 * k], c = pr[q][2 * k + 1];
-          const uint32_t h = pack_bf16x2(a, c);
-          hi[q][k] = h;
-          lw[q][k] = pack_bf16x2(a - __uint_as_float(h << 16), c - __uint_as_float(h & 0xffff0000u));
+          float a = pr[q][2 * k], c = pr[q][2 * k + 1];
+#pragma unroll
+          for (int i = 0; i < 3; ++i) {   // what a part leaves is exact
+            const uint32_t w = pack_bf16x2(a, c);
+            parts[i][q][k] = w;
+            a -= __uint_as_float(w << 16);
+            c -= __uint_as_float(w & 0xffff0000u);
+          }
         }
       }
     }
@@ -351,10 +356,10 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
 #pragma unroll
           for (int q = 0; q < NT; ++q) {
             f32x4& o = acc[q][c * VC + j];
-            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                        __builtin_bit_cast(bf16x8, hi[q]), o, 0, 0, 0);
-            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                        __builtin_bit_cast(bf16x8, lw[q]), o, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+              o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                          __builtin_bit_cast(bf16x8, parts[i][q]), o, 0, 0, 0);
           }
         }
       } else {

@@ -871,3 +871,30 @@ def test_graph_replays(tpp):
             assert torch.equal(x, y)
         attend(tpp, big, draw(big.rng, (4, 512), "bf16"), 8, "f32", 0.1,
                totals=np.zeros((4, 6000), np.float32))
+
+
+# ---- weights in 32 bits -------------------------------------------------------------------------------
+@pytest.mark.parametrize("D,hq", [(64, 16), (128, 16), (256, 16), (128, 64)])
+def test_attention_weights_in_32_bits(tpp, D, hq):
+    """A bf16 cache, an fp32 output: the softmax weights keep their 32 bits.  Two positions, scores 0 and
+    s = q k exactly (one entry each), -4 <= s < 0; values 0 and 1, so that out = p = e^s / (1 + e^s).  In
+    u = 2^-24: the scaled score (its factor and its product) is off by 2 u |s| log2 e, e^s by 8 u for that,
+    by 2 u in the exponential; the sum of weights by half that; the sums and the quotient by 2 u each: below
+    20 u in all.  64 heads to one key head with room for 65536 positions are two head tiles a workgroup."""
+    n, room = 32, (65536 if hq == 64 else 0)
+    pc = Paged([2] * n, D, 1, 16, "bf16", room=room)
+    rng = np.random.default_rng(D + hq)
+    one = wk.bf16_bits(np.ones(1, np.float32))[0]
+    for b in range(n):
+        a = pc.row(b, 0)
+        k, v = (p[a:a + 2 * D].reshape(2, D) for p in pc.pool)
+        k[:], v[0], v[1] = 0, 0, one
+        k[1, b % D] = one
+    pc.dev = [up(p) for p in pc.pool]
+    s = wk.bf16_bits(-rng.uniform(2.0 ** -8, 4, (n, hq)).astype(np.float32)).reshape(n, hq)
+    q = np.zeros((n, hq, D), np.uint16)
+    q[np.arange(n), :, np.arange(n) % D] = s
+    out, _, _ = attend(tpp, pc, q.reshape(n, hq * D), hq, "f32", 1.0, max_len=room or 2)
+    p = 1 / (1 + np.exp(-values(s, "bf16").astype(np.float64)))
+    off = np.abs(out.reshape(n, hq, D) - p[..., None]) / p[..., None]
+    assert off.max() <= 20 * U, f"off by {off.max() / U:.0f} u"
