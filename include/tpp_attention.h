@@ -112,7 +112,9 @@ tpp_status tpp_qk_norm_rope_append(const tpp_qk_desc* desc, int64_t tokens, cons
  * t >= n - window:
  *     s_t = scale * (q . k_t),   lse = log sum_t exp(s_t),   p_t = exp(s_t - lse),   out = sum_t p_t v_t
  * A head with no such position gives out = 0 and lse = -inf.  Nothing that is stored at other places
- * (NaN included) has any influence. */
+ * (NaN included) has any influence.  An infinity among the values counted gives its entry that infinity
+ * (both signs, or a NaN: NaN), since every p_t is positive.  The sum is formed with exp(s_t - max s) and
+ * divided last: it has to stay in fp32's range. */
 typedef struct {
   int32_t q_heads;         /* a multiple of the cache's kv_heads                                  */
   int32_t out_type;

@@ -898,3 +898,39 @@ def test_attention_weights_in_32_bits(tpp, D, hq):
     p = 1 / (1 + np.exp(-values(s, "bf16").astype(np.float64)))
     off = np.abs(out.reshape(n, hq, D) - p[..., None]) / p[..., None]
     assert off.max() <= 20 * U, f"off by {off.max() / U:.0f} u"
+
+
+# ---- infinities -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,hq,hk,page,lens,window,room,std", [
+    (64, 4, 2, 16, [1, 2, 33, 100, 31], 0, 0, 1.0),
+    (77, 6, 3, 7, [300, 45, 513, 700], 40, 0, 1.0),
+    (128, 8, 2, 16, [3000, 2049, 17], 0, 0, 20.0),       # several spans, weights that 32 bits cannot hold
+    (64, 2, 1, 64, [20000], 0, 0, 1.0),
+    (256, 4, 1, 16, [600, 64], 0, 0, 20.0),
+    (64, 24, 1, 16, [1500, 33], 0, 65536, 1.0)], ids=str)   # (spans of several blocks, two head tiles)
+def test_attention_infinite_values(tpp, dtype, D, hq, hk, page, lens, window, room, std):
+    """sum p_t v_t with p_t > 0: one infinity among the held values is the entry's result, two signs or a NaN
+    are NaN; no other entry changes, and what lies outside the window or in unused places (NaN) counts nothing."""
+    holes = [(len(lens) - 1, 1)] if page < 64 else []
+    n, pad = len(lens), max(0, 40 - len(lens)) if room else 0
+    pc = Paged(list(lens) + [0] * pad, D, hk, page, dtype, seed=D, holes=holes, room=room)
+    inf = {"f32": np.float32(np.inf), "bf16": np.uint16(0x7F80)}[dtype]
+    neg = {"f32": np.float32(-np.inf), "bf16": np.uint16(0xFF80)}[dtype]
+    rng = np.random.default_rng(D)
+    for b in range(n):
+        lo = max(0, lens[b] - window) if window else 0
+        held = [t for t in range(lo, lens[b]) if pc.row(b, t) is not None]
+        first, last, some = held[0], held[-1], int(rng.choice(held))
+        for t, e, x in ((last, 1, inf), (last, 3, neg), (first, 5, inf), (some, 7, neg), (first, 2, inf),
+                        (last, 2, inf)):
+            pc.pool[1][pc.row(b, t) + e] = x
+        if lo > 0 and pc.row(b, lo - 1) is not None:   # outside the window
+            pc.pool[1][pc.row(b, lo - 1) + 8] = inf
+        if first != last:   # both signs, and a NaN beside an infinity
+            pc.pool[1][pc.row(b, first) + 4], pc.pool[1][pc.row(b, last) + 4] = inf, neg
+            pc.pool[1][pc.row(b, first) + 6], pc.pool[1][pc.row(b, last) + 6] = NAN[dtype], inf
+    pc.dev = [up(p) for p in pc.pool]
+    max_len = room or None
+    check_attention(tpp, pc, hq, "f32", window=window, with_totals=True, std=std, max_len=max_len)
+    check_attention(tpp, pc, hq, "bf16", window=window, std=std, max_len=max_len)
