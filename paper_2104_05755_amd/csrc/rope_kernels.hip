@@ -212,7 +212,7 @@ __device__ __forceinline__ Chunks chunks_of(const QkParams& p, int32_t c) {
 
 // Cosines and sines of the pairs of a lane's chunks: halves: entry e of both chunks; pairs: pair e / 2
 // of chunk A at e / 2, of chunk B at V / 2 + e / 2.  What is not turned (behind the rotated part, or of a
-// padding token: pos < 0) has cosine 1, sine 0, and reads nothing.
+// padding token: pos < 0) reads nothing and has cosine 1, sine 0.
 template <int V>
 __device__ __forceinline__ void load_angles(const QkParams& p, int64_t pos, int32_t a, int32_t b,
                                             bool turned, float (&c)[V], float (&s)[V]) {
@@ -239,24 +239,26 @@ __device__ __forceinline__ void load_angles(const QkParams& p, int64_t pos, int3
     s[e] = in ? gld<float>(row + half + i) : 0.0f;
   }
 }
-// The rotation of a lane's two chunks (the other way where back).
+// The rotation of a lane's two chunks (the other way where back).  What is not turned is left as it is: a
+// sine of 0 times an infinity would be NaN in an entry that has nothing to do with it.
 template <int V>
-__device__ __forceinline__ void turn(bool pairs, bool back, const float (&c)[V], const float (&s)[V],
-                                     float (&x)[V], float (&y)[V]) {
-  const auto one = [&](float& a, float& b, float co, float si) {
+__device__ __forceinline__ void turn(const QkParams& p, bool back, const Chunks& k, const float (&c)[V],
+                                     const float (&s)[V], float (&x)[V], float (&y)[V]) {
+  const auto one = [&](bool on, float& a, float& b, float co, float si) {
     if (back) si = -si;
-    const float t = a * co - b * si;
-    b = b * co + a * si;
-    a = t;
+    const float t = a * co - b * si, u = b * co + a * si;
+    a = on ? t : a;
+    b = on ? u : b;
   };
-  if (!pairs) {
+  if (!p.pairs) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) one(x[e], y[e], c[e], s[e]);
+    for (int e = 0; e < V; ++e) one(k.turned, x[e], y[e], c[e], s[e]);
   } else {
+    const int32_t half = p.rot_dim / 2;
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) {
-      one(x[2 * e], x[2 * e + 1], c[e], s[e]);
-      one(y[2 * e], y[2 * e + 1], c[V / 2 + e], s[V / 2 + e]);
+      one(k.a / 2 + e < half, x[2 * e], x[2 * e + 1], c[e], s[e]);
+      one(k.b / 2 + e < half, y[2 * e], y[2 * e + 1], c[V / 2 + e], s[V / 2 + e]);
     }
   }
 }
@@ -334,7 +336,7 @@ __global__ __launch_bounds__(QT) void qk_chunk_kernel(QkParams p, int32_t rows, 
     x[e] = r.pos < 0 ? 0.0f : x[e] * rstd * wa[e];
     y[e] = r.pos < 0 ? 0.0f : y[e] * rstd * wb[e];
   }
-  turn<V>(p.pairs, false, c, s, x, y);
+  turn<V>(p, false, k, c, s, x, y);
   if (in) {
     store_own<BF16, WHOLE, HOW>(r.out, r.to + a, x, k.dup_a);
     store_own<BF16, WHOLE, HOW>(r.out, r.to + b, y, k.dup_b);
@@ -383,7 +385,7 @@ __global__ __launch_bounds__(QT) void qk_backward_chunk_kernel(QkParams p, int32
     widen<BF16>(yw, y);
     widen<BF16>(gw, g);
     widen<BF16>(fw, f);
-    turn<V>(p.pairs, true, c, s, g, f);
+    turn<V>(p, true, k, c, s, g, f);
     const float xx = squares<V>(x, k.dup_a) + squares<V>(y, k.dup_b);
     float ux = 0.0f;
 #pragma unroll
@@ -573,9 +575,11 @@ __global__ __launch_bounds__(QT) void qk_backward_unit_kernel(QkParams p, int32_
       float xx = 0.0f, ux = 0.0f;
 #pragma unroll
       for (int i = 0; i < NU; ++i) {
-        const float g = ga[k][i] * c[k][i] + gb[k][i] * s[k][i];
-        gb[k][i] = gb[k][i] * c[k][i] - ga[k][i] * s[k][i];
-        ga[k][i] = g;
+        if (lane + 64 * i < p.rot_dim / 2) {   // (an entry alone: 0 times an infinity would be NaN)
+          const float g = ga[k][i] * c[k][i] + gb[k][i] * s[k][i];
+          gb[k][i] = gb[k][i] * c[k][i] - ga[k][i] * s[k][i];
+          ga[k][i] = g;
+        }
         xx += xa[k][i] * xa[k][i] + xb[k][i] * xb[k][i];
         ux += ga[k][i] * wa[i] * xa[k][i] + gb[k][i] * wb[i] * xb[k][i];
       }

@@ -934,3 +934,49 @@ def test_attention_infinite_values(tpp, dtype, D, hq, hk, page, lens, window, ro
     max_len = room or None
     check_attention(tpp, pc, hq, "f32", window=window, with_totals=True, std=std, max_len=max_len)
     check_attention(tpp, pc, hq, "bf16", window=window, std=std, max_len=max_len)
+
+
+ROPE_INF = [  # q heads, k heads, D, rot_dim, form, dtype: by whole chunks, by others, by units
+    (2, 1, 128, 64, "halves", "bf16"), (2, 1, 128, 0, "halves", "bf16"), (2, 1, 64, 32, "pairs", "bf16"),
+    (2, 1, 64, 32, "halves", "f32"), (2, 1, 64, 6, "pairs", "f32"), (2, 1, 77, 38, "halves", "bf16"),
+    (2, 1, 77, 32, "pairs", "f32"), (2, 1, 77, 0, "halves", "f32"), (2, 1, 77, 76, "pairs", "f32"),
+    (2, 1, 72, 36, "halves", "f32"), (2, 1, 9, 4, "halves", "f32"), (2, 1, 6, 2, "pairs", "bf16"),
+    (2, 1, 511, 10, "halves", "f32")]
+
+
+@pytest.mark.parametrize("case", ROPE_INF, ids=str)
+def test_norm_rope_infinities_behind_the_rotated_part(tpp, case):
+    """An entry that is not rotated meets no other: an infinite weight shows in that entry's outputs alone, an
+    infinite gradient in its own dw and, by the mean, in its head's dx."""
+    hq, hk, D, R, form, dtype = case
+    T, inf = 5, {"f32": np.float32(np.inf), "bf16": np.uint16(0x7F80)}[dtype]
+    for e in sorted({R, R + 1, (R + D) // 2, D - 1} - {D}):
+        r = Rope((T, hq, hk, D, R, form, dtype, 0, 0), e)
+        r.pos[:] = np.arange(T) % 4
+        r.dev["pos"] = up(r.pos)
+        w = r.w[0].copy()
+        r.w[0][e] = np.float32(np.inf)
+        r.dev["w"] = [up(x) for x in r.w]
+        outs = [up(np.full(T * h * D, NAN[dtype])) for h in (hq, hk)]
+        tpp.tpp_qk_norm_rope(r.desc(tpp), T, r.at[0], r.ld, r.at[1], r.ld, r.dev["w"][0], r.dev["w"][1],
+                             r.dev["rot"], r.dev["pos"], outs[0], hq * D, outs[1], hk * D, tpp.current_stream())
+        torch.cuda.synchronize()
+        ref = r.ref(0)
+        assert np.isinf(ref[..., e]).all() and np.isfinite(np.delete(ref, e, -1)).all()
+        rest = np.abs(np.delete(ref, e, -1)).max(-1, keepdims=True)
+        close(down(outs[0], dtype).reshape(T, hq, D), ref, 64 * U * (1 + D / 64) * rest, dtype, f"entry {e}")
+        r.w[0] = w
+        r.dev["w"] = [up(x) for x in r.w]
+        g = [draw(np.random.default_rng(e), (T, h * D + 1), dtype) for h in (hq, hk)]
+        g[0][3, D + e] = inf           # token 3, head 1
+        outs, dw = run_backward(tpp, r, g)
+        with np.errstate(invalid="ignore"):
+            dx, ref_w = oracle.qk_norm_rope_backward(r.flat[r.off[0]:], r.ld, hq, D, R, form, r.w[0], r.rot,
+                                                     r.pos, EPS, dtype, g[0], hq * D + 1)
+            bx, bw = gradient_bounds(r, 0, g[0], dx)
+        assert np.isinf(ref_w[e]) and np.isfinite(np.delete(ref_w, e)).all()
+        gf = g[0].copy()
+        gf[3, D + e] = 0
+        _, bw = gradient_bounds(r, 0, gf, dx)
+        close(dw[0].cpu().numpy()[:D], ref_w, (64 + T * hq) * U * bw, "f32", f"dw, entry {e}")
+        close(down(outs[0], dtype).reshape(T, hq, D), dx, bx, dtype, f"dx, entry {e}")
