@@ -154,7 +154,10 @@ tpp_status tpp_paged_attention(const tpp_attn_desc* desc, const tpp_kv_cache* ca
  * has to move.  A moved position whose page (old or new) holds nothing moves no keys or values.
  * Outputs may be the inputs themselves; otherwise they must not overlap them.  d_pos, d_horizon and
  * pos_out are given or NULL together.  No two sequences that lose positions may share a page.
- * Work buffer and its errors as tpp_reduce (a capture without one: NO_MEMORY).
+ * Where no sequence can move more than a few rows (2048 chunks of 16 bytes of the keys: max_len - budget,
+ * or half of max_len if that is less, times kv_heads times those of a row) and the totals stay in place or
+ * max_len is at most 8192, one launch without work space; else work buffer and its errors as tpp_reduce
+ * (a capture without one: NO_MEMORY).
  * Errors: INVALID_ARG for sizes < 0, max_len > 2^30, ldt < max_len, a malformed cache or a NULL
  * pointer when there is work; UNSUPPORTED for a launch of more than 2^31 - 1 workgroups, or where the
  * moves of one sequence could be more than 2^30 rows (positions * kv_heads). */

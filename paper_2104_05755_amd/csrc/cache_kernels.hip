@@ -456,22 +456,7 @@ int64_t move_cap(const EvictParams& p) {
 // Words of 16 bits of a sequence: a thread writes all of its own, up to 32 positions.
 int64_t gone_words(const EvictParams& p) { return (p.max_len + 31) / 32 * 2; }
 
-}  // namespace
-
-int64_t evict_work_floats(const EvictParams& p) {
-  if (p.n_seqs > 0x7fffffff || move_cap(p) > (1 << 30) / p.kv_heads) return -1;
-  return p.n_seqs * (2 * move_cap(p) + 1 + gone_words(p) / 2);
-}
-
-hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
-  MoveLists ml;
-  ml.cap = move_cap(p);
-  ml.words = gone_words(p);
-  ml.count = reinterpret_cast<int32_t*>(work);
-  ml.to = ml.count + p.n_seqs;
-  ml.from = ml.to + p.n_seqs * ml.cap;
-  const bool in_place = p.totals_out == p.totals && p.pos_out == p.pos;
-  ml.gone = in_place ? nullptr : reinterpret_cast<uint16_t*>(ml.from + p.n_seqs * ml.cap);
+CopyShape copy_shape(const EvictParams& p) {
   CopyShape cs;
   const int32_t bytes = p.d * p.es;
   cs.unit = bytes >= 16 ? 16 : 2;
@@ -479,29 +464,55 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   cs.lanes = 1;
   while (cs.lanes < cs.units && cs.lanes < 64) cs.lanes *= 2;
   cs.heads = FastDiv(p.kv_heads);
-  const int64_t rows = ml.cap * p.kv_heads, chunks = rows * cs.units;   // of a sequence's moves
+  return cs;
+}
+
+// Totals and positions stay where they are.
+bool in_place(const EvictParams& p) { return p.totals_out == p.totals && p.pos_out == p.pos; }
+
+// Whether the selecting workgroup hands on and copies what there is itself, with its lists in LDS and no work
+// space: a chunk or two per thread, and totals that stay where they are or are few (32 sequences of 2049
+// that lose one position: 10.9 us so, 16.4 with a copy of its own; handed on and losing one: 4 of 8000
+// 14.0 us so, 15.2 with the copy's workgroups, 4 of 16000 16.7 and 15.5).
+bool one_launch(const EvictParams& p) {
+  return move_cap(p) * p.kv_heads * copy_shape(p).units <= FUSED_CHUNKS && (in_place(p) || p.max_len <= 8 * ST);
+}
+
+}  // namespace
+
+int64_t evict_work_floats(const EvictParams& p) {
+  if (p.n_seqs > 0x7fffffff || move_cap(p) > (1 << 30) / p.kv_heads) return -1;
+  if (one_launch(p)) return 0;
+  return p.n_seqs * (2 * move_cap(p) + 1 + gone_words(p) / 2);
+}
+
+hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
   if (evict_work_floats(p) < 0) return hipErrorInvalidConfiguration;
-  // A chunk or two per thread of the selecting workgroup, and totals that stay where they are or are few:
-  // no second launch (32 sequences of 2049 that lose one position: 10.9 us so, 16.4 with a copy of its own;
-  // handed on and losing one: 4 of 8000 14.0 us so, 15.2 with the copy's workgroups, 4 of 16000 16.7 and 15.5).
-  const bool fused = chunks <= FUSED_CHUNKS && (in_place || p.max_len <= 8 * ST);
+  const CopyShape cs = copy_shape(p);
+  MoveLists ml = {};
+  ml.cap = move_cap(p);
   const dim3 grid((uint32_t)p.n_seqs);
 #define TPP_SELECT(KPT, FUSED)                                                                    \
   hipLaunchKernelGGL((evict_select_kernel<KPT, FUSED>), grid, dim3(ST), 0, stream, p, ml, cs)
-  if (fused) {
+  if (one_launch(p)) {
     if (p.max_len <= 4 * ST) TPP_SELECT(4, true);
     else if (p.max_len <= 16 * ST) TPP_SELECT(16, true);
     else TPP_SELECT(32, true);
   } else {
+    ml.words = gone_words(p);
+    ml.count = reinterpret_cast<int32_t*>(work);
+    ml.to = ml.count + p.n_seqs;
+    ml.from = ml.to + p.n_seqs * ml.cap;
+    ml.gone = in_place(p) ? nullptr : reinterpret_cast<uint16_t*>(ml.from + p.n_seqs * ml.cap);
     // as few positions to a thread as do: with 16, the fewest that were turned in LDS, one sequence of 3082
     // cut to 1541 18.3 us, 11.3 so
     if (p.max_len <= 4 * ST) TPP_SELECT(4, false);
     else if (p.max_len <= 16 * ST) TPP_SELECT(16, false);
     else TPP_SELECT(32, false);
     // two rows per set of lanes, at most 8192 workgroups (2048: 66.6 us for 8 x 16384 cut to 4096, 64.1 so)
-    const int64_t want = (rows * cs.lanes + 2 * CT - 1) / (2 * CT);
+    const int64_t want = (ml.cap * p.kv_heads * cs.lanes + 2 * CT - 1) / (2 * CT);
     const int64_t most = 8192 / p.n_seqs > 0 ? 8192 / p.n_seqs : 1;
-    const int64_t hand = in_place ? 0 : (p.max_len + 4 * CT - 1) / (4 * CT);
+    const int64_t hand = in_place(p) ? 0 : (p.max_len + 4 * CT - 1) / (4 * CT);
     const int64_t per = hand + (want < most ? want : most);
     if (per * p.n_seqs > 0x7fffffff) return hipErrorInvalidConfiguration;
     if (per > 0)

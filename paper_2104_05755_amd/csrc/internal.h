@@ -338,7 +338,7 @@ struct EvictParams {
   float* totals_out;
   int64_t* pos_out;
 };
-// Floats of work space (-1: more than the launches count).
+// Floats of work space (0: one launch without any; -1: more than the launches count).
 int64_t evict_work_floats(const EvictParams& p);
 hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream);
 
