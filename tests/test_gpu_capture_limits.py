@@ -9,8 +9,13 @@ import os
 import subprocess
 import sys
 
+import numpy as np
 import pytest
 import torch
+
+import oracle
+from helpers import values
+from test_gpu_attention import U, Paged, close, draw, up
 
 pytestmark = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -31,6 +36,42 @@ def captured(calls):
         g.replay()
         torch.cuda.synchronize()
     return g
+
+
+@pytest.mark.parametrize("D,hq,hk,dtype,max_len", [(128, 64, 4, "bf16", 1 << 25), (77, 64, 4, "f32", 1 << 26),
+                                                   (128, 64, 1, "bf16", 1 << 27)])
+def test_attention_captured_without_work_space(D, hq, hk, dtype, max_len):
+    """Room for sequences so long that the partial results (512 heads' spans, at most 4096 positions each)
+    would pass what captures may take: a span of several blocks for every sequence, the outputs written
+    directly."""
+    import paper_2104_05755_amd as tpp
+    lens, f, scale = [3000, 2500, 1025, 1024, 700, 0, 5, 2049], hq * D, D ** -0.5
+    pc = Paged(lens, D, hk, 1024, dtype, seed=D, holes=[(0, 1), (3, 0), (7, 2)], room=max_len)
+    n, q = len(lens), draw(pc.rng, (len(lens), f), dtype)
+    out, lse = torch.full((n, f), 9.0, device="cuda"), torch.full((n, hq), 9.0, device="cuda")
+    qd, desc = up(q), tpp.tpp_attn_desc(hq, tpp.TPP_DT_F32, scale, 0, max_len)
+    print(f"attention D{D} {hq}x{hk} {dtype} max_len {max_len}, captured", flush=True)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        tpp.tpp_paged_attention(desc, pc.c(tpp), n, qd, f, pc.d_lens, pc.d_pages, pc.pages.shape[1], out, f, lse,
+                                None, None, 0, s.cuda_stream)
+    k, v = pc.host()
+    mag = {"f32": np.abs, "bf16": lambda x: x & 0x7FFF}[dtype]
+    args = (dtype, D, hk, 1024, pc.n_pages, pc.strides, pc.pages, q, f, hq, lens, scale)
+    ref, ref_lse, _ = oracle.paged_attention(k, v, *args)
+    big, _, _ = oracle.paged_attention(k, mag(v), *args)
+    # the bounds of test_gpu_attention
+    qn = np.abs(values(q, dtype)).reshape(n, hq, D).sum(-1)
+    ds = (D + 4) * U * scale * qn * np.nanmax(np.abs(values(k, dtype)))
+    rel = 2 * ds + (64 + max(lens)) * U + 2.0 ** -20
+    for _ in range(2):
+        out.fill_(9), lse.fill_(9)
+        g.replay()
+        torch.cuda.synchronize()
+        close(out.cpu().numpy().reshape(n, hq, D), ref, (rel + (2.0 ** -16 if dtype == "bf16" else 0))[..., None] * big,
+              "f32", "out")
+        close(lse.cpu().numpy().astype(np.float64), ref_lse, rel, "f32", "lse")
 
 
 CODE = r"""
