@@ -52,8 +52,8 @@ typedef struct {
 /* Forward.  d_pos: device int64[tokens].  q_out / k_out may be q / k themselves (same ld); otherwise
  * outputs must not overlap inputs.  tokens == 0 is a no-op.
  * Errors: INVALID_ARG for a NULL desc, sizes, flags or leading dimensions (each >= heads * D) out of
- * their ranges, or a NULL pointer when there is work; UNSUPPORTED for D above 512 or a launch of more
- * than 2^31 - 1 workgroups; HIP if the launch fails. */
+ * their ranges, or a NULL pointer when there is work; UNSUPPORTED for D above 512 or more than 2^20
+ * heads; HIP if a launch fails. */
 tpp_status tpp_qk_norm_rope(const tpp_qk_desc* desc, int64_t tokens, const void* q, int64_t ldq,
                             const void* k, int64_t ldk, const float* wq, const float* wk,
                             const float* rot, const int64_t* d_pos, void* q_out, int64_t ldqo,

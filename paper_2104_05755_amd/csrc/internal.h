@@ -269,6 +269,9 @@ const char* equation_compile(const tpp_eq_node* nodes, int32_t n_nodes, int32_t 
                              EqProgram& prog, bool* too_many_tmps);
 hipError_t launch_equation(const EqProgram& prog, hipStream_t stream);
 
+// Workgroups of `threads` threads that one launch can have: a grid has fewer than 2^32 threads.
+constexpr int64_t most_groups(int64_t threads) { return 0xffffffffLL / threads; }
+
 // Norms and rotation of query and key heads (rope_kernels.hip).  A side is the heads of the queries or
 // of the keys.
 struct QkSide {

@@ -696,8 +696,9 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
   if (per == 0) return hipSuccess;
   const int32_t units = p.d - p.rot_dim / 2;
   const FastDiv div(per);
-  // rows count in 32 bits within a launch
-  const int64_t step = 0x7fff0000 / per;
+  // rows count in 31 bits within a launch, and threads in 32
+  const int32_t wg = QW * rows_at_once(p);
+  const int64_t most = most_groups(QT) * wg, step = (most < 0x7fff0000 ? most : 0x7fff0000) / per;
   for (int64_t t0 = 0; t0 < p.tokens; t0 += step) {
     QkParams q = p;
     q.tokens = p.tokens - t0 < step ? p.tokens - t0 : step;
@@ -711,7 +712,7 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
       q.slot += t0;
     }
     q.pos += t0;
-    const int32_t rows = (int32_t)(q.tokens * per), wg = QW * rows_at_once(p);
+    const int32_t rows = (int32_t)(q.tokens * per);
     const dim3 grid((uint32_t)(((int64_t)rows + wg - 1) / wg));
 #define TPP_QK(LANES, BF16, WHOLE, HOW)                                                             \
   case LANES:                                                                                       \

@@ -980,3 +980,25 @@ def test_norm_rope_infinities_behind_the_rotated_part(tpp, case):
         _, bw = gradient_bounds(r, 0, gf, dx)
         close(dw[0].cpu().numpy()[:D], ref_w, (64 + T * hq) * U * bw, "f32", f"dw, entry {e}")
         close(down(outs[0], dtype).reshape(T, hq, D), dx, bx, dtype, f"dx, entry {e}")
+
+
+def test_norm_rope_more_rows_than_a_grid(tpp):
+    """Heads of one entry go 16 to a workgroup: more than 2^28 of them would pass a grid's 2^32 threads.  In
+    place; the bound of this file's head with two u more for the reference in fp32."""
+    T, heads = (1 << 18) + 5, 1024
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn(T, heads, generator=g, device="cuda").bfloat16()
+    pos = torch.zeros(T, dtype=torch.int64, device="cuda")
+    pos[7::1000] = -1
+    pos[-2] = -1
+    w = torch.tensor([1.25], device="cuda")
+    ref = x.float()
+    ref = ref / torch.sqrt(ref * ref + EPS) * w
+    ref[pos < 0] = 0
+    desc = tpp.tpp_qk_desc(1, 0, tpp.TPP_ROT_HALVES, heads, 0, tpp.TPP_DT_BF16, EPS, 1)
+    print(f"norm of {T} x {heads} heads of one entry", flush=True)
+    tpp.tpp_qk_norm_rope(desc, T, x, heads, None, 0, w, None, None, pos, x, heads, None, 0, tpp.current_stream())
+    torch.cuda.synchronize()
+    off = (x.float() - ref).abs()
+    assert bool((off <= ref.abs() * (2.0 ** -8 + 70 * U)).all()) and bool((ref[-1] != 0).any())
