@@ -133,8 +133,10 @@ typedef struct {
  * Long caches are split over workgroups whose partial results (and, for totals, the scores) go to a
  * work buffer as tpp_reduce's do, under stream capture to one of the capture's own; where a capture
  * can have none, the launch is unsplit, and one with totals fails with NO_MEMORY.
- * Errors: INVALID_ARG as above and for a malformed desc or cache; UNSUPPORTED for other D or a launch
- * of more than 2^31 - 1 workgroups; NO_MEMORY; HIP if the launch fails. */
+ * Errors: INVALID_ARG as above and for a malformed desc or cache; UNSUPPORTED for other D, max_len above
+ * 2^30 or a launch of 2^32 threads or more, before anything is done (256 for each span of 64 to 4096
+ * positions of each key head of each sequence, and, where those are joined, for each of the q_heads *
+ * n_seqs rows); NO_MEMORY; HIP if a launch fails. */
 tpp_status tpp_paged_attention(const tpp_attn_desc* desc, const tpp_kv_cache* cache, int64_t n_seqs,
                                const void* q, int64_t ldq, const int64_t* d_len,
                                const int64_t* d_pages, int64_t ld_pages, void* out, int64_t ldo,
@@ -159,7 +161,8 @@ tpp_status tpp_paged_attention(const tpp_attn_desc* desc, const tpp_kv_cache* ca
  * max_len is at most 8192, one launch without work space; else work buffer and its errors as tpp_reduce
  * (a capture without one: NO_MEMORY).
  * Errors: INVALID_ARG for sizes < 0, max_len > 2^30, ldt < max_len, a malformed cache or a NULL
- * pointer when there is work; UNSUPPORTED for a launch of more than 2^31 - 1 workgroups, or where the
+ * pointer when there is work; UNSUPPORTED for a launch of 2^32 threads or more (1024 for each
+ * sequence, 256 for each 1024 positions of max_len where totals are not in place), or where the
  * moves of one sequence could be more than 2^30 rows (positions * kv_heads). */
 tpp_status tpp_cache_evict(const tpp_kv_cache* cache, int64_t n_seqs, int64_t max_len, int64_t budget,
                            const int64_t* d_len, const int64_t* d_pages, int64_t ld_pages,

@@ -716,29 +716,35 @@ void launch_dim(const AttnParams& p, const AttnPlan& pl, dim3 grid, size_t bytes
   else launch_tail<BF16, 256, 1>(p, pl, grid, bytes, stream);
 }
 
+// Workgroups of the attention, and of the join with `threads` each.
+int64_t groups(const AttnParams& p, const AttnPlan& pl) {
+  return pl.round ? (p.n_seqs * pl.splits + 7) / 8 * pl.round
+                  : (int64_t)pl.splits * p.kv_heads * pl.tiles * p.n_seqs;
+}
+int64_t joins(const AttnParams& p, int threads) {
+  return p.n_seqs * p.q_heads + (p.totals_out ? (p.max_len + threads - 1) / threads * p.n_seqs : 0);
+}
+
 }  // namespace
 
 int64_t attn_work_floats(const AttnParams& p) {
   // every grid below is in bounds before anything is multiplied further
-  const int64_t most = 0x7fffffff;
-  if (p.n_seqs > most || p.n_seqs * p.q_heads > most) return -1;
+  const int64_t most = most_groups(AT);
+  if (p.n_seqs > most || p.n_seqs * p.q_heads > 0x7fffffff) return -1;
   const AttnPlan pl = plan(p, true);
-  const int64_t rows = p.n_seqs * p.q_heads;
-  const int64_t units = (int64_t)p.kv_heads * pl.tiles * p.n_seqs, blocks = (p.max_len + AT - 1) / AT;
-  if (units > most / pl.splits || rows + blocks * p.n_seqs > most) return -1;
+  const int64_t rows = p.n_seqs * p.q_heads, units = (int64_t)p.kv_heads * pl.tiles * p.n_seqs;
+  if (units > most / pl.splits || groups(p, pl) > most) return -1;
   if (pl.splits == 1 && !p.totals_out) return 0;
+  if (joins(p, AT) > most) return -1;
   return rows * pl.splits * (p.d + 2) + (p.totals_out ? 64 + rows * pl.score_ld : 0);
 }
 
 hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
+  if (attn_work_floats(p) < 0) return hipErrorInvalidConfiguration;
   AttnPlan pl = plan(p, work != nullptr);
   const int64_t rows = p.n_seqs * p.q_heads;
-  const int jt = pl.splits > 16 ? 1024 : AT;   // more wavefronts where there are many spans to join
-  const int64_t blocks = work && p.totals_out ? (p.max_len + jt - 1) / jt : 0;
-  const int64_t wgs = pl.round ? (p.n_seqs * pl.splits + 7) / 8 * pl.round
-                               : (int64_t)pl.splits * p.kv_heads * pl.tiles * p.n_seqs;
-  const int64_t joins = rows + blocks * p.n_seqs;
-  if (attn_work_floats(p) < 0 || wgs > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidConfiguration;
+  // more wavefronts where there are many spans to join
+  const int jt = pl.splits > 16 && joins(p, 1024) <= most_groups(1024) ? 1024 : AT;
   if (work) {
     pl.o = work;
     pl.m = pl.o + rows * pl.splits * p.d;
@@ -749,7 +755,7 @@ hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
   const int32_t heads = pl.group < 16 * nt ? pl.group : 16 * nt;
   const size_t block = (size_t)pl.block * 8 + (pl.s ? (size_t)heads * pl.stage_ld * 4 : 0);
   const size_t part = (size_t)AW * meet * p.d * 4, bytes = block > part ? block : part;
-  const dim3 grid((uint32_t)wgs);
+  const dim3 grid((uint32_t)groups(p, pl));   // (unsplit no more than split)
   if (p.bf16)
     nt == 1 ? launch_dim<true, 1>(p, pl, grid, bytes, stream)
             : launch_dim<true, 2>(p, pl, grid, bytes, stream);
@@ -757,11 +763,11 @@ hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream) {
     nt == 1 ? launch_dim<false, 1>(p, pl, grid, bytes, stream)
             : launch_dim<false, 2>(p, pl, grid, bytes, stream);
   if (work) {
-    const dim3 jgrid((uint32_t)joins);
-    const int32_t keys = p.bf16 ? 32 : 16;
+    const dim3 jgrid((uint32_t)joins(p, jt));
+    const int32_t keys = p.bf16 ? 32 : 16, blocks = (int32_t)((p.max_len + jt - 1) / jt);
 #define TPP_JOIN_WAVES(NE, JW)                                                                    \
   hipLaunchKernelGGL((attn_join_kernel<NE, JW>), jgrid, dim3(JW * 64), 0, stream, p, pl, (int32_t)rows, \
-                     (int32_t)blocks, keys)
+                     blocks, keys)
 #define TPP_JOIN(NE)                          \
   if (jt == 1024) TPP_JOIN_WAVES(NE, 16);     \
   else TPP_JOIN_WAVES(NE, AW)

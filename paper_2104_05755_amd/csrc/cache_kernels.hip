@@ -478,11 +478,21 @@ bool one_launch(const EvictParams& p) {
   return move_cap(p) * p.kv_heads * copy_shape(p).units <= FUSED_CHUNKS && (in_place(p) || p.max_len <= 8 * ST);
 }
 
+// Workgroups of a sequence that hand on its totals, and with those that copy rows: two rows per set of lanes,
+// at most 8192 of the latter in all (2048: 66.6 us for 8 x 16384 cut to 4096, 64.1 so).
+int64_t hand_groups(const EvictParams& p) { return in_place(p) ? 0 : (p.max_len + 4 * CT - 1) / (4 * CT); }
+int64_t copy_groups(const EvictParams& p) {
+  const int64_t want = (move_cap(p) * p.kv_heads * copy_shape(p).lanes + 2 * CT - 1) / (2 * CT);
+  const int64_t most = 8192 / p.n_seqs > 0 ? 8192 / p.n_seqs : 1;
+  return hand_groups(p) + (want < most ? want : most);
+}
+
 }  // namespace
 
 int64_t evict_work_floats(const EvictParams& p) {
-  if (p.n_seqs > 0x7fffffff || move_cap(p) > (1 << 30) / p.kv_heads) return -1;
+  if (p.n_seqs > most_groups(ST) || move_cap(p) > (1 << 30) / p.kv_heads) return -1;
   if (one_launch(p)) return 0;
+  if (copy_groups(p) * p.n_seqs > most_groups(CT)) return -1;
   return p.n_seqs * (2 * move_cap(p) + 1 + gone_words(p) / 2);
 }
 
@@ -509,15 +519,10 @@ hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream) {
     if (p.max_len <= 4 * ST) TPP_SELECT(4, false);
     else if (p.max_len <= 16 * ST) TPP_SELECT(16, false);
     else TPP_SELECT(32, false);
-    // two rows per set of lanes, at most 8192 workgroups (2048: 66.6 us for 8 x 16384 cut to 4096, 64.1 so)
-    const int64_t want = (ml.cap * p.kv_heads * cs.lanes + 2 * CT - 1) / (2 * CT);
-    const int64_t most = 8192 / p.n_seqs > 0 ? 8192 / p.n_seqs : 1;
-    const int64_t hand = in_place(p) ? 0 : (p.max_len + 4 * CT - 1) / (4 * CT);
-    const int64_t per = hand + (want < most ? want : most);
-    if (per * p.n_seqs > 0x7fffffff) return hipErrorInvalidConfiguration;
+    const int64_t per = copy_groups(p);
     if (per > 0)
       hipLaunchKernelGGL(evict_copy_kernel, dim3((uint32_t)(per * p.n_seqs)), dim3(CT), 0, stream, p, ml,
-                         cs, (int32_t)per, FastDiv(per), (int32_t)hand);
+                         cs, (int32_t)per, FastDiv(per), (int32_t)hand_groups(p));
   }
 #undef TPP_SELECT
   return hipGetLastError();

@@ -320,7 +320,7 @@ struct AttnParams {
   int32_t page_size, q_heads, kv_heads, d, bf16, out_bf16;
   float scale;
 };
-// Floats of work space (-1: a launch would need more than 2^31 - 1 workgroups).  Without work space (null)
+// Floats of work space (-1: a launch would need 2^32 threads or more).  Without work space (null)
 // the launch is unsplit; one with totals has to have it.
 int64_t attn_work_floats(const AttnParams& p);
 hipError_t launch_attn(const AttnParams& p, float* work, hipStream_t stream);

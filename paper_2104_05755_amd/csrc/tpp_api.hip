@@ -1064,7 +1064,7 @@ tpp_status check_heads(const char* what, const tpp::QkParams& p, int side, const
 
 tpp_status launched(const char* what, hipError_t e) {
   if (e == hipErrorInvalidConfiguration)
-    return fail(TPP_ERR_UNSUPPORTED, "%s needs more than 2^31 - 1 workgroups", what);
+    return fail(TPP_ERR_UNSUPPORTED, "%s needs a launch of 2^32 threads or more", what);
   if (e != hipSuccess) return fail(TPP_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
   return ok();
 }
@@ -1206,7 +1206,7 @@ tpp_status tpp_paged_attention(const tpp_attn_desc* desc, const tpp_kv_cache* ca
   float* work = nullptr;
   std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
   const int64_t need = tpp::attn_work_floats(p);
-  if (need < 0) return fail(TPP_ERR_UNSUPPORTED, "attention needs more than 2^31 - 1 workgroups");
+  if (need < 0) return fail(TPP_ERR_UNSUPPORTED, "attention needs a launch of 2^32 threads or more");
   if (tpp_status s = call_work(WORK_ATTENTION, stream, need, &work, hold)) return s;
   if (need > 0 && !work && totals_out)
     return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
@@ -1257,7 +1257,7 @@ tpp_status tpp_cache_evict(const tpp_kv_cache* cache, int64_t n_seqs, int64_t ma
   float* work = nullptr;
   std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
   const int64_t need = tpp::evict_work_floats(p);
-  const char* too_many = "eviction needs more than 2^31 - 1 workgroups, or 2^30 rows for one sequence's moves";
+  const char* too_many = "eviction needs a launch of 2^32 threads or more, or 2^30 rows for one sequence's moves";
   if (need < 0) return fail(TPP_ERR_UNSUPPORTED, "%s", too_many);
   if (tpp_status s = call_work(WORK_EVICT, stream, need, &work, hold)) return s;
   if (need > 0 && !work)

@@ -150,3 +150,21 @@ def test_nothing_to_do(tpp):
     append(tpp, qk_desc(tpp), cache(tpp), 0, **none, q_out=None, v=None, slot=None)
     attend(tpp, cache(tpp), n=0, q=None, out=None, lens=None, pages=None)
     evict(tpp, cache(tpp), n=0, lens=None, pages=None, totals=None, totals_out=None, len_out=None)
+
+
+@pytest.mark.parametrize("kw,ckw", [
+    (dict(n=1 << 23), {}),                                            # 2^24 workgroups of one launch
+    (dict(n=1 << 18, max_len=1 << 15, ld_pages=1 << 11), {}),         # of its spans
+    (dict(n=1 << 19, q_heads=64, max_len=1 << 15, ld_pages=1 << 11), dict(kv_heads=1)),   # of the join's rows
+    (dict(n=1 << 19, max_len=1 << 13, ld_pages=1 << 9, totals_out=P, ldt=1 << 13), dict(kv_heads=1))],   # and positions
+    ids=str)
+def test_attention_refuses_a_grid_of_2_pow_32_threads(tpp, kw, ckw):
+    """Before it asks for work space or launches anything."""
+    refused(tpp, UNS, lambda: attend(tpp, cache(tpp, **ckw), **kw))
+
+
+@pytest.mark.parametrize("kw", [dict(n=1 << 22), dict(n=1 << 22, budget=39),
+                                dict(n=1 << 18, max_len=1 << 16, ldt=1 << 16, ld_pages=1 << 12)], ids=str)
+def test_evict_refuses_a_grid_of_2_pow_32_threads(tpp, kw):
+    a = dict(kw)
+    refused(tpp, UNS, lambda: evict(tpp, cache(tpp), **dict(a, totals_out=2 * P)))
