@@ -26,18 +26,6 @@ def gpu():
     assert torch.cuda.is_available(), "GPU tests need an MI355X"
 
 
-def captured(calls):
-    """calls(stream) captured into a graph, which is replayed twice."""
-    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
-    torch.cuda.synchronize()
-    with torch.cuda.graph(g, stream=s):
-        calls(s.cuda_stream)
-    for _ in range(2):
-        g.replay()
-        torch.cuda.synchronize()
-    return g
-
-
 @pytest.mark.parametrize("D,hq,hk,dtype,max_len", [(128, 64, 4, "bf16", 1 << 25), (77, 64, 4, "f32", 1 << 26),
                                                    (128, 64, 1, "bf16", 1 << 27)])
 def test_attention_captured_without_work_space(D, hq, hk, dtype, max_len):
