@@ -1002,3 +1002,32 @@ def test_norm_rope_more_rows_than_a_grid(tpp):
     torch.cuda.synchronize()
     off = (x.float() - ref).abs()
     assert bool((off <= ref.abs() * (2.0 ** -8 + 70 * U)).all()) and bool((ref[-1] != 0).any())
+
+
+def test_decode_step_totals(tpp):
+    """The totals of the chain, position by position: against the oracle's weights for the queries, keys and
+    values that the device itself has after its first two steps, with the bounds of check_attention.  Uniform
+    weights, weights one position on and totals that nothing was added to are past those bounds."""
+    from paper_2104_05755_amd import torch_io
+    wl = wk.decode_step()
+    dev = torch_io.upload(wl)
+    for s in wl.steps[:3]:
+        torch_io.launch_step(torch_io.prepare_step(s, dev), dev)
+    torch.cuda.synchronize()
+    at, a = wl.steps[2], {k: torch_io.to_host(dev[k], wl.arrays[k]) for k in ("q", "kc", "vc", "totals")}
+    d, hq, hk, lens, was = at.dim, at.q_heads, at.k_heads, wl.arrays["lens"], wl.arrays["totals"].astype(np.float64)
+    _, _, ref = oracle.paged_attention(a["kc"], a["vc"], "bf16", d, hk, at.page, len(a["kc"]),
+                                       (at.page * hk * d, hk * d, d), wl.arrays["pages"], a["q"], hq * d, hq, lens,
+                                       at.scale, 0, was)
+    qn = np.abs(values(a["q"], "bf16")).reshape(len(lens), hq, d).sum(-1)
+    rel = 2 * (d + 4) * U * at.scale * qn.max(-1) * np.abs(values(a["kc"], "bf16")).max() + \
+        (64 + lens.max()) * U + 2.0 ** -20
+    for b, n in enumerate(lens):
+        more = ref[b, :n] - was[b, :n]
+        bound = rel[b] * more + 1e-30
+        close(a["totals"][b, :n].astype(np.float64), ref[b, :n], bound, "f32", f"totals of sequence {b}")
+        limit = bound + U * np.abs(ref[b, :n])
+        assert (more > limit).any()
+        if n >= 8:
+            assert (np.abs(hq / n - more) > limit).any() and (np.abs(np.roll(more, 1) - more) > limit).any()
+        assert np.array_equal(a["totals"][b, n:], wl.arrays["totals"][b, n:])
