@@ -19,6 +19,8 @@
 // TB/s: 20 chunks a row leave 12 of the 32 places of its lanes empty, and the fold is 4 us.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "brgemm_device.h"
 #include "internal.h"
 
@@ -675,6 +677,35 @@ int cache_use(const QkParams& p, bool backward) {
   return lines && out * (backward ? 3 : 2) > int64_t(128) << 20 ? STREAM : STREAM_OUT;
 }
 
+// f(type, whole chunks, lanes of a row, cache use) for the instance that rows of chunks take.
+template <bool BF16, bool WHOLE, int HOW, typename F>
+void by_lanes(const QkParams& p, const F& f) {
+  const std::integral_constant<bool, BF16> t;
+  const std::integral_constant<bool, WHOLE> w;
+  const IntC<HOW> how;
+  switch (lanes_of(p)) {
+    case 4: return f(t, w, IntC<4>(), how);
+    case 8: return f(t, w, IntC<8>(), how);
+    case 16: return f(t, w, IntC<16>(), how);
+    case 32: return f(t, w, IntC<32>(), how);
+  }
+  // (512 entries of bf16 in whole chunks are 32 lanes)
+  if constexpr (!BF16 || !WHOLE) f(t, w, IntC<64>(), how);
+}
+template <typename F>
+void by_chunks(const QkParams& p, bool backward, const F& f) {
+  const int how = cache_use(p, backward);
+  const auto type = [&](auto t) {
+    constexpr bool BF16 = decltype(t)::value;
+    if (!whole_chunks(p)) by_lanes<BF16, false, CACHED>(p, f);
+    else if (how == STREAM) by_lanes<BF16, true, STREAM>(p, f);
+    else if (how == STREAM_OUT) by_lanes<BF16, true, STREAM_OUT>(p, f);
+    else by_lanes<BF16, true, CACHED>(p, f);
+  };
+  if (p.bf16) type(std::true_type());
+  else type(std::false_type());
+}
+
 // Workgroups of the two sides in the backward pass: 1024 in all where there are rows for them.
 void backward_groups(const QkParams& p, int32_t& nq, int32_t& nk) {
   const int32_t heads = p.side[0].heads + p.side[1].heads, rows = QW * rows_at_once(p);
@@ -714,30 +745,14 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
     q.pos += t0;
     const int32_t rows = (int32_t)(q.tokens * per);
     const dim3 grid((uint32_t)(((int64_t)rows + wg - 1) / wg));
-#define TPP_QK(LANES, BF16, WHOLE, HOW)                                                             \
-  case LANES:                                                                                       \
-    hipLaunchKernelGGL((qk_chunk_kernel<BF16, WHOLE, LANES, HOW>), grid, dim3(QT), 0, stream, q,    \
-                       rows, per, div, chunk_lanes(p));                                             \
-    break
-#define TPP_QK_LANES(BF16, WHOLE, HOW)                                                              \
-  switch (lanes_of(p)) {                                                                            \
-    TPP_QK(4, BF16, WHOLE, HOW);                                                                    \
-    TPP_QK(8, BF16, WHOLE, HOW);                                                                    \
-    TPP_QK(16, BF16, WHOLE, HOW);                                                                   \
-    TPP_QK(32, BF16, WHOLE, HOW);                                                                   \
-    TPP_QK(64, BF16, WHOLE, HOW);                                                                   \
-  }
-#define TPP_QK_TYPE(WHOLE, HOW) \
-  if (p.bf16) { TPP_QK_LANES(true, WHOLE, HOW) } else { TPP_QK_LANES(false, WHOLE, HOW) }
 #define TPP_QK_UNITS(NU) \
   hipLaunchKernelGGL((qk_unit_kernel<NU>), grid, dim3(QT), 0, stream, q, rows, per, div)
-    if (whole_chunks(p)) {
-      const int how = cache_use(p, false);
-      if (how == STREAM) { TPP_QK_TYPE(true, STREAM) }
-      else if (how == STREAM_OUT) { TPP_QK_TYPE(true, STREAM_OUT) }
-      else { TPP_QK_TYPE(true, CACHED) }
-    } else if (chunked(p)) {
-      TPP_QK_TYPE(false, CACHED)
+    if (chunked(p)) {
+      by_chunks(p, false, [&](auto bf16, auto whole, auto lanes, auto how) {
+        hipLaunchKernelGGL((qk_chunk_kernel<decltype(bf16)::value, decltype(whole)::value, decltype(lanes)::value,
+                                            decltype(how)::value>),
+                           grid, dim3(QT), 0, stream, q, rows, per, div, chunk_lanes(p));
+      });
     } else if (units <= 64) {
       TPP_QK_UNITS(1);
     } else if (units <= 128) {
@@ -748,9 +763,6 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
       TPP_QK_UNITS(8);
     }
 #undef TPP_QK_UNITS
-#undef TPP_QK_TYPE
-#undef TPP_QK_LANES
-#undef TPP_QK
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -773,30 +785,14 @@ hipError_t launch_qk_backward(const QkParams& p, float* work, hipStream_t stream
     nk = nk < 1 ? nk : 1;
   }
   const int32_t units = p.d - p.rot_dim / 2;
-#define TPP_QKB(LANES, BF16, WHOLE, HOW)                                                            \
-  case LANES:                                                                                       \
-    hipLaunchKernelGGL((qk_backward_chunk_kernel<BF16, WHOLE, LANES, HOW>), dim3(nq + nk), dim3(QT), 0, \
-                       stream, p, nq, work, chunk_lanes(p));                                        \
-    break
-#define TPP_QKB_LANES(BF16, WHOLE, HOW)                                                             \
-  switch (lanes_of(p)) {                                                                            \
-    TPP_QKB(4, BF16, WHOLE, HOW);                                                                   \
-    TPP_QKB(8, BF16, WHOLE, HOW);                                                                   \
-    TPP_QKB(16, BF16, WHOLE, HOW);                                                                  \
-    TPP_QKB(32, BF16, WHOLE, HOW);                                                                  \
-    TPP_QKB(64, BF16, WHOLE, HOW);                                                                  \
-  }
-#define TPP_QKB_TYPE(WHOLE, HOW) \
-  if (p.bf16) { TPP_QKB_LANES(true, WHOLE, HOW) } else { TPP_QKB_LANES(false, WHOLE, HOW) }
 #define TPP_QKB_UNITS(NU) \
   hipLaunchKernelGGL((qk_backward_unit_kernel<NU>), dim3(nq + nk), dim3(QT), 0, stream, p, nq, work)
-  if (whole_chunks(p)) {
-    const int how = cache_use(p, true);
-    if (how == STREAM) { TPP_QKB_TYPE(true, STREAM) }
-    else if (how == STREAM_OUT) { TPP_QKB_TYPE(true, STREAM_OUT) }
-    else { TPP_QKB_TYPE(true, CACHED) }
-  } else if (chunked(p)) {
-    TPP_QKB_TYPE(false, CACHED)
+  if (chunked(p)) {
+    by_chunks(p, true, [&](auto bf16, auto whole, auto lanes, auto how) {
+      hipLaunchKernelGGL((qk_backward_chunk_kernel<decltype(bf16)::value, decltype(whole)::value,
+                                                   decltype(lanes)::value, decltype(how)::value>),
+                         dim3(nq + nk), dim3(QT), 0, stream, p, nq, work, chunk_lanes(p));
+    });
   } else if (units <= 64) {
     TPP_QKB_UNITS(1);
   } else if (units <= 128) {
@@ -807,9 +803,6 @@ hipError_t launch_qk_backward(const QkParams& p, float* work, hipStream_t stream
     TPP_QKB_UNITS(8);
   }
 #undef TPP_QKB_UNITS
-#undef TPP_QKB_TYPE
-#undef TPP_QKB_LANES
-#undef TPP_QKB
   if (work)
     hipLaunchKernelGGL(qk_fold_kernel, dim3((p.d + FE - 1) / FE, 2), dim3(FT), 0, stream, p, nq, nk, work);
   return hipGetLastError();
