@@ -171,6 +171,10 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   // only the work of long sequences (64 of 1 to 8192: 244 us so, 215 turned by the sequence, which is as
   // uneven for each head, 192 by both).  With the heads first the interleaved rows of the heads are read at
   // once, at a lower rate (223 us; 64 of 4096 189, 180 so; 32 of 2049 to 4096 with totals 107 and 103).
+  // Workgroups of two head tiles, one to a compute unit, often run all at once: those of a key head are turned
+  // alike, so that a span is read by one XCD (64 heads to one: 64 sequences of 8192 102 us turned by the tile,
+  // 87 so, one of 131072 37.3 and 31.4; of one tile each, 24 heads of 192 to one, 64 sequences of 1 to 4096
+  // 65.2 by the tile, 68.9 alike).
   // Where rows share lines with other heads' (plan()), all heads of a span follow each other on one XCD,
   // whose L2 has what they share.
   int32_t seq, sp, y, turn;
@@ -187,7 +191,7 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
     sp = (int32_t)blockIdx.x - ys * pl.splits;
     y = fdiv(ys, pl.div_seqs);
     seq = ys - y * (int32_t)p.n_seqs;
-    turn = seq + y;
+    turn = seq + (NT == 2 ? fdiv(y, pl.div_tiles) : y);
   }
   const int32_t from = turn - fdiv(turn, pl.div_splits) * pl.splits;
   const int32_t split = sp + from >= pl.splits ? sp + from - pl.splits : sp + from;
