@@ -29,7 +29,7 @@
 // An infinite value has no place in the products: a weight of 0, one of a weight's parts, or a masked place
 // that stands on its row would make it NaN.  Its entry's sum is known without them -- the weights are
 // positive, so it is that infinity, or NaN where both signs or a NaN are held -- and comes out of the products
-// as infinite or NaN in any case.  A wavefront that finds such a sum after a block looks its values up again.
+// as infinite or NaN in any case, so that only then the span's values of the entry are looked up again.
 //
 // Bound by HBM where the cache is large.  32 heads to 8 of 128 bf16: 64 sequences of 4096 180 us, 6.0 TB/s;
 // 64 of 1 to 8192 192 us, 5.6 TB/s, 7 of them the join; one of 131072 97 us, 5.5 TB/s; 32 of 2049 to 4096
@@ -109,6 +109,7 @@ __device__ __forceinline__ float share(float m, float top) {
 constexpr int32_t BLOCK = 1024;   // most positions whose addresses are in LDS at a time
 constexpr int JOINED = 4;         // partial results that a lane of the joining kernel has in flight
 constexpr int SCORES = 16;        // heads whose scores of a position a lane has in flight
+constexpr int LOOK = 8;           // values in flight of an entry whose sum is not finite
 constexpr int32_t MEET = 8;       // query heads whose sums are in LDS at a time
 
 // What one launch needs beside AttnParams.
@@ -162,7 +163,6 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   __shared__ int32_t missing;   // 1 + the first position of the last block that lacks a page
   __shared__ int32_t first_held;
   __shared__ float wave_m[AW][NT * 16], wave_l[AW][NT * 16];
-  __shared__ uint32_t odd[DP / 16];   // 2 bits an entry: held values of +inf (1), of -inf (2), NaN (both)
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, grp = lane >> 4;
@@ -199,7 +199,6 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   const int64_t b = seq;
   const int32_t D = TAIL ? p.d : DP;
   if (tid == 0) missing = 0;
-  if (tid < DP / 16) odd[tid] = 0;
   const int32_t n = length_of(p, b);
   const int32_t lo = window_start(p, n);
   const int32_t c0 = lo / KEYS * KEYS + split * pl.span;   // this span: [c0, c1)
@@ -389,24 +388,6 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   };
 
   constexpr int32_t step = AW * KEYS, NONE = 0x7fffffff;
-  // Marks the entries of this wavefront's held values of a block that are not finite.
-  const auto find_odd = [&](int32_t cnt) {
-    for (int32_t i0 = wave * KEYS; i0 < cnt; i0 += step) {
-      load_v(i0);
-#pragma unroll
-      for (int k = 0; k < VKEYS; ++k)
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-          for (int j = 0; j < VC; ++j) {
-            const uint32_t w = BF16 ? vf[k][c][j / 2] : vf[k][c][j];
-            const float v = __uint_as_float(!BF16 ? w : j & 1 ? w & 0xffff0000u : w << 16);
-            if (v - v == 0.0f || (masks >> k & 1)) continue;
-            const int32_t e0 = (c * 16 + col) * VC, e = (OVER && e0 > D - VC ? D - VC : e0) + j;
-            atomicOr(&odd[e >> 4], (v > 0.0f ? 1u : v < 0.0f ? 2u : 3u) << 2 * (e & 15));
-          }
-    }
-  };
   for (int32_t t0 = c0; t0 < c1; t0 += pl.block) {
     // ---- addresses of the block's rows --------------------------------------------------------------
     // A position outside the span's or the window's gets the row of the nearest one inside, masked.  Where
@@ -443,12 +424,6 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
       load_v(i0);
       for (; i0 + step < cnt; i0 += step) tile(std::true_type(), i0, i0 + step);
       tile(std::false_type(), i0, 0);
-      f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};   // NaN where a sum is not finite
-#pragma unroll
-      for (int q = 0; q < NT; ++q)
-#pragma unroll
-        for (int j = 0; j < NV * VC; ++j) zero += acc[q][j] * 0.0f;
-      if (__ballot((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.0f) != 0) find_odd(cnt);
     }
     // ---- its scores: a query head's row to a wavefront ------------------------------------------------
     // (Stored by each tile, 64 bytes of a head at a time: 32 sequences of 2049 to 4096 103 us, 95 so.)
@@ -461,6 +436,23 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
       }
     }
   }
+
+  // The sum of entry e, o by the products, where values held in the span are not finite: LOOK of them at a time.
+  const auto without_products = [&](float o, int32_t e) {
+    uint32_t found = 0;   // 1: +inf, 2: -inf, 3: both, or NaN
+    for (int32_t t = c0 < lo ? lo : c0; t < c1 && found != 3; t += LOOK) {
+      float v[LOOK];
+#pragma unroll
+      for (int u = 0; u < LOOK; ++u) {
+        const int64_t row = row_of(p, b, t + u < c1 ? t + u : c1 - 1);
+        v[u] = row < 0 ? 0.0f : load_elem(vb, row + e, BF16);
+      }
+#pragma unroll
+      for (int u = 0; u < LOOK; ++u)
+        if (v[u] - v[u] != 0.0f) found |= v[u] > 0.0f ? 1u : v[u] < 0.0f ? 2u : 3u;
+    }
+    return found == 0 ? o : found == 1 ? INFINITY : found == 2 ? -INFINITY : NAN;
+  };
 
   // ---- the wavefronts meet ------------------------------------------------------------------------
 #pragma unroll
@@ -505,8 +497,7 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
         sum += wave_l[w][h] * share(wave_m[w][h], top);
         o += part[w * ng * D + i];
       }
-      if (const uint32_t bits = odd[e >> 4] >> 2 * (e & 15) & 3u)
-        o = bits == 1 ? INFINITY : bits == 2 ? -INFINITY : NAN;
+      if (__builtin_expect(o - o != 0.0f && sum == sum, 0)) o = without_products(o, e);
       const int64_t row = b * p.q_heads + h0 + h;
       if (pl.o) {
         const int64_t at = row * pl.splits + split;
