@@ -132,7 +132,9 @@ typedef struct {
  * entries.
  * Long caches are split over workgroups whose partial results (and, for totals, the scores) go to a
  * work buffer as tpp_reduce's do, under stream capture to one of the capture's own; where a capture
- * can have none, the launch is unsplit, and one with totals fails with NO_MEMORY.
+ * can have none, the launch is unsplit, and one with totals fails with NO_MEMORY.  Its size goes by
+ * max_len, whatever the lengths are: 4 (D + 2) bytes for each of the n_seqs * q_heads rows and spans of
+ * max_len (or window) positions, and with totals 4 bytes for each row and position of max_len.
  * Errors: INVALID_ARG as above and for a malformed desc or cache; UNSUPPORTED for other D, max_len above
  * 2^30 or a launch of 2^32 threads or more, before anything is done (256 for each span of 64 to 4096
  * positions of each key head of each sequence, and, where those are joined, for each of the q_heads *

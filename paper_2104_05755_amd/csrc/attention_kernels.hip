@@ -32,9 +32,10 @@
 // as infinite or NaN in any case, so that only then the span's values of the entry are looked up again.
 //
 // Bound by HBM where the cache is large.  32 heads to 8 of 128 bf16: 64 sequences of 4096 180 us, 6.0 TB/s;
-// 64 of 1 to 8192 192 us, 5.6 TB/s, 7 of them the join; one of 131072 97 us, 5.5 TB/s; 32 of 2049 to 4096
-// with totals 92 us, 4.4 TB/s.  One of 100 positions 5.4 us from call to call, 4.4 of them the kernel: the
-// loads of length, page, keys and values wait for each other.
+// 64 of 1 to 8192 191 us, 5.6 TB/s, 7 of them the join; one of 131072 96 us, 5.6 TB/s; 32 of 2049 to 4096
+// with totals 92 us, 4.4 TB/s (a kernel that only reads as many bytes: 7.1 to 7.2 TB/s).  One of 100 positions
+// 5.5 us from call to call, 4.6 of them the GPU's: the loads of length, page, keys and values wait for each
+// other.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -149,9 +150,9 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   constexpr int NK = DP / S::STEP;                   // steps of the first product
   constexpr int VC = BF16 && DP > 64 ? 8 : 4;        // entries of a lane's chunk of a value
   constexpr int NV = (DP + 16 * VC - 1) / (16 * VC); // chunks
-  // Values are read once, whole lines by one load: past the caches' replacement (64 sequences of 4096: 199 us
-  // without, 181 so; a sequence of 131072 107 and 97).  The keys' lines take two loads, which would then both
-  // go to memory (64 of 1 to 8192 215 us, 234 so), and rows that are no whole lines share some with the next.
+  // Values are read once, whole lines by one load: past the caches' replacement (64 sequences of 4096: 198 us
+  // without, 180 so; a sequence of 131072 108 and 99).  The keys' lines take two loads, which would then both
+  // go to memory (64 of 1 to 8192 196 us, 205 so), and rows that are no whole lines share some with the next.
   constexpr bool STREAM = !TAIL && DP * ES % 128 == 0;
   constexpr bool OVER = TAIL || DP % (16 * VC) != 0; // lanes past the last entry take the last chunk
   typedef typename std::conditional<VC * ES == 16, u32x4, u32x2>::type vchunk;
@@ -168,9 +169,9 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
   const int col = lane & 15, grp = lane >> 4;
   // Spans first, those of each sequence and head from another one on, then sequences, heads last.
   // Workgroups go to the 8 XCDs in turn: with every sequence's first span on the same XCD, the others had
-  // only the work of long sequences (64 of 1 to 8192: 244 us so, 215 turned by the sequence, which is as
-  // uneven for each head, 192 by both).  With the heads first the interleaved rows of the heads are read at
-  // once, at a lower rate (223 us; 64 of 4096 189, 180 so; 32 of 2049 to 4096 with totals 107 and 103).
+  // only the work of long sequences (64 of 1 to 8192: 253 us so, 213 turned by the sequence, which is as
+  // uneven for each head, 196 by both).  With the heads first the interleaved rows of the heads are read at
+  // once, at a lower rate (206 us; 64 of 4096 191, 180 so; 32 of 2049 to 4096 with totals 99 and 93).
   // Workgroups of two head tiles, one to a compute unit, often run all at once: those of a key head are turned
   // alike, so that a span is read by one XCD (64 heads to one: 64 sequences of 8192 102 us turned by the tile,
   // 87 so, one of 131072 37.3 and 31.4; of one tile each, 24 heads of 192 to one, 64 sequences of 1 to 4096
@@ -437,7 +438,8 @@ __global__ __launch_bounds__(AT) void attn_kernel(AttnParams p, AttnPlan pl) {
     }
   }
 
-  // The sum of entry e, o by the products, where values held in the span are not finite: LOOK of them at a time.
+  // The sum of entry e, o by the products, where it is not finite: by the values held in the span, LOOK of them
+  // at a time.
   const auto without_products = [&](float o, int32_t e) {
     uint32_t found = 0;   // 1: +inf, 2: -inf, 3: both, or NaN
     for (int32_t t = c0 < lo ? lo : c0; t < c1 && found != 3; t += LOOK) {
@@ -606,7 +608,7 @@ __global__ __launch_bounds__(JW * 64) void attn_join_kernel(AttnParams p, AttnPl
     __syncthreads();
     const int32_t heads = p.q_heads - hb < JW * 64 ? p.q_heads - hb : JW * 64;
     if (held)
-      // (one by one: 64 heads, 22 sequences of 0 to 54 15.1 us, 13.6 so)
+      // (one by one: 64 heads, 22 sequences of 0 to 54 14.3 us, 13.4 so)
       for (int32_t h = 0; h < heads; h += SCORES) {
         float s[SCORES];
 #pragma unroll
@@ -629,8 +631,8 @@ int64_t range_of(const AttnParams& p) {
 
 // Tiles of 16 query heads per workgroup.  Two read the keys and values once for twice the heads, and have
 // the registers for it up to 128 entries a head, but one wavefront per SIMD: for more than 16 heads to a
-// key head and 32 MB of cache on (64 heads to one, 64 sequences of 8192: 81 us, 173 with one tile; 16 of
-// 4096 23.4 and 24.9; one sequence of 300, 24 heads to one 12.7 and 9.5).
+// key head and 32 MB of cache on (64 heads to one, 64 sequences of 8192: 91 us, 176 with one tile; 16 of
+// 4096 24.7 and 31.8; one sequence of 300, 24 heads to one 14.1 and 10.1).
 int32_t head_tiles(const AttnParams& p) {
   const int64_t bytes = range_of(p) * p.n_seqs * p.kv_heads * p.d * (p.bf16 ? 4 : 8);
   return p.q_heads / p.kv_heads > 16 && p.d <= 128 && bytes >= int64_t(32) << 20 ? 2 : 1;
@@ -638,13 +640,14 @@ int32_t head_tiles(const AttnParams& p) {
 
 // Spans that give the 256 compute units two workgroups each, as many as have the registers at once (one
 // of two head tiles), between a tile per wavefront and a block; `split` false: the whole sequence.  (Four
-// each: the odd fp32 case 26.4 us, 21.7 so; spans of two blocks: 64 sequences of 1 to 8192 235 us, 215 with one.)
+// each: 13 sequences of 0 to 1533, window 1000, 21 fp32 heads to 7 of 77 26.9 us, 21.3 so; spans of two
+// blocks: 64 sequences of 1 to 8192 209 us, 196 with one, one of 131072 105 and 99.)
 // Two head tiles leave twice the partial results a span, and the start of a workgroup alone on its compute
-// unit is covered by nothing: up to four blocks (64 heads to one, 64 sequences of 8192 128 us with one, 81
-// so; 24 to one, 256 of 2000 to 4096 118 and 82; 32 heads of 64 to one, 64 of 1 to 8192 29 and 31).
+// unit is covered by nothing: up to four blocks (64 heads to one, 64 sequences of 8192 135 us with one, 91
+// so; 24 to one, 256 of 2000 to 4096 126 and 88; 32 heads of 64 to one, 64 of 1 to 8192 31 and 34).
 // Where blocks would make less than two rounds of workgroups, sequences of several lengths leave compute
-// units idle: half a block (22 of 0 to 1760, 16 heads to 16 of 64 30.0 us with a block, 25.6 so; 52 of 0 to
-// 8745, 8 heads to 2 of 32 34.2 and 29.3; of 96 39.3 and 40.0).
+// units idle: half a block (22 of 0 to 1760, 16 heads to 16 of 64 30.5 us with a block, 26.2 so; 52 of 0 to
+// 8745, 8 heads to 2 of 32 27.3 and 27.3; of 96 54.1 and 49.3; but one of 131072 99 and 102).
 AttnPlan plan(const AttnParams& p, bool split) {
   AttnPlan pl = {};
   pl.group = p.q_heads / p.kv_heads;
@@ -658,15 +661,15 @@ AttnPlan plan(const AttnParams& p, bool split) {
   const int64_t most = nt == 2 ? 4 * BLOCK : p.n_seqs > 1 && range * units < 1024 * BLOCK ? BLOCK / 2 : BLOCK;
   if (span > most) span = most;
   // Few tiles to a sequence: their workgroup is done sooner than a second kernel has joined parts (one
-  // sequence of 512, 8 key heads of 128 bf16: 9.3 us whole and 9.1, of 256 6.4 and 8.9; fp32 256 10.0 whole and
-  // 9.6; 16 sequences of 1024 bf16 18.3 and 18.9, of 512 fp32 17.2 and 20.0).
+  // sequence of 512, 8 key heads of 128 bf16: 9.8 us whole and 9.4, of 256 6.9 and 9.4; fp32 256 10.4 whole and
+  // 10.2; 16 sequences of 1024 bf16 19.0 and 19.5, of 512 fp32 17.6 and 20.3).
   const bool few = range <= keys * (units >= 128 ? 32 : p.bf16 ? 16 : 8);
   if (!split || few) span = range < step ? step : (range + step - 1) / step * step;
   pl.span = (int32_t)span;
   pl.splits = range > span ? (int32_t)((range + span - 1) / span) : 1;
   pl.score_ld = ((p.max_len + 63) / 64 | 1) * 64;
   const int32_t heads = pl.group < 16 * nt ? pl.group : 16 * nt;
-  // at most 33 KB of scores, so that as many workgroups have room as have registers
+  // at most 34 KB of scores, so that as many workgroups have room as have registers
   pl.block = !p.totals_out || heads <= 8 ? BLOCK : heads <= 16 ? BLOCK / 2 : BLOCK / 4;
   if (pl.block > span) pl.block = (int32_t)span;
   pl.stage_ld = pl.block + 16;   // four heads' chunks at once to different banks
@@ -676,8 +679,8 @@ AttnPlan plan(const AttnParams& p, bool split) {
   // Heads side by side in the cache whose rows are no whole lines: two workgroups read a line, and the bytes
   // past L2 are those of whole lines unless they do so on one XCD.  With fewer workgroups than run at once
   // all of a sequence's on one XCD would leave others idle.  (32 heads to 8, 64 sequences: of 96 bf16, 4096
-  // 171 us apart, 151 together; of 77, 1 to 8192 211 and 185; 16 of 3000, of 80, 38.5 and 34.6; the odd
-  // fp32 case 21.8 and 21.1; but 16 heads to 16 of 77, 22 of 0 to 1760, 50.5 and 54.5.)
+  // 169 us apart, 150 together; of 77, 1 to 8192 213 and 185; 16 of 3000, of 80, 40.3 and 36.6; 13 of 0 to
+  // 1533, fp32 heads of 77 as above, 22.2 and 21.3; but 16 heads to 16 of 77, 22 of 0 to 1760, 51.1 and 51.4.)
   const int64_t lines = p.head_stride % 128 * (p.bf16 ? 2 : 4) % 128, spans = p.n_seqs * pl.splits;
   const int64_t round = 8 * (int64_t)p.kv_heads * pl.tiles;
   if (lines != 0 && p.kv_heads > 1 && p.head_stride < p.pos_stride && units * pl.splits >= 512 &&

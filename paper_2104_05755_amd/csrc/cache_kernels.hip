@@ -14,8 +14,9 @@
 // chunk per lane -- or, where a sequence can lose only a few, by the selecting workgroup itself, since a
 // second launch would cost more than the copy.
 //
-// 8 key heads of 128 bf16: 8 sequences of 9001 to 16384 cut to 4096 54 us, of them 19 the selection, whose
-// passes wait for each other, and 35 the copy, 5.3 TB/s; 32 of 2049 that lose one 7.5 us.
+// 8 key heads of 128 bf16: 8 sequences of 9001 to 16384 cut to 4096 55 us, of them 19 the selection, whose
+// passes wait for each other on 8 of 256 compute units, and 36 the copy, 5.2 TB/s; 32 of 2049 that lose one
+// 7.5 us.
 #include <hip/hip_runtime.h>
 
 #include "brgemm_device.h"

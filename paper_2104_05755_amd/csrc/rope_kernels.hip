@@ -13,10 +13,11 @@
 // entries another lane counts and stores.  Rows that are too short for that: one per wavefront, a rotated
 // pair or an entry behind the rotated part to a lane, four rows in flight.
 //
-// 32 + 8 heads of 128 bf16, 8192 tokens: forward 33.0 us, 5.2 TB/s; backward 51.1 us with the fold of the
-// norm weights' gradients, 5.0 TB/s.  2048 tokens into a cache 10.8 us, 4.7 TB/s; one token 5.8 us from
+// 32 + 8 heads of 128 bf16, 8192 tokens: forward 33.2 us, 5.2 TB/s; backward 50.8 us, 5.0 TB/s, 4 of them the
+// fold of the norm weights' gradients.  2048 tokens into a cache 10.8 us, 4.8 TB/s; one token 5.8 us from
 // call to call, 3.0 of them the kernel.  1533 tokens of 21 + 7 fp32 heads of 77, backward: 15.5 us, 2.6
-// TB/s: 20 chunks a row leave 12 of the 32 places of its lanes empty, and the fold is 4 us.
+// TB/s, where a copy of as many bytes takes 7.0: a workgroup goes two or three times through a loop whose
+// position, angles (4 bytes a load in the pairs form) and rows wait for each other, and the fold is 4 us.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -749,8 +750,8 @@ hipError_t launch_qk(const QkParams& p, hipStream_t stream) {
   hipLaunchKernelGGL((qk_unit_kernel<NU>), grid, dim3(QT), 0, stream, q, rows, per, div)
     if (chunked(p)) {
       by_chunks(p, false, [&](auto bf16, auto whole, auto lanes, auto how) {
-        hipLaunchKernelGGL((qk_chunk_kernel<decltype(bf16)::value, decltype(whole)::value, decltype(lanes)::value,
-                                            decltype(how)::value>),
+        hipLaunchKernelGGL((qk_chunk_kernel<decltype(bf16)::value, decltype(whole)::value,
+                                            decltype(lanes)::value, decltype(how)::value>),
                            grid, dim3(QT), 0, stream, q, rows, per, div, chunk_lanes(p));
       });
     } else if (units <= 64) {
