@@ -634,8 +634,8 @@ int64_t range_of(const AttnParams& p) {
 // key head and 32 MB of cache on (64 heads to one, 64 sequences of 8192: 91 us, 176 with one tile; 16 of
 // 4096 24.7 and 31.8; one sequence of 300, 24 heads to one 14.1 and 10.1).
 int32_t head_tiles(const AttnParams& p) {
-  const int64_t bytes = range_of(p) * p.n_seqs * p.kv_heads * p.d * (p.bf16 ? 4 : 8);
-  return p.q_heads / p.kv_heads > 16 && p.d <= 128 && bytes >= int64_t(32) << 20 ? 2 : 1;
+  const double bytes = (double)range_of(p) * (double)(p.n_seqs * p.kv_heads) * (p.d * (p.bf16 ? 4 : 8));
+  return p.q_heads / p.kv_heads > 16 && p.d <= 128 && bytes >= 32 << 20 ? 2 : 1;
 }
 
 // Spans that give the 256 compute units two workgroups each, as many as have the registers at once (one
