@@ -124,6 +124,13 @@ def lib():
                                                 vp, i64]
         _lib.oracle_cache_evict.restype = ctypes.c_int
         _lib.oracle_cache_evict.argtypes = [i64, i64, vp, vp, vp, vp, i64, vp, vp]
+        for name, args in (("norm", [i64, i32, i32, i32, dbl, vp, i64, vp, vp, vp]),
+                           ("norm_backward", [i64, i32, i32, i32, dbl, vp, i64] + [vp] * 5),
+                           ("act", [i32, i64, vp, vp, vp]),
+                           ("q8_rows", [i64, i32, i32, vp, vp, vp]),
+                           ("q8_product", [i32, i32, i32, vp, i64, vp, i64, vp])):
+            f = getattr(_lib, "oracle_" + name)
+            f.restype, f.argtypes = ctypes.c_int, args
     return _lib
 
 
@@ -508,3 +515,67 @@ def cache_evict(lens, budget, totals, pos=None, horizon=None):
     if rc != 0:
         raise ValueError("oracle_cache_evict rejected its arguments")
     return new, keep
+
+
+# ---- the residual stream's norms and 8-bit rows ---------------------------------------------------
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+ACTS = {"none": 0, "relu": 1, "gelu_tanh": 2, "silu": 3}
+
+
+def _rows(x, dtype, f):
+    """x as [tokens][ld] with at least f entries a row, and ld."""
+    _check_dtype(x, dtype, "x")
+    assert x.ndim == 2 and x.shape[1] >= f and x.flags.c_contiguous
+    return x, x.shape[1]
+
+
+def norm(v, f, dtype, form, eps, w=None, c=None):
+    """Unrounded norms [tokens][f] of the rows of v ([tokens][ld])."""
+    v, ld = _rows(v, dtype, f)
+    w, c = (None if a is None else _f32(a) for a in (w, c))
+    out = np.zeros((len(v), f))
+    if lib().oracle_norm(len(v), f, _DTYPES[dtype], NORMS[form], eps, _ptr(v), ld, _ptr(w), _ptr(c),
+                         _ptr(out)) != 0:
+        raise ValueError("oracle_norm rejected its arguments")
+    return out
+
+
+def norm_backward(v, f, dtype, form, eps, w, g):
+    """Unrounded (dv [tokens][f], dw [f], dc [f]) for gradients g ([tokens][f], float64)."""
+    v, ld = _rows(v, dtype, f)
+    w, g = None if w is None else _f32(w), np.ascontiguousarray(g, dtype=np.float64)
+    dv, dw, dc = np.zeros((len(v), f)), np.zeros(f), np.zeros(f)
+    if lib().oracle_norm_backward(len(v), f, _DTYPES[dtype], NORMS[form], eps, _ptr(v), ld, _ptr(w),
+                                  _ptr(g), _ptr(dv), _ptr(dw), _ptr(dc)) != 0:
+        raise ValueError("oracle_norm_backward rejected its arguments")
+    return dv, dw, dc
+
+
+def act(z, form):
+    """(act(z), act'(z)) in float64."""
+    z = np.ascontiguousarray(z, dtype=np.float64)
+    value, slope = np.zeros_like(z), np.zeros_like(z)
+    if lib().oracle_act(ACTS[form], z.size, _ptr(z), _ptr(value), _ptr(slope)) != 0:
+        raise ValueError("oracle_act rejected its arguments")
+    return value, slope
+
+
+def q8_rows(v, group=0):
+    """(q int8 [tokens][f], scale fp32 [tokens][groups]) of values v ([tokens][f], float64)."""
+    v = np.ascontiguousarray(v, dtype=np.float64)
+    n, f = v.shape
+    g = group or f
+    q, scale = np.zeros((n, f), np.int8), np.zeros((n, -(-f // g)), np.float32)
+    if lib().oracle_q8_rows(n, f, g, _ptr(v), _ptr(q), _ptr(scale)) != 0:
+        raise ValueError("oracle_q8_rows rejected its arguments")
+    return q, scale
+
+
+def q8_product(a, b, k):
+    """int64 [n][m] of the first k entries of the rows of a ([m][lda]) and b ([n][ldb])."""
+    assert a.dtype == b.dtype == np.int8 and a.flags.c_contiguous and b.flags.c_contiguous
+    out = np.zeros((len(b), len(a)), np.int64)
+    if lib().oracle_q8_product(len(a), len(b), k, _ptr(a), a.shape[1], _ptr(b), b.shape[1],
+                               _ptr(out)) != 0:
+        raise ValueError("oracle_q8_product rejected its arguments")
+    return out

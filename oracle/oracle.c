@@ -832,3 +832,113 @@ int oracle_cache_evict(int64_t n_seqs, int64_t budget, const int64_t* len, const
   }
   return 0;
 }
+
+/* ---- the residual stream's norms and 8-bit rows ------------------------------------------------ */
+
+/* The row's mean (0 unless layer norm) and 1 / sqrt(mean square distance from it + eps). */
+static void norm_stats(const void* v, int64_t at, int32_t f, int32_t dtype, int32_t form, double eps,
+                       double* mean, double* rstd) {
+  double m = 0.0, s = 0.0;
+  if (form == 2)
+    for (int32_t i = 0; i < f; ++i) m += oracle_widen(v, at + i, dtype) / f;
+  for (int32_t i = 0; i < f; ++i) {
+    const double d = oracle_widen(v, at + i, dtype) - m;
+    s += d * d;
+  }
+  *mean = m;
+  *rstd = form == 0 ? 1.0 : 1.0 / sqrt(s / f + eps);
+}
+
+int oracle_norm(int64_t tokens, int32_t f, int32_t dtype, int32_t form, double eps, const void* v,
+                int64_t ldv, const float* w, const float* c, double* out) {
+  if (tokens < 0 || f <= 0 || form < 0 || form > 2) return -1;
+  for (int64_t t = 0; t < tokens; ++t) {
+    double mean, rstd;
+    norm_stats(v, t * ldv, f, dtype, form, eps, &mean, &rstd);
+    for (int32_t i = 0; i < f; ++i) {
+      double n = (oracle_widen(v, t * ldv + i, dtype) - mean) * rstd;
+      if (form != 0) n *= w[i];
+      if (form == 2 && c) n += c[i];
+      out[t * f + i] = n;
+    }
+  }
+  return 0;
+}
+
+int oracle_norm_backward(int64_t tokens, int32_t f, int32_t dtype, int32_t form, double eps,
+                         const void* v, int64_t ldv, const float* w, const double* g, double* dv,
+                         double* dw, double* dc) {
+  if (tokens < 0 || f <= 0 || form < 0 || form > 2) return -1;
+  for (int32_t i = 0; i < f; ++i) dw[i] = dc[i] = 0.0;
+  for (int64_t t = 0; t < tokens; ++t) {
+    double mean, rstd, along = 0.0, level = 0.0;
+    norm_stats(v, t * ldv, f, dtype, form, eps, &mean, &rstd);
+    for (int32_t i = 0; i < f; ++i) {
+      const double n = (oracle_widen(v, t * ldv + i, dtype) - mean) * rstd, gi = g[t * f + i];
+      const double u = form == 0 ? gi : gi * w[i];
+      along += u * n / f;
+      if (form == 2) level += u / f;
+      dw[i] += gi * n;
+      dc[i] += gi;
+    }
+    for (int32_t i = 0; i < f; ++i) {
+      const double n = (oracle_widen(v, t * ldv + i, dtype) - mean) * rstd, gi = g[t * f + i];
+      dv[t * f + i] = form == 0 ? gi : rstd * (gi * w[i] - n * along - level);
+    }
+  }
+  return 0;
+}
+
+int oracle_act(int32_t form, int64_t n, const double* z, double* value, double* slope) {
+  if (form < 0 || form > 3) return -1;
+  for (int64_t i = 0; i < n; ++i) {
+    const double s = 1.0 / (1.0 + exp(-z[i]));
+    value[i] = form == 0 ? z[i] : form == 1 ? (z[i] > 0 ? z[i] : 0.0)
+             : form == 2 ? oracle_gelu_tanh(z[i]) : z[i] * s;
+    slope[i] = form == 0 ? 1.0 : form == 1 ? (z[i] > 0 ? 1.0 : 0.0)
+             : form == 2 ? oracle_gelu_tanh_grad(z[i]) : s + z[i] * s * (1.0 / (1.0 + exp(z[i])));
+  }
+  return 0;
+}
+
+/* 127 v / top is compared with whole numbers and halves as 127 v with their product with top: exact for
+ * fp32 v and top. */
+int oracle_q8_rows(int64_t tokens, int32_t f, int32_t group, const double* v, int8_t* q, float* scale) {
+  if (tokens < 0 || f <= 0 || group <= 0) return -1;
+  const int32_t groups = (f + group - 1) / group;
+  for (int64_t t = 0; t < tokens; ++t)
+    for (int32_t j = 0; j < groups; ++j) {
+      const int32_t end = (j + 1) * group < f ? (j + 1) * group : f;
+      double top = 0.0;
+      int bad = 0;
+      for (int32_t i = j * group; i < end; ++i) {
+        const double a = fabs(v[t * f + i]);
+        if (!isfinite(a)) bad = 1;
+        if (a > top) top = a;
+      }
+      scale[t * groups + j] = bad ? NAN : (float)top / 127.0f;
+      for (int32_t i = j * group; i < end; ++i) {
+        const double a = 127.0 * fabs(v[t * f + i]);
+        int32_t k = 0;
+        if (!bad && top > 0.0) {
+          while (k < 127 && (k + 0.5) * top < a) ++k;           /* a <= (k + 1/2) top */
+          if (k < 127 && (k + 0.5) * top == a && (k & 1)) ++k;   /* a tie goes to even */
+        }
+        q[t * f + i] = (int8_t)(v[t * f + i] < 0 ? -k : k);
+      }
+    }
+  return 0;
+}
+
+int oracle_q8_product(int32_t m, int32_t n, int32_t k, const int8_t* a, int64_t lda, const int8_t* b,
+                      int64_t ldb, int64_t* out) {
+  if (m <= 0 || n < 0 || k <= 0) return -1;
+#pragma omp parallel for
+  for (int32_t j = 0; j < n; ++j)
+    for (int32_t i = 0; i < m; ++i) {
+      int64_t s = 0;
+      for (int32_t p = 0; p < k; ++p) s += (int64_t)a[i * lda + p] * b[j * ldb + p];
+      out[(int64_t)j * m + i] = s;
+    }
+  return 0;
+}

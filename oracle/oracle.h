@@ -214,6 +214,22 @@ double   oracle_gelu_tanh(double x);
 double   oracle_gelu_tanh_grad(double x);
 int      oracle_max_threads(void);
 
+/* Norms of rows of f entries (form 0: none, 1: v / sqrt(mean v^2 + eps) w, 2: layer norm with w and c,
+ * c may be NULL), unrounded, tokens x f; and the gradients dv (tokens x f), dw, dc (f) of sum(g * out). */
+int oracle_norm(int64_t tokens, int32_t f, int32_t dtype, int32_t form, double eps, const void* v,
+                int64_t ldv, const float* w, const float* c, double* out);
+int oracle_norm_backward(int64_t tokens, int32_t f, int32_t dtype, int32_t form, double eps,
+                         const void* v, int64_t ldv, const float* w, const double* g, double* dv,
+                         double* dw, double* dc);
+/* act(z) and act'(z): form 0 identity, 1 RELU, 2 GELU in its tanh form, 3 z / (1 + exp(-z)). */
+int oracle_act(int32_t form, int64_t n, const double* z, double* value, double* slope);
+/* 8-bit rows of v (tokens x f, fp32 or bf16 values): q = 127 v / max |v| of its group, to the nearest
+ * whole number, ties to even; scale = max / 127 in fp32; a group with an infinity or NaN: 0 and NaN. */
+int oracle_q8_rows(int64_t tokens, int32_t f, int32_t group, const double* v, int8_t* q, float* scale);
+/* out[j * m + i] = sum_p a[i * lda + p] b[j * ldb + p]. */
+int oracle_q8_product(int32_t m, int32_t n, int32_t k, const int8_t* a, int64_t lda, const int8_t* b,
+                      int64_t ldb, int64_t* out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,6 +1,6 @@
 """MI355X (gfx950) TPP library: thin Python binding of the C ABI in include/tpp_brgemm.h,
-include/tpp_transform.h, include/tpp_embedding.h, include/tpp_equation.h and
-include/tpp_attention.h.
+include/tpp_transform.h, include/tpp_embedding.h, include/tpp_equation.h,
+include/tpp_attention.h, include/tpp_residual.h and include/tpp_q8.h.
 
 Argument marshalling only: every step of the computation runs in the HIP kernels of
 ``libtpp_mi355x.so``.  The functions keep the C names; pointers are plain integers (device
@@ -37,6 +37,9 @@ TPP_RED_SUM, TPP_RED_MUL, TPP_RED_MIN, TPP_RED_MAX = 0, 1, 2, 3
 TPP_RED_BY_COLS, TPP_RED_BY_ROWS, TPP_RED_X, TPP_RED_X2 = 1, 2, 4, 8
 TPP_TR_TRANSPOSE, TPP_TR_VNNI, TPP_TR_VNNI_TO_VNNI_T = 0, 1, 2
 TPP_ROT_HALVES, TPP_ROT_PAIRS = 0, 1
+TPP_NORM_NONE, TPP_NORM_RMS, TPP_NORM_LAYER = 0, 1, 2
+TPP_GATE_NONE, TPP_GATE_IDENTITY, TPP_GATE_SIGMOID, TPP_GATE_TANH = 0, 1, 2, 3
+TPP_ACT_NONE, TPP_ACT_RELU, TPP_ACT_GELU_TANH, TPP_ACT_SILU = 0, 1, 2, 3
 
 _c_void_p, _i64, _i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
 
@@ -153,6 +156,38 @@ _sig("tpp_paged_attention", _i32, ctypes.POINTER(tpp_attn_desc), _kvc, _i64, _c_
      _c_void_p, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p)
 _sig("tpp_cache_evict", _i32, _kvc, _i64, _i64, _i64, _c_void_p, _c_void_p, _i64, _c_void_p,
      _c_void_p, _c_void_p, _i64, _c_void_p, _c_void_p, _c_void_p, _c_void_p)
+
+
+class tpp_residual_desc(ctypes.Structure):
+    _fields_ = [("features", _i32), ("dtype", _i32), ("after", _i32), ("before", _i32), ("gate", _i32),
+                ("gate_type", _i32), ("scale", ctypes.c_float), ("eps", ctypes.c_float),
+                ("gate_every", _i64)]
+
+
+class tpp_q8_desc(ctypes.Structure):
+    _fields_ = [(f, _i32) for f in ("features", "group", "dtype", "act", "gated")]
+
+
+class tpp_q8_gemm_desc(ctypes.Structure):
+    _fields_ = [("m", _i32), ("n", _i32), ("k", _i32), ("lda", _i64), ("ldb", _i64), ("ldc", _i64),
+                ("b_type", _i32), ("c_type", _i32), ("flags", ctypes.c_uint32)]
+
+
+_rsd, _q8d, _q8g = (ctypes.POINTER(t) for t in (tpp_residual_desc, tpp_q8_desc, tpp_q8_gemm_desc))
+_sig("tpp_residual_norm", _i32, _rsd, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p,
+     _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p,
+     _c_void_p)
+_sig("tpp_residual_norm_backward", _i32, _rsd, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p,
+     _c_void_p, _c_void_p, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p,
+     _i64, _c_void_p, _i64, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p)
+_sig("tpp_q8_quantize", _i32, _q8d, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p)
+_sig("tpp_q8_act", _i32, _q8d, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64,
+     _c_void_p)
+_sig("tpp_q8_act_backward", _i32, _q8d, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64,
+     _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _c_void_p)
+_sig("tpp_q8_gemm", _i32, _q8g, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+     _c_void_p)
+_sig("tpp_q8_linear", _i32, _q8g, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p)
 
 
 def _p(x):
@@ -374,6 +409,55 @@ def tpp_cache_evict(cache, n_seqs, max_len, budget, lens, pages, ld_pages, total
     _check(_lib.tpp_cache_evict(cache, n_seqs, max_len, budget, _p(lens), _p(pages), ld_pages,
                                 _p(totals), _p(pos), _p(horizon), ldt, _p(len_out), _p(totals_out),
                                 _p(pos_out), stream), "tpp_cache_evict")
+
+
+def tpp_residual_norm(desc, tokens, x, ldx, b, ldb, gate, ldg, w_after, c_after, w_before, c_before, r,
+                      ldr, y, ldy, q, ldq, q_scale, stream=None):
+    """desc: tpp_residual_desc; gate, the norms' vectors, y, and q with q_scale may be None."""
+    _check(_lib.tpp_residual_norm(
+        desc, tokens, _p(x), ldx, _p(b), ldb, _p(gate), ldg, _p(w_after), _p(c_after), _p(w_before),
+        _p(c_before), _p(r), ldr, _p(y), ldy, _p(q), ldq, _p(q_scale), stream), "tpp_residual_norm")
+
+
+def tpp_residual_norm_backward(desc, tokens, b, ldb, gate, ldg, w_after, c_after, w_before, r, ldr, gr,
+                               ldgr, gy, ldgy, dx, lddx, db, lddb, dgate, lddg, dw_after, dc_after,
+                               dw_before, dc_before, stream=None):
+    """Gradients that are not wanted are None."""
+    _check(_lib.tpp_residual_norm_backward(
+        desc, tokens, _p(b), ldb, _p(gate), ldg, _p(w_after), _p(c_after), _p(w_before), _p(r), ldr,
+        _p(gr), ldgr, _p(gy), ldgy, _p(dx), lddx, _p(db), lddb, _p(dgate), lddg, _p(dw_after),
+        _p(dc_after), _p(dw_before), _p(dc_before), stream), "tpp_residual_norm_backward")
+
+
+def tpp_q8_quantize(desc, tokens, z, ldz, q, ldq, scale, lds, stream=None):
+    """desc: tpp_q8_desc; act(z) in 8-bit rows."""
+    _check(_lib.tpp_q8_quantize(desc, tokens, _p(z), ldz, _p(q), ldq, _p(scale), lds, stream),
+           "tpp_q8_quantize")
+
+
+def tpp_q8_act(desc, tokens, z, ldz, h, ldh, q, ldq, scale, lds, stream=None):
+    """desc: tpp_q8_desc; h = act(z) (or None), and z in 8-bit rows."""
+    _check(_lib.tpp_q8_act(desc, tokens, _p(z), ldz, _p(h), ldh, _p(q), ldq, _p(scale), lds, stream),
+           "tpp_q8_act")
+
+
+def tpp_q8_act_backward(desc, tokens, q, ldq, scale, lds, gh, ldgh, dz, lddz, h2, ldh2, dbias,
+                        stream=None):
+    """From the rows that tpp_q8_act kept; outputs that are not wanted are None."""
+    _check(_lib.tpp_q8_act_backward(desc, tokens, _p(q), ldq, _p(scale), lds, _p(gh), ldgh, _p(dz), lddz,
+                                    _p(h2), ldh2, _p(dbias), stream), "tpp_q8_act_backward")
+
+
+def tpp_q8_gemm(desc, a, a_scale, b, b_scale, c, bias, stream=None):
+    """desc: tpp_q8_gemm_desc; 8-bit weights a, 8-bit tokens b."""
+    _check(_lib.tpp_q8_gemm(desc, _p(a), _p(a_scale), _p(b), _p(b_scale), _p(c), _p(bias), stream),
+           "tpp_q8_gemm")
+
+
+def tpp_q8_linear(desc, a, a_scale, x, c, bias, stream=None):
+    """tpp_q8_gemm of activations x, turned into 8-bit rows first."""
+    _check(_lib.tpp_q8_linear(desc, _p(a), _p(a_scale), _p(x), _p(c), _p(bias), stream),
+           "tpp_q8_linear")
 
 
 def tpp_status_string(s: int) -> str:

@@ -10,6 +10,8 @@
 #include "tpp_brgemm.h"
 #include "tpp_embedding.h"
 #include "tpp_equation.h"
+#include "tpp_q8.h"
+#include "tpp_residual.h"
 #include "tpp_transform.h"
 
 namespace tpp {
@@ -344,5 +346,76 @@ struct EvictParams {
 // Floats of work space (0: one launch without any; -1: more than the launches count).
 int64_t evict_work_floats(const EvictParams& p);
 hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream);
+
+// The residual stream's norms (residual_kernels.hip).
+struct ResidualParams {
+  const void *x, *b, *gate;   // forward: the stream; both: the block's output, its gate
+  const float *wa, *ca, *wb, *cb;
+  void *r, *y;                // forward's outputs; backward reads r
+  int8_t* q;                  // null, or y in 8-bit rows
+  float* qs;
+  const void *gr, *gy;        // backward
+  void *dx, *db, *dgate;
+  float* dv[4];               // gradients of wa, ca, wb, cb
+  int64_t ldx, ldb, ldg, ldr, ldy, ldq, ldgr, ldgy, lddx, lddb, lddg;
+  int64_t tokens, gate_every;
+  int32_t f, bf16, after, before, gate_form, gate_bf16;
+  float scale, eps;
+};
+hipError_t launch_residual(const ResidualParams& p, hipStream_t stream);
+// Floats of work space of the backward pass.
+int64_t residual_backward_work_floats(const ResidualParams& p);
+hipError_t launch_residual_backward(const ResidualParams& p, float* work, hipStream_t stream);
+
+// What the backward passes return without tokens: `n` zeros; and those of all sums over tokens.
+hipError_t launch_zeros(void* to, int64_t n, bool bf16, hipStream_t stream);
+hipError_t launch_residual_zeros(const ResidualParams& p, hipStream_t stream);
+
+// 8-bit rows (q8_kernels.hip).
+struct Q8Params {
+  const void* z;
+  const void* gh;      // backward
+  void *h, *dz;        // h: act(z); backward: act(z')
+  int8_t* q;           // read by the backward pass
+  float* s;
+  float* dbias;
+  int64_t ldz, ldh, ldq, lds, ldgh, lddz, tokens;
+  int32_t f, group, bf16, act, gated;
+};
+hipError_t launch_q8_quantize(const Q8Params& p, hipStream_t stream);
+hipError_t launch_q8_act(const Q8Params& p, hipStream_t stream);
+int64_t q8_backward_work_floats(const Q8Params& p);
+hipError_t launch_q8_act_backward(const Q8Params& p, float* work, hipStream_t stream);
+
+// Products of 8-bit rows (q8_gemm_kernels.hip).
+struct Q8GemmParams {
+  const int8_t *a, *b;
+  const float *sa, *sb, *bias;
+  void* c;
+  int64_t lda, ldb, ldc;
+  int32_t m, n, k, c_bf16;
+  uint32_t flags;
+};
+hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream);
+
+// out = the sum over `parts` rows of `width` floats, for each of `n` outputs of its own (fold_kernels in
+// residual_kernels.hip).
+struct FoldJob {
+  const float* from;   // the first part; parts follow `width` floats apart
+  int64_t parts;       // of one output row
+  int64_t rows;        // output rows: row g sums the parts from g * parts on
+  void* to;            // ld apart
+  int64_t ld;
+  int32_t bf16;
+  int32_t slope;       // tpp_gate_form of the gate whose slope the sums are multiplied with (0: none)
+  const void* gate;    // ldg apart
+  int64_t ldg;
+};
+constexpr int FOLD_JOBS = 5;
+struct FoldParams {
+  FoldJob job[FOLD_JOBS];
+  int32_t n, width;
+};
+hipError_t launch_fold(const FoldParams& p, hipStream_t stream);
 
 }  // namespace tpp

@@ -1,9 +1,10 @@
 // tpp_api.hip -- the C ABI of include/tpp_brgemm.h, include/tpp_transform.h,
-// include/tpp_embedding.h, include/tpp_equation.h and include/tpp_attention.h: argument checks,
-// the dispatch cache, kernel selection and launches.  Host code only; the kernels live in
-// brgemm_kernels.hip, brgemm_dl_kernels.hip, reduce_kernels.hip, transform_kernels.hip,
-// embedding_kernels.hip, equation.hip (which also holds the equation planner), rope_kernels.hip,
-// attention_kernels.hip and cache_kernels.hip.
+// include/tpp_embedding.h, include/tpp_equation.h, include/tpp_attention.h, include/tpp_residual.h and
+// include/tpp_q8.h: argument checks, the dispatch cache, kernel selection and launches.  Host code
+// only; the kernels live in brgemm_kernels.hip, brgemm_dl_kernels.hip, reduce_kernels.hip,
+// transform_kernels.hip, embedding_kernels.hip, equation.hip (which also holds the equation planner),
+// rope_kernels.hip, attention_kernels.hip, cache_kernels.hip, residual_kernels.hip, q8_kernels.hip and
+// q8_gemm_kernels.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -181,7 +182,10 @@ int32_t choose_kernel(const tpp_brgemm_kernel_s& h, const tpp::BrgemmParams& p) 
 // a device synchronisation, since queued work may still use the old one), kept until exit.  The
 // caller keeps `hold` (the cache's lock) until its kernels are enqueued, so another host thread
 // cannot free the buffer between the lookup and the launch that uses it.
-enum WorkPurpose { WORK_REDUCE = 0, WORK_SPLIT = 1, WORK_ROPE = 2, WORK_ATTENTION = 3, WORK_EVICT = 4 };
+enum WorkPurpose {
+  WORK_REDUCE = 0, WORK_SPLIT = 1, WORK_ROPE = 2, WORK_ATTENTION = 3, WORK_EVICT = 4, WORK_RESIDUAL = 5,
+  WORK_Q8 = 6
+};
 struct WorkBuffer {
   float* ptr = nullptr;
   int64_t floats = 0;
@@ -1266,6 +1270,334 @@ tpp_status tpp_cache_evict(const tpp_kv_cache* cache, int64_t n_seqs, int64_t ma
   if (e == hipErrorInvalidConfiguration)
     return fail(TPP_ERR_UNSUPPORTED, "%s", too_many);
   return launched("eviction", e);
+}
+
+}  // extern "C"
+
+// ---- the residual stream's norms (include/tpp_residual.h) ------------------------------------------
+
+namespace {
+
+constexpr int32_t MOST_FEATURES = 1 << 20;
+
+tpp_status check_ld(const char* what, const void* ptr, int64_t ld, int64_t features) {
+  if (ptr && ld < features) return fail(TPP_ERR_INVALID_ARG, "leading dimension of %s below its features", what);
+  return TPP_OK;
+}
+
+// The description and what both directions read of it; fills p.
+tpp_status check_residual(const tpp_residual_desc* d, int64_t tokens, const void* b, int64_t ldb,
+                          const void* gate, int64_t ldg, const float* w_after, const float* c_after,
+                          const float* w_before, const float* c_before, tpp::ResidualParams& p) {
+  if (!d) return fail(TPP_ERR_INVALID_ARG, "NULL desc");
+  if (tokens < 0) return fail(TPP_ERR_INVALID_ARG, "tokens < 0");
+  if (d->features <= 0) return fail(TPP_ERR_INVALID_ARG, "features must be > 0");
+  if (!valid_dtype(d->dtype) || !valid_dtype(d->gate_type))
+    return fail(TPP_ERR_INVALID_ARG, "unknown datatype code");
+  for (int32_t form : {d->after, d->before})
+    if (form < TPP_NORM_NONE || form > TPP_NORM_LAYER) return fail(TPP_ERR_INVALID_ARG, "unknown norm %d", form);
+  if (d->gate < TPP_GATE_NONE || d->gate > TPP_GATE_TANH)
+    return fail(TPP_ERR_INVALID_ARG, "unknown gate %d", d->gate);
+  if (!std::isfinite(d->scale)) return fail(TPP_ERR_INVALID_ARG, "scale must be finite");
+  if (!std::isfinite(d->eps) || d->eps < 0) return fail(TPP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (d->gate_every < 0) return fail(TPP_ERR_INVALID_ARG, "gate_every must be >= 0");
+  if (tpp_status s = check_ld("b", b, ldb, d->features)) return s;
+  if (d->gate != TPP_GATE_NONE)
+    if (tpp_status s = check_ld("gate", gate, ldg, d->features)) return s;
+  if (d->features > MOST_FEATURES)
+    return fail(TPP_ERR_UNSUPPORTED, "%d features are above %d", d->features, MOST_FEATURES);
+  if (tokens > 0) {
+    if (!b || (d->gate != TPP_GATE_NONE && !gate)) return fail(TPP_ERR_INVALID_ARG, "NULL b or gate");
+    if (d->after != TPP_NORM_NONE && !w_after) return fail(TPP_ERR_INVALID_ARG, "NULL w_after");
+  }
+  p = tpp::ResidualParams();
+  p.b = b;
+  p.ldb = ldb;
+  p.gate = d->gate != TPP_GATE_NONE ? gate : nullptr;
+  p.ldg = ldg;
+  p.wa = w_after;
+  p.ca = c_after;
+  p.wb = w_before;
+  p.cb = c_before;
+  p.tokens = tokens;
+  p.gate_every = d->gate_every;
+  p.f = d->features;
+  p.bf16 = d->dtype == TPP_DT_BF16;
+  p.after = d->after;
+  p.before = d->before;
+  p.gate_form = d->gate;
+  p.gate_bf16 = d->gate_type == TPP_DT_BF16;
+  p.scale = d->scale;
+  p.eps = d->eps;
+  return TPP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+tpp_status tpp_residual_norm(const tpp_residual_desc* desc, int64_t tokens, const void* x, int64_t ldx,
+                             const void* b, int64_t ldb, const void* gate, int64_t ldg,
+                             const float* w_after, const float* c_after, const float* w_before,
+                             const float* c_before, void* r, int64_t ldr, void* y, int64_t ldy,
+                             int8_t* q, int64_t ldq, float* q_scale, void* stream) {
+  tpp::ResidualParams p;
+  if (tpp_status s = check_residual(desc, tokens, b, ldb, gate, ldg, w_after, c_after, w_before, c_before, p))
+    return s;
+  if (tpp_status s = check_ld("x", x, ldx, p.f)) return s;
+  if (tpp_status s = check_ld("r", r, ldr, p.f)) return s;
+  if (tpp_status s = check_ld("y", y, ldy, p.f)) return s;
+  if (tpp_status s = check_ld("q", q, ldq, p.f)) return s;
+  if ((q != nullptr) != (q_scale != nullptr))
+    return fail(TPP_ERR_INVALID_ARG, "q and q_scale are given or NULL together");
+  if (tokens == 0) return ok();
+  if (!x || !r) return fail(TPP_ERR_INVALID_ARG, "NULL x or r");
+  if ((y || q) && p.before != TPP_NORM_NONE && !w_before) return fail(TPP_ERR_INVALID_ARG, "NULL w_before");
+  if (r == b || y == x || y == r || (r == x && ldr != ldx) || (y == b && ldy != ldb))
+    return fail(TPP_ERR_INVALID_ARG, "outputs overlap inputs or each other (only r = x and y = b may, with one ld)");
+  p.x = x;
+  p.ldx = ldx;
+  p.r = r;
+  p.ldr = ldr;
+  p.y = y;
+  p.ldy = ldy;
+  p.q = q;
+  p.ldq = ldq;
+  p.qs = q_scale;
+  return launched("residual norm", tpp::launch_residual(p, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_residual_norm_backward(const tpp_residual_desc* desc, int64_t tokens, const void* b,
+                                      int64_t ldb, const void* gate, int64_t ldg, const float* w_after,
+                                      const float* c_after, const float* w_before, const void* r,
+                                      int64_t ldr, const void* gr, int64_t ldgr, const void* gy,
+                                      int64_t ldgy, void* dx, int64_t lddx, void* db, int64_t lddb,
+                                      void* dgate, int64_t lddg, float* dw_after, float* dc_after,
+                                      float* dw_before, float* dc_before, void* stream) {
+  tpp::ResidualParams p;
+  if (tpp_status s = check_residual(desc, tokens, b, ldb, gate, ldg, w_after, c_after, w_before, nullptr, p))
+    return s;
+  if (tpp_status s = check_ld("r", r, ldr, p.f)) return s;
+  if (tpp_status s = check_ld("gr", gr, ldgr, p.f)) return s;
+  if (tpp_status s = check_ld("gy", gy, ldgy, p.f)) return s;
+  if (tpp_status s = check_ld("dx", dx, lddx, p.f)) return s;
+  if (tpp_status s = check_ld("db", db, lddb, p.f)) return s;
+  if (tpp_status s = check_ld("dgate", dgate, lddg, p.f)) return s;
+  if (dgate && p.gate_form == TPP_GATE_NONE) return fail(TPP_ERR_INVALID_ARG, "dgate without a gate");
+  if ((dw_after && p.after == TPP_NORM_NONE) || (dc_after && p.after != TPP_NORM_LAYER) ||
+      (dw_before && p.before == TPP_NORM_NONE) || (dc_before && p.before != TPP_NORM_LAYER))
+    return fail(TPP_ERR_INVALID_ARG, "gradient of a vector that the norm does not have");
+  p.r = const_cast<void*>(r);
+  p.ldr = ldr;
+  p.gr = gr;
+  p.ldgr = ldgr;
+  p.gy = gy;
+  p.ldgy = ldgy;
+  p.dx = dx;
+  p.lddx = lddx;
+  p.db = db;
+  p.lddb = lddb;
+  p.dgate = dgate;
+  p.lddg = lddg;
+  p.dv[0] = dw_after;
+  p.dv[1] = dc_after;
+  p.dv[2] = dw_before;
+  p.dv[3] = dc_before;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (tokens == 0) return launched("residual norm backward", tpp::launch_residual_zeros(p, st));
+  if (!gr && !gy) return fail(TPP_ERR_INVALID_ARG, "NULL gr and gy");
+  if (gy && p.before != TPP_NORM_NONE && (!r || !w_before))
+    return fail(TPP_ERR_INVALID_ARG, "NULL r or w_before");
+  for (const void* out : {static_cast<const void*>(dx), static_cast<const void*>(db)})
+    if (out && (out == b || out == r || out == gr || out == gy))
+      return fail(TPP_ERR_INVALID_ARG, "dx or db overlaps an input");
+  float* work = nullptr;
+  std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
+  const int64_t need = tpp::residual_backward_work_floats(p);
+  if (tpp_status s = call_work(WORK_RESIDUAL, stream, need, &work, hold)) return s;
+  if (need > 0 && !work)
+    return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
+  return launched("residual norm backward", tpp::launch_residual_backward(p, work, st));
+}
+
+}  // extern "C"
+
+// ---- 8-bit rows (include/tpp_q8.h) -------------------------------------------------------------------
+
+namespace {
+
+// The description, the 8-bit rows of `width` entries (0: features, or twice that if gated) and their scales.
+tpp_status check_q8(const tpp_q8_desc* d, int64_t tokens, bool whole_z, const int8_t* q, int64_t ldq,
+                    const float* scale, int64_t lds, tpp::Q8Params& p) {
+  if (!d) return fail(TPP_ERR_INVALID_ARG, "NULL desc");
+  if (tokens < 0) return fail(TPP_ERR_INVALID_ARG, "tokens < 0");
+  if (d->features <= 0 || d->group < 0) return fail(TPP_ERR_INVALID_ARG, "features must be > 0, group >= 0");
+  if (!valid_dtype(d->dtype)) return fail(TPP_ERR_INVALID_ARG, "unknown datatype code");
+  if (d->act < TPP_ACT_NONE || d->act > TPP_ACT_SILU)
+    return fail(TPP_ERR_INVALID_ARG, "unknown activation %d", d->act);
+  if (d->gated != 0 && d->gated != 1) return fail(TPP_ERR_INVALID_ARG, "gated must be 0 or 1");
+  if (d->group != 0 && (d->group < 16 || d->group > 512 || (d->group & (d->group - 1)) != 0))
+    return fail(TPP_ERR_UNSUPPORTED, "group %d is not 0, 16, 32, 64, 128, 256 or 512", d->group);
+  if (d->features > MOST_FEATURES >> d->gated)
+    return fail(TPP_ERR_UNSUPPORTED, "%d features are above %d", d->features, MOST_FEATURES >> d->gated);
+  const int64_t width = whole_z && d->gated ? 2 * (int64_t)d->features : d->features;
+  if (ldq < width) return fail(TPP_ERR_INVALID_ARG, "ldq below the row's entries");
+  if (lds < (d->group ? (width + d->group - 1) / d->group : 1))
+    return fail(TPP_ERR_INVALID_ARG, "lds below the row's groups");
+  if (tokens > 0 && (!q || !scale)) return fail(TPP_ERR_INVALID_ARG, "NULL q or scale");
+  p = tpp::Q8Params();
+  p.q = const_cast<int8_t*>(q);
+  p.ldq = ldq;
+  p.s = const_cast<float*>(scale);
+  p.lds = lds;
+  p.tokens = tokens;
+  p.f = d->features;
+  p.group = d->group;
+  p.bf16 = d->dtype == TPP_DT_BF16;
+  p.act = d->act;
+  p.gated = d->gated;
+  return TPP_OK;
+}
+
+tpp_status check_z(tpp::Q8Params& p, const void* z, int64_t ldz) {
+  if (ldz < ((int64_t)p.f << p.gated)) return fail(TPP_ERR_INVALID_ARG, "ldz below the entries of a token");
+  if (!z && p.tokens > 0) return fail(TPP_ERR_INVALID_ARG, "NULL z");
+  p.z = z;
+  p.ldz = ldz;
+  return TPP_OK;
+}
+
+tpp_status check_q8_gemm(const tpp_q8_gemm_desc* d, const int8_t* a, const float* a_scale, const void* b,
+                         void* c, const float* bias, tpp::Q8GemmParams& p) {
+  if (!d) return fail(TPP_ERR_INVALID_ARG, "NULL desc");
+  if (d->m <= 0 || d->n < 0 || d->k <= 0) return fail(TPP_ERR_INVALID_ARG, "m, k must be > 0, n >= 0");
+  if (d->lda < d->k || d->ldb < d->k || d->ldc < d->m)
+    return fail(TPP_ERR_INVALID_ARG, "lda, ldb below k or ldc below m");
+  if (!valid_dtype(d->c_type) || !valid_dtype(d->b_type))
+    return fail(TPP_ERR_INVALID_ARG, "unknown datatype code");
+  if (d->flags & ~(uint32_t)(TPP_EPI_BIAS | TPP_EPI_RELU | TPP_EPI_GELU_TANH))
+    return fail(TPP_ERR_INVALID_ARG, "unknown epilogue bits");
+  if ((d->flags & TPP_EPI_RELU) && (d->flags & TPP_EPI_GELU_TANH))
+    return fail(TPP_ERR_INVALID_ARG, "RELU and GELU_TANH exclude each other");
+  if (d->k > 131071) return fail(TPP_ERR_UNSUPPORTED, "k %d is above 131071", d->k);
+  if (d->n > 0) {
+    if (!a || !a_scale || !b || !c) return fail(TPP_ERR_INVALID_ARG, "NULL weights, scales, tokens or c");
+    if ((d->flags & TPP_EPI_BIAS) && !bias) return fail(TPP_ERR_INVALID_ARG, "NULL bias");
+  }
+  p = tpp::Q8GemmParams();
+  p.a = a;
+  p.sa = a_scale;
+  p.bias = bias;
+  p.c = c;
+  p.lda = d->lda;
+  p.ldb = d->ldb;
+  p.ldc = d->ldc;
+  p.m = d->m;
+  p.n = d->n;
+  p.k = d->k;
+  p.c_bf16 = d->c_type == TPP_DT_BF16;
+  p.flags = d->flags;
+  return TPP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+tpp_status tpp_q8_quantize(const tpp_q8_desc* desc, int64_t tokens, const void* z, int64_t ldz, int8_t* q,
+                           int64_t ldq, float* scale, int64_t lds, void* stream) {
+  tpp::Q8Params p;
+  if (tpp_status s = check_q8(desc, tokens, false, q, ldq, scale, lds, p)) return s;
+  if (tpp_status s = check_z(p, z, ldz)) return s;
+  if (tokens == 0) return ok();
+  return launched("8-bit rows", tpp::launch_q8_quantize(p, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_q8_act(const tpp_q8_desc* desc, int64_t tokens, const void* z, int64_t ldz, void* h,
+                      int64_t ldh, int8_t* q, int64_t ldq, float* scale, int64_t lds, void* stream) {
+  tpp::Q8Params p;
+  if (tpp_status s = check_q8(desc, tokens, true, q, ldq, scale, lds, p)) return s;
+  if (tpp_status s = check_z(p, z, ldz)) return s;
+  if (tpp_status s = check_ld("h", h, ldh, p.f)) return s;
+  if (tokens == 0) return ok();
+  if (h == z) return fail(TPP_ERR_INVALID_ARG, "h overlaps z");
+  p.h = h;
+  p.ldh = ldh;
+  return launched("8-bit activation", tpp::launch_q8_act(p, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_q8_act_backward(const tpp_q8_desc* desc, int64_t tokens, const int8_t* q, int64_t ldq,
+                               const float* scale, int64_t lds, const void* gh, int64_t ldgh, void* dz,
+                               int64_t lddz, void* h2, int64_t ldh2, float* dbias, void* stream) {
+  tpp::Q8Params p;
+  if (tpp_status s = check_q8(desc, tokens, true, q, ldq, scale, lds, p)) return s;
+  if (tpp_status s = check_ld("gh", gh, ldgh, p.f)) return s;
+  if (tpp_status s = check_ld("dz", dz, lddz, (int64_t)p.f << p.gated)) return s;
+  if (tpp_status s = check_ld("h2", h2, ldh2, p.f)) return s;
+  p.gh = gh;
+  p.ldgh = ldgh;
+  p.dz = dz;
+  p.lddz = lddz;
+  p.h = h2;
+  p.ldh = ldh2;
+  p.dbias = dbias;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (tokens == 0) {
+    if (!dbias) return ok();
+    return launched("8-bit activation backward", tpp::launch_zeros(dbias, p.f << p.gated, false, st));
+  }
+  if (!gh) return fail(TPP_ERR_INVALID_ARG, "NULL gh");
+  if (dz == gh || (h2 == gh && ldh2 != ldgh) || (h2 && h2 == dz))
+    return fail(TPP_ERR_INVALID_ARG, "outputs overlap gh or each other (only h2 = gh may, with one ld)");
+  float* work = nullptr;
+  std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
+  const int64_t need = tpp::q8_backward_work_floats(p);
+  if (tpp_status s = call_work(WORK_Q8, stream, need, &work, hold)) return s;
+  if (need > 0 && !work)
+    return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
+  return launched("8-bit activation backward", tpp::launch_q8_act_backward(p, work, st));
+}
+
+tpp_status tpp_q8_gemm(const tpp_q8_gemm_desc* desc, const int8_t* a, const float* a_scale,
+                       const int8_t* b, const float* b_scale, void* c, const float* bias, void* stream) {
+  tpp::Q8GemmParams p;
+  if (tpp_status s = check_q8_gemm(desc, a, a_scale, b, c, bias, p)) return s;
+  if (p.n == 0) return ok();
+  if (!b_scale) return fail(TPP_ERR_INVALID_ARG, "NULL b_scale");
+  p.b = b;
+  p.sb = b_scale;
+  return launched("8-bit product", tpp::launch_q8_gemm(p, static_cast<hipStream_t>(stream)));
+}
+
+tpp_status tpp_q8_linear(const tpp_q8_gemm_desc* desc, const int8_t* a, const float* a_scale,
+                         const void* x, void* c, const float* bias, void* stream) {
+  tpp::Q8GemmParams p;
+  if (tpp_status s = check_q8_gemm(desc, a, a_scale, x, c, bias, p)) return s;
+  if (p.n == 0) return ok();
+  if (c == x) return fail(TPP_ERR_INVALID_ARG, "c overlaps x");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  // the scales, then the rows, whose whole 16-byte chunks the product reads
+  const int64_t ldq = ((int64_t)p.k + 15) / 16 * 16, scales = ((int64_t)p.n + 3) / 4 * 4;
+  const int64_t need = scales + (int64_t)p.n * (ldq / 4);
+  float* work = nullptr;
+  std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
+  if (tpp_status s = call_work(WORK_Q8, stream, need, &work, hold)) return s;
+  if (!work) return fail(TPP_ERR_NO_MEMORY, "no work buffer of %lld floats under capture", (long long)need);
+  tpp::Q8Params z = {};
+  z.z = x;
+  z.ldz = desc->ldb;
+  z.q = reinterpret_cast<int8_t*>(work + scales);
+  z.ldq = ldq;
+  z.s = work;
+  z.lds = 1;
+  z.tokens = p.n;
+  z.f = p.k;
+  z.bf16 = desc->b_type == TPP_DT_BF16;
+  p.b = z.q;
+  p.ldb = ldq;
+  p.sb = z.s;
+  if (tpp_status s = launched("8-bit rows", tpp::launch_q8_quantize(z, st))) return s;
+  return launched("8-bit product", tpp::launch_q8_gemm(p, st));
 }
 
 }  // extern "C"
