@@ -415,7 +415,9 @@ constexpr int FOLD_JOBS = 5;
 struct FoldParams {
   FoldJob job[FOLD_JOBS];
   int32_t n, width;
+  uint32_t blocks[FOLD_JOBS];   // filled by the launcher: workgroup rows of a job, sets of its parts
+  int32_t sets[FOLD_JOBS];
 };
-hipError_t launch_fold(const FoldParams& p, hipStream_t stream);
+hipError_t launch_fold(FoldParams& p, hipStream_t stream);
 
 }  // namespace tpp

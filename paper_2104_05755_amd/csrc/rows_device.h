@@ -92,6 +92,12 @@ __device__ __forceinline__ T over_group(T v, T* part) {
   return v;
 }
 
+// 1 / sqrt(v): the instruction's unit in the last place is enough, but it takes no numbers below the normal
+// ones.
+__device__ __forceinline__ float rsqrt_of(float v) {
+  return v < 0x1p-100f ? 1.0f / sqrtf(v) : __builtin_amdgcn_rsqf(v);
+}
+
 // ---- activations --------------------------------------------------------------------------------
 __device__ __forceinline__ float sigmoid(float z) {   // (exp(-z) = inf gives 0)
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
@@ -159,6 +165,132 @@ __device__ __forceinline__ int32_t q8_round(float v, const Q8Group& g) {
     k = v < 0.0f ? -m : m;
   }
   return k == k ? (int32_t)k : 0;   // (NaN: an entry of a group without a scale)
+}
+
+// ---- chunks of eight entries --------------------------------------------------------------------
+// A lane has chunks of 8 consecutive entries of a row.  In a row that is no multiple of 8 the last chunk
+// ends with the row, and its first entries, which another lane has, count for nothing: they are taken as
+// zeros and not stored.  So there is no branch around a load, and nothing outside the row is read; the row
+// has 8 entries at least.
+struct Place {
+  int32_t at, skip;   // first entry, entries that another lane has (8: the lane has none)
+  Place() = default;
+  __device__ __forceinline__ Place(int32_t chunk, int32_t f) {
+    const int32_t start = chunk * 8;
+    at = min(start, f - 8);
+    skip = min(start - at, 8);
+  }
+  __device__ __forceinline__ bool none() const { return skip >= 8; }
+};
+
+// How a pass goes through the caches: what is moved once only displaces what may be read again.
+enum { CACHED, STREAM_OUT, STREAM };
+
+template <bool BF16>
+struct Raw {
+  u32x4 w[BF16 ? 1 : 2];
+};
+typedef uint32_t u32x2_a1 __attribute__((ext_vector_type(2), aligned(1)));
+
+template <bool BF16, int HOW>
+__device__ __forceinline__ Raw<BF16> load_raw(const void* p, int64_t at) {
+  Raw<BF16> r;
+  const char* from = static_cast<const char*>(p) + at * (BF16 ? 2 : 4);
+#pragma unroll
+  for (int h = 0; h < (BF16 ? 1 : 2); ++h) {
+    const GLOBAL_AS u32x4_a2* q = (const GLOBAL_AS u32x4_a2*)(from + 16 * h);
+    r.w[h] = HOW == STREAM ? (u32x4)__builtin_nontemporal_load(q) : (u32x4)*q;
+  }
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ void widen(const Raw<BF16>& r, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (BF16)
+      v[e] = __uint_as_float(e & 1 ? r.w[0][e / 2] & 0xffff0000u : r.w[0][e / 2] << 16);
+    else
+      v[e] = __uint_as_float(r.w[e / 4][e % 4]);
+  }
+}
+// Zeros in the place of what another lane has: as loaded, or widened.
+template <bool WHOLE, bool BF16>
+__device__ __forceinline__ void mask(const Place& c, Raw<BF16>& r) {
+#pragma unroll
+  for (int i = 0; i < (BF16 ? 4 : 8); ++i) {
+    uint32_t w = r.w[i / 4][i % 4];
+    if constexpr (WHOLE)
+      w = c.skip ? 0u : w;
+    else if constexpr (BF16)
+      w &= (2 * i >= c.skip ? 0xffffu : 0u) | (2 * i + 1 >= c.skip ? 0xffff0000u : 0u);
+    else
+      w = i >= c.skip ? w : 0u;
+    r.w[i / 4][i % 4] = w;
+  }
+}
+template <bool WHOLE>
+__device__ __forceinline__ void mask(const Place& c, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (WHOLE ? c.skip != 0 : e < c.skip) ? 0.0f : v[e];
+}
+__device__ __forceinline__ void load8(const float* p, int32_t at, float (&v)[8]) {
+  widen<false>(load_raw<false, CACHED>(p, at), v);
+}
+__device__ __forceinline__ void load8(const void* p, int64_t at, bool bf16, float (&v)[8]) {
+  if (bf16)
+    widen<true>(load_raw<true, CACHED>(p, at), v);
+  else
+    widen<false>(load_raw<false, CACHED>(p, at), v);
+}
+template <bool BF16>
+__device__ __forceinline__ Raw<BF16> narrow(const float (&v)[8]) {
+  Raw<BF16> r;
+#pragma unroll
+  for (int e = 0; e < (BF16 ? 4 : 8); ++e) {
+    if constexpr (BF16)
+      r.w[0][e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+    else
+      r.w[e / 4][e % 4] = __float_as_uint(v[e]);
+  }
+  return r;
+}
+template <bool BF16, bool WHOLE, int HOW>
+__device__ __forceinline__ void store_raw(void* p, int64_t row, const Place& c, const Raw<BF16>& r) {
+  char* to = static_cast<char*>(p) + (row + c.at) * (BF16 ? 2 : 4);
+  if (c.skip == 0) {
+#pragma unroll
+    for (int h = 0; h < (BF16 ? 1 : 2); ++h) {
+      GLOBAL_AS u32x4_a2* q = (GLOBAL_AS u32x4_a2*)(to + 16 * h);
+      if constexpr (HOW != CACHED)
+        __builtin_nontemporal_store((u32x4_a2)r.w[h], q);
+      else
+        *q = (u32x4_a2)r.w[h];
+    }
+  } else if (!WHOLE && !c.none()) {
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
+      if (e < c.skip) continue;
+      if constexpr (BF16)
+        gst<uint16_t>(to + 2 * e, (uint16_t)(e & 1 ? r.w[0][e / 2] >> 16 : r.w[0][e / 2]));
+      else
+        gst<uint32_t>(to + 4 * e, r.w[e / 4][e % 4]);
+    }
+  }
+}
+// Eight entries of an 8-bit row.
+template <bool WHOLE>
+__device__ __forceinline__ void store_q8(int8_t* row, const Place& c, const float (&v)[8], const Q8Group& g) {
+  if (c.none()) return;
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e / 4] |= ((uint32_t)q8_round(v[e], g) & 0xffu) << (8 * (e % 4));
+  if (c.skip == 0) {
+    gst<u32x2_a1>(row + c.at, (u32x2_a1){w[0], w[1]});
+  } else if (!WHOLE) {
+#pragma unroll
+    for (int e = 1; e < 8; ++e)
+      if (e >= c.skip) gst<uint8_t>(row + c.at + e, (uint8_t)(w[e / 4] >> (8 * (e % 4))));
+  }
 }
 
 }  // namespace rows
