@@ -8,6 +8,12 @@
 
 #include "internal.h"
 #include "rows_device.h"
+#ifndef TPP_BIG
+#define TPP_BIG 200
+#endif
+#ifndef TPP_MID
+#define TPP_MID 256
+#endif
 
 namespace tpp {
 namespace {
@@ -125,11 +131,248 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_direct_kernel(Q8GemmParams p)
   }
 }
 
+// ---- operands through LDS -------------------------------------------------------------------------
+// A workgroup has a BM x BN tile of C.  A stage is 128 bytes of k of its rows and columns, copied from
+// memory straight into one of SLOTS places in LDS (buffer_load_dwordx4 .. lds, a whole line to eight lanes)
+// and read as 16-byte fragments, rows' chunks XOR-swizzled so that 16 rows meet all banks.  A wavefront has
+// TM x TN products of 32 x 32 x 32; the fragments of a k-step are read while the one before is multiplied,
+// across the stages too: the last k-step of a stage comes after the barrier that ends its reading, beside
+// the next stage's first reads and the copies into the place that the barrier freed.
+typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
+constexpr int STAGE = 128;   // bytes of k
+
+struct TileGrid {
+  int32_t tiles_m, tiles_n, total, run, rest;   // tiles of an XCD, XCDs that have one more
+};
+// Workgroups go to the 8 XCDs in turn: each gets a run of tiles, in bands of 8 tile rows, so that the 32 it
+// has at once share rows and columns in its L2.
+__device__ __forceinline__ void tile_of(const TileGrid& g, int32_t& tm, int32_t& tn) {
+  const int32_t xcd = blockIdx.x & 7, nth = blockIdx.x >> 3;
+  const int32_t t = xcd * g.run + min(xcd, g.rest) + nth;
+  const int32_t band = t / (8 * g.tiles_n), in = t - band * 8 * g.tiles_n;
+  const int32_t rows = min(8, g.tiles_m - band * 8);
+  tn = in / rows;
+  tm = band * 8 + in - tn * rows;
+}
+
+template <int BM, int BN, int WM, int WN, int SLOTS, bool TAIL>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_tile_kernel(Q8GemmParams p, TileGrid grid) {
+  constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
+  constexpr int A_BYTES = BM * STAGE, SLOT = A_BYTES + BN * STAGE;
+  constexpr int A_LOADS = A_BYTES / 1024 / NW, B_LOADS = BN * STAGE / 1024 / NW, LOADS = A_LOADS + B_LOADS;
+  constexpr int KQ = STAGE / 32;
+  constexpr int SLAB = 32 * WTM * 4;   // a wavefront's 32 columns of C on their way out
+  constexpr int LDS = SLOTS * SLOT > NW * SLAB ? SLOTS * SLOT : NW * SLAB;
+  static_assert(LDS <= 160 * 1024 && A_LOADS >= 1 && B_LOADS >= 1, "tile");
+  __shared__ __attribute__((aligned(1024))) char lds[LDS];
+  const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t wm = wave % WM, wn = wave / WM;
+  int32_t tm_, tn_;
+  tile_of(grid, tm_, tn_);
+  const int32_t i0 = tm_ * BM, j0 = tn_ * BN;
+  const int32_t stages = (p.k + STAGE - 1) / STAGE;
+
+  // copies: load r of a wavefront fills 8 rows of 128 bytes; a lane has one chunk of one row (rows behind
+  // the last read the last: they reach only outputs that are not stored)
+  uint32_t la[A_LOADS], lb[B_LOADS];
+  const int32_t sub = lane >> 3, pos = lane & 7;
+  const auto chunk_at = [&](int32_t row) { return pos ^ ((row >> 1) & 7); };
+#pragma unroll
+  for (int r = 0; r < A_LOADS; ++r) {
+    const int32_t row = (wave * A_LOADS + r) * 8 + sub;
+    la[r] = (uint32_t)((int64_t)min(row, p.m - 1 - i0) * p.lda) + chunk_at(row) * 16;
+  }
+#pragma unroll
+  for (int r = 0; r < B_LOADS; ++r) {
+    const int32_t row = (wave * B_LOADS + r) * 8 + sub;
+    lb[r] = (uint32_t)((int64_t)min(row, p.n - 1 - j0) * p.ldb) + chunk_at(row) * 16;
+  }
+  const int8_t* base_a = p.a + (int64_t)i0 * p.lda;
+  const int8_t* base_b = p.b + (int64_t)j0 * p.ldb;
+  const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_AS char*)lds);
+  const auto issue = [&](int32_t s) {
+    const int32_t k0 = s * STAGE;
+    const uint32_t to = lds_at + (uint32_t)(s % SLOTS) * SLOT;
+    const i32x4 ra = raw_buffer(base_a + k0), rb = raw_buffer(base_b + k0);
+    if (TAIL && k0 + STAGE > p.k) {   // chunks behind k: the stage's first (the products mask them)
+      uint32_t ta[A_LOADS], tb[B_LOADS];
+#pragma unroll
+      for (int r = 0; r < A_LOADS; ++r) {
+        const int32_t c = chunk_at((wave * A_LOADS + r) * 8 + sub) * 16;
+        ta[r] = k0 + c < p.k ? la[r] : la[r] - c;
+      }
+#pragma unroll
+      for (int r = 0; r < B_LOADS; ++r) {
+        const int32_t c = chunk_at((wave * B_LOADS + r) * 8 + sub) * 16;
+        tb[r] = k0 + c < p.k ? lb[r] : lb[r] - c;
+      }
+      buffer_load_lds16_block<A_LOADS>(ra, ta, to + wave * A_LOADS * 1024);
+      buffer_load_lds16_block<B_LOADS>(rb, tb, to + A_BYTES + wave * B_LOADS * 1024);
+    } else {
+      buffer_load_lds16_block<A_LOADS>(ra, la, to + wave * A_LOADS * 1024);
+      buffer_load_lds16_block<B_LOADS>(rb, lb, to + A_BYTES + wave * B_LOADS * 1024);
+    }
+  };
+  // this wavefront's copies of all but the newest `later` stages are done
+  const auto landed = [&](int32_t later) {
+    if (SLOTS > 3 && later >= 3) __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * LOADS));
+    else if (SLOTS > 2 && later >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * LOADS));
+    else if (later >= 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));
+    else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  };
+
+  const int32_t half = lane >> 5, swz = ((lane & 31) >> 1) & 7;
+  const int32_t frag = (lane & 31) * STAGE + ((half ^ swz) << 4);   // (wavefronts' rows start at multiples of 32)
+  const auto read = [&](int32_t s, int kq, i32x4_t (&fa)[TM], i32x4_t (&fb)[TN]) {
+    const char* at = lds + (s % SLOTS) * SLOT;
+    const int32_t f = frag ^ (kq << 5);
+#pragma unroll
+    for (int t = 0; t < TM; ++t) fa[t] = *reinterpret_cast<const i32x4_t*>(at + (wm * WTM + t * 32) * STAGE + f);
+#pragma unroll
+    for (int t = 0; t < TN; ++t) fb[t] = *reinterpret_cast<const i32x4_t*>(at + A_BYTES + (wn * WTN + t * 32) * STAGE + f);
+  };
+  i32x16 acc[TM][TN];
+#pragma unroll
+  for (int x = 0; x < TM; ++x)
+#pragma unroll
+    for (int y = 0; y < TN; ++y)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[x][y][v] = 0;
+  const auto multiply = [&](int32_t s, int kq, const i32x4_t (&fa)[TM], i32x4_t (&fb)[TN]) {
+    if (TAIL && s == stages - 1) {
+      const int32_t have = p.k - s * STAGE - 32 * kq - 16 * half;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const int32_t n = have - 4 * d;
+        const uint32_t keep = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+#pragma unroll
+        for (int t = 0; t < TN; ++t) fb[t][d] &= keep;
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+#pragma unroll
+      for (int y = 0; y < TN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[x], fb[y], acc[x][y], 0, 0, 0);
+  };
+
+  for (int32_t s = 0; s < SLOTS && s < stages; ++s) issue(s);
+  landed(min(stages, SLOTS) - 1);
+  lds_barrier();
+  i32x4_t fa[2][TM], fb[2][TN];
+  read(0, 0, fa[0], fb[0]);
+  for (int32_t s = 0; s < stages; ++s) {
+#pragma unroll
+    for (int kq = 0; kq + 1 < KQ; ++kq) {
+      read(s, kq + 1, fa[(kq + 1) & 1], fb[(kq + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);   // the reads stay ahead of the products
+      multiply(s, kq, fa[kq & 1], fb[kq & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (s + 1 < stages) {
+      landed(min(stages - 2 - s, SLOTS - 2));
+      lds_barrier();   // every wavefront has read all of stage s, and stage s + 1 is there
+      read(s + 1, 0, fa[0], fb[0]);
+      if (s + SLOTS < stages) issue(s + SLOTS);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    multiply(s, KQ - 1, fa[(KQ - 1) & 1], fb[(KQ - 1) & 1]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  lds_barrier();
+
+  // C: a wavefront's 32 columns at a time through LDS, so that a store takes whole lines
+  char* slab = lds + wave * SLAB;
+  const int32_t iw = i0 + wm * WTM;
+  const bool full = i0 + BM <= p.m;
+#pragma unroll
+  for (int y = 0; y < TN; ++y) {
+    const int32_t j = j0 + wn * WTN + y * 32;   // first column
+    const float sb = gld<float>(p.sb + min(j + (lane & 31), p.n - 1));
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int32_t r = x * 32 + 8 * q + 4 * half;   // first of four rows
+        float sa[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
+        if (full) {
+          const f32x4_a4 w = gld<f32x4_a4>(p.sa + iw + r);
+          sa[0] = w[0], sa[1] = w[1], sa[2] = w[2], sa[3] = w[3];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sa[e] = gld<float>(p.sa + min(iw + r + e, p.m - 1));
+        }
+        if (p.flags & TPP_EPI_BIAS) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bias[e] = gld<float>(p.bias + min(iw + r + e, p.m - 1));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = activate((float)acc[x][y][4 * q + e] * sb * sa[e] + bias[e], p.flags);
+        const int32_t col = lane & 31;
+        if (p.c_bf16) {   // chunks of 8 rows
+          const int32_t ch = (x * 4 + q) ^ (col & (WTM / 8 - 1));
+          *reinterpret_cast<u32x2*>(slab + col * WTM * 2 + ch * 16 + half * 8) =
+              (u32x2){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        } else {          // of 4
+          const int32_t ch = ((x * 4 + q) * 2 + half) ^ (col & (WTM / 4 - 1));
+          *reinterpret_cast<f32x4*>(slab + col * WTM * 4 + ch * 16) = (f32x4){v[0], v[1], v[2], v[3]};
+        }
+      }
+    const auto out = [&](auto rows) {
+      constexpr int V = decltype(rows)::value, PER = WTM / V;   // entries of a chunk, chunks of a column
+#pragma unroll
+      for (int it = 0; it < 32 * PER / 64; ++it) {
+        const int32_t col = (it * 64 + lane) / PER, ch = (it * 64 + lane) % PER;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(slab + col * WTM * (16 / V) + ((ch ^ (col & (PER - 1))) << 4));
+        const int32_t i = iw + ch * V;
+        if (j + col >= p.n || i >= p.m) continue;
+        char* to = static_cast<char*>(p.c) + ((int64_t)(j + col) * p.ldc + i) * (16 / V);
+        if (i + V <= p.m) {
+          gst<u32x4_a2>(to, (u32x4_a2)w);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            if (i + e >= p.m) continue;
+            if constexpr (V == 8) gst<uint16_t>(to + 2 * e, (uint16_t)(w[e >> 1] >> (16 * (e & 1))));
+            else gst<uint32_t>(to + 4 * e, w[e]);
+          }
+        }
+      }
+    };
+    if (p.c_bf16) out(IntC<8>());
+    else out(IntC<4>());
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int SLOTS>
+hipError_t launch_tiles(const Q8GemmParams& p, hipStream_t stream) {
+  TileGrid g;
+  g.tiles_m = (int32_t)(((int64_t)p.m + BM - 1) / BM);
+  g.tiles_n = (int32_t)(((int64_t)p.n + BN - 1) / BN);
+  const int64_t total = (int64_t)g.tiles_m * g.tiles_n;
+  if (total > most_groups(64 * WM * WN)) return hipErrorInvalidConfiguration;
+  g.total = (int32_t)total;
+  g.run = g.total / 8;
+  g.rest = g.total % 8;
+  if (p.k % STAGE)
+    hipLaunchKernelGGL((q8_gemm_tile_kernel<BM, BN, WM, WN, SLOTS, true>), dim3(g.total), dim3(64 * WM * WN), 0, stream, p, g);
+  else
+    hipLaunchKernelGGL((q8_gemm_tile_kernel<BM, BN, WM, WN, SLOTS, false>), dim3(g.total), dim3(64 * WM * WN), 0, stream, p, g);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream) {
   const bool aligned = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) |
                          (uint64_t)p.lda | (uint64_t)p.ldb) & 15) == 0;
+  // offsets inside a tile count in 31 bits
+  if (aligned && p.n > 64 && 256 * p.lda < 0x7fffffff && 256 * p.ldb < 0x7fffffff) {
+    const int64_t big = (((int64_t)p.m + 255) / 256) * (((int64_t)p.n + 255) / 256);
+    const int64_t mid = (((int64_t)p.m + 127) / 128) * (((int64_t)p.n + 127) / 128);
+    if (big >= TPP_BIG) return launch_tiles<256, 256, 2, 4, 2>(p, stream);
+    if (mid >= TPP_MID) return launch_tiles<128, 128, 2, 2, 2>(p, stream);
+    return launch_tiles<64, 64, 2, 2, 4>(p, stream);
+  }
   const int64_t rows = ((int64_t)p.m + 63) / 64, cols = ((int64_t)p.n + 63) / 64;
   const int64_t most = most_groups(256) / rows;   // (m below 2^31: at least 1)
   const int64_t ny = cols < most ? cols : most;
