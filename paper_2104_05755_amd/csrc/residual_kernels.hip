@@ -219,13 +219,6 @@ __device__ __forceinline__ void with_vectors(float (&v)[8], int32_t form, const 
   for (int e = 0; e < 8; ++e) v[e] += x[e];
 }
 
-template <int W, int C>
-__device__ __forceinline__ void places(int32_t f, Place (&c)[C]) {
-  const int32_t lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
-#pragma unroll
-  for (int k = 0; k < C; ++k) c[k] = Place((k * W + wave) * 64 + lane, f);
-}
-
 template <bool BF16, int W, int C, bool WHOLE, int HOW>
 __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_row_kernel(ResidualParams p) {
   __shared__ float part[2][2][W];

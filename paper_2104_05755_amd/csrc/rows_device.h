@@ -77,6 +77,18 @@ __device__ __forceinline__ T over_lanes(T v) {
   }
   return v;
 }
+// The same for a number of lanes that only the launch knows.
+template <typename OP, typename T>
+__device__ __forceinline__ T over_lanes(T v, int32_t lanes) {
+  switch (lanes) {
+    case 2: return over_lanes<OP, 2>(v);
+    case 4: return over_lanes<OP, 4>(v);
+    case 8: return over_lanes<OP, 8>(v);
+    case 16: return over_lanes<OP, 16>(v);
+    case 32: return over_lanes<OP, 32>(v);
+  }
+  return over_lanes<OP, 64>(v);
+}
 // op over a workgroup of W wavefronts, in order, in every thread.  `part`: W words of LDS, free again
 // after the next barrier that is not this one's.
 template <typename OP, int W, typename T>
@@ -113,16 +125,19 @@ __device__ __forceinline__ void act_both(float z, int32_t act, float& value, flo
   if (act == TPP_ACT_RELU) {
     value = z > 0.0f ? z : 0.0f;
     slope = z > 0.0f ? 1.0f : 0.0f;
-  } else if (act == TPP_ACT_GELU_TANH) {
-    value = gelu_tanh(z);
-    slope = gelu_tanh_grad(z);
-    slope = z != z ? z : slope;   // (its clamp would drop a NaN)
+  } else if (act == TPP_ACT_GELU_TANH) {   // gelu_tanh and gelu_tanh_grad with one exponential
+    const float x = fminf(fmaxf(z, -9.0f), 9.0f);
+    const float e = __builtin_amdgcn_exp2f(x * __builtin_fmaf(-0.10294324f, x * x, -2.3022082f));
+    const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    value = z * s;
+    slope = s * __builtin_fmaf(1.5957691f * x * (e * s), __builtin_fmaf(0.134145f, x * x, 1.0f), 1.0f);
+    slope = z != z ? z : slope;   // (the clamp drops a NaN)
   } else if (act == TPP_ACT_SILU) {
     const float e = __builtin_amdgcn_exp2f(fminf(z * -1.44269504f, 126.0f));   // 1 - s = e s, finite
     const float s = __builtin_amdgcn_rcpf(1.0f + e);
     value = z * s;
     slope = s + z * (e * s) * s;
-    slope = z != z ? z : slope;
+    slope = z != z ? z : slope;   // (so does the minimum)
   } else {
     value = z;
     slope = 1.0f;
@@ -182,6 +197,14 @@ struct Place {
   }
   __device__ __forceinline__ bool none() const { return skip >= 8; }
 };
+// The chunks of a lane in a row that W wavefronts have, 64 consecutive ones to a wavefront at a time (W 1:
+// every wavefront of the workgroup has a row of its own).
+template <int W, int C>
+__device__ __forceinline__ void places(int32_t f, Place (&c)[C]) {
+  const int32_t lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
+#pragma unroll
+  for (int k = 0; k < C; ++k) c[k] = Place((k * W + wave) * 64 + lane, f);
+}
 
 // How a pass goes through the caches: what is moved once only displaces what may be read again.
 enum { CACHED, STREAM_OUT, STREAM };
