@@ -23,20 +23,11 @@ using namespace rows;
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_a1 __attribute__((ext_vector_type(4), aligned(1)));
 
-// 16 bytes of a row from byte kk on, those behind k zero.  ALIGNED: row and kk at multiples of 16, and the
-// whole chunk is read where its first byte is in the row.
-template <bool ALIGNED>
-__device__ __forceinline__ i32x4_t tail16(const int8_t* row, int32_t kk, int32_t k) {
+// 16 bytes of a row from byte kk on, those from byte k on zero; nothing behind byte k is read.
+__device__ __forceinline__ i32x4_t any16(const int8_t* row, int32_t kk, int32_t k) {
   const int32_t have = k - kk;
   u32x4 w = {0, 0, 0, 0};
-  if constexpr (ALIGNED) {
-    w = gld<u32x4>(row + (have > 0 ? kk : 0));
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      const int32_t n = have - 4 * d;
-      w[d] = n >= 4 ? w[d] : n <= 0 ? 0u : w[d] & ((1u << (8 * n)) - 1);
-    }
-  } else if (have >= 16) {
+  if (have >= 16) {
     w = (u32x4)gld<u32x4_a1>(row + kk);
   } else {
     for (int32_t e = 0; e < have; ++e) {
@@ -46,6 +37,15 @@ __device__ __forceinline__ i32x4_t tail16(const int8_t* row, int32_t kk, int32_t
     }
   }
   return __builtin_bit_cast(i32x4_t, w);
+}
+// The first `have` bytes of 16.
+__device__ __forceinline__ i32x4_t first_bytes(i32x4_t w, int32_t have) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int32_t n = have - 4 * d;
+    w[d] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+  }
+  return w;
 }
 
 // Four channels of one token: scales, bias, activation, rounding and store.
@@ -82,53 +82,161 @@ __device__ __forceinline__ void finish4(const Q8GemmParams& p, i32x4_t acc, int3
   }
 }
 
-// ---- operands straight from memory ----------------------------------------------------------------
-// A workgroup has 16 TM channels of 16 TN tokens; its NW wavefronts take a share of k each, which are added
-// in LDS.
-template <int TM, int TN, int NW, bool ALIGNED>
-__global__ __launch_bounds__(64 * NW) void q8_gemm_direct_kernel(Q8GemmParams p) {
-  __shared__ i32x4_t part[NW][TM * TN][64];
+// A workgroup's wavefronts have each a share of k of its 16 TM x 16 TN tile: the sums of all, and the stores.
+template <int TM, int TN, int NW>
+__device__ __forceinline__ void join(const Q8GemmParams& p, i32x4_t (&part)[NW][TM * TN][64],
+                                     const i32x4_t (&acc)[TM][TN], int32_t i0, int32_t j0, int32_t wave, int32_t lane) {
+#pragma unroll
+  for (int x = 0; x < TM; ++x)
+#pragma unroll
+    for (int y = 0; y < TN; ++y) part[wave][x * TN + y][lane] = acc[x][y];
+  __syncthreads();
+  for (int32_t t = wave; t < TM * TN; t += NW) {
+    i32x4_t sum = part[0][t][lane];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) sum += part[w][t][lane];
+    finish4(p, sum, i0 + 16 * (t / TN) + 4 * (lane >> 4), j0 + 16 * (t % TN) + (lane & 15));
+  }
+  __syncthreads();
+}
+template <int TM, int TN>
+__device__ __forceinline__ void zero(i32x4_t (&acc)[TM][TN]) {
+#pragma unroll
+  for (int x = 0; x < TM; ++x)
+#pragma unroll
+    for (int y = 0; y < TN; ++y) acc[x][y] = (i32x4_t){0, 0, 0, 0};
+}
+
+// ---- rows at any byte -----------------------------------------------------------------------------
+// Fragments straight from memory.
+constexpr int AT = 4, AW = 4;   // 16-row tiles each way, wavefronts
+__global__ __launch_bounds__(64 * AW) void q8_gemm_any_kernel(Q8GemmParams p) {
+  __shared__ i32x4_t part[AW][AT * AT][64];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t i0 = blockIdx.x * 16 * TM, k16 = 16 * (lane >> 4);
-  const int32_t steps = (p.k + 63) / 64;
-  for (int32_t j0 = blockIdx.y * 16 * TN; j0 < p.n; j0 += gridDim.y * 16 * TN) {
-    const int8_t* a[TM];
-    const int8_t* b[TN];
+  const int32_t i0 = blockIdx.x * 16 * AT, steps = (p.k + 63) / 64;
+  for (int64_t j0 = (int64_t)blockIdx.y * 16 * AT; j0 < p.n; j0 += (int64_t)gridDim.y * 16 * AT) {
+    i32x4_t acc[AT][AT];
+    zero(acc);
+    for (int32_t s = wave; s < steps; s += AW) {
+      const int32_t kk = s * 64 + 16 * (lane >> 4);
+      i32x4_t fa[AT], fb[AT];
 #pragma unroll
-    for (int t = 0; t < TM; ++t) a[t] = p.a + (int64_t)min(i0 + 16 * t + (lane & 15), p.m - 1) * p.lda;
+      for (int t = 0; t < AT; ++t) {
+        fa[t] = any16(p.a + (int64_t)min(i0 + 16 * t + (lane & 15), p.m - 1) * p.lda, kk, p.k);
+        fb[t] = any16(p.b + (int64_t)min((int32_t)j0 + 16 * t + (lane & 15), p.n - 1) * p.ldb, kk, p.k);
+      }
 #pragma unroll
-    for (int t = 0; t < TN; ++t) b[t] = p.b + (int64_t)min(j0 + 16 * t + (lane & 15), p.n - 1) * p.ldb;
-    i32x4_t acc[TM][TN];
+      for (int x = 0; x < AT; ++x)
 #pragma unroll
-    for (int x = 0; x < TM; ++x)
-#pragma unroll
-      for (int y = 0; y < TN; ++y) acc[x][y] = (i32x4_t){0, 0, 0, 0};
-    for (int32_t s = wave; s < steps; s += NW) {
-      const int32_t kk = s * 64 + k16;
-      i32x4_t fa[TM], fb[TN];
-#pragma unroll
-      for (int t = 0; t < TM; ++t) fa[t] = tail16<ALIGNED>(a[t], kk, p.k);
-#pragma unroll
-      for (int t = 0; t < TN; ++t) fb[t] = tail16<ALIGNED>(b[t], kk, p.k);
-#pragma unroll
-      for (int x = 0; x < TM; ++x)
-#pragma unroll
-        for (int y = 0; y < TN; ++y)
+        for (int y = 0; y < AT; ++y)
           acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[x], fb[y], acc[x][y], 0, 0, 0);
     }
-#pragma unroll
-    for (int x = 0; x < TM; ++x)
-#pragma unroll
-      for (int y = 0; y < TN; ++y) part[wave][x * TN + y][lane] = acc[x][y];
-    __syncthreads();
-    for (int32_t t = wave; t < TM * TN; t += NW) {
-      i32x4_t sum = part[0][t][lane];
-#pragma unroll
-      for (int w = 1; w < NW; ++w) sum += part[w][t][lane];
-      finish4(p, sum, i0 + 16 * (t / TN) + 4 * (lane >> 4), j0 + 16 * (t % TN) + (lane & 15));
-    }
-    __syncthreads();
+    join<AT, AT, AW>(p, part, acc, i0, (int32_t)j0, wave, lane);
   }
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------
+// Up to 64 tokens: the weights' bytes count.  A workgroup has 16 TM channels and all tokens (16 TN); its NW
+// wavefronts take consecutive stages of k, each with SLOTS places in LDS of its own, so that there is no barrier
+// before the end: copies into a place are issued when its fragments have been read, and waited for by count.
+// (Fragments straight from memory are 16 rows to every 16 lanes, a look-up of a line for every 16 bytes: 16
+// bytes a clock and compute unit, 23.7 us where this takes TODO.)
+constexpr int STAGE = 128;   // bytes of k
+
+template <int N>
+__device__ __forceinline__ void copy_rows(i32x4 from, const uint32_t (&at)[N], uint32_t to) {
+  if constexpr (N == 6) {
+    buffer_load_lds16_block<4>(from, at, to);
+    buffer_load_lds16_block<2>(from, at + 4, to + 4096);
+  } else {
+    buffer_load_lds16_block<N>(from, at, to);
+  }
+}
+
+template <int TM, int TN, int NW, int SLOTS>
+__global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
+  constexpr int A_LOADS = 2 * TM, B_LOADS = 2 * TN, LOADS = A_LOADS + B_LOADS, SLOT = LOADS * 1024;
+  constexpr int RING = NW * SLOTS * SLOT, JOIN = NW * TM * TN * 1024;
+  static_assert(RING <= 160 * 1024 && JOIN <= 160 * 1024, "LDS");
+  static_assert(SLOTS * LOADS <= 64, "vmcnt");
+  __shared__ __attribute__((aligned(1024))) char lds[RING > JOIN ? RING : JOIN];
+  const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t i0 = blockIdx.x * 16 * TM;
+  const int32_t stages = (p.k + STAGE - 1) / STAGE, share = (stages + NW - 1) / NW;
+  const int32_t s0 = min(wave * share, stages), s1 = min(s0 + share, stages);
+  // a lane copies one 16-byte chunk of a row; rows' chunks XOR-swizzled as in the tiles below
+  const int32_t sub = lane >> 3, pos = lane & 7;
+  uint32_t la[A_LOADS], lb[B_LOADS], ta[A_LOADS], tb[B_LOADS];   // t: in a last stage that is not whole
+  const int32_t last0 = (stages - 1) * STAGE;
+  const auto offset = [&](int32_t row, int64_t ld, int32_t rows, uint32_t& whole, uint32_t& tail) {
+    const int32_t c = (pos ^ ((row >> 1) & 7)) * 16;
+    const uint32_t at = (uint32_t)(min(row, rows) * ld);
+    whole = at + c;
+    tail = at + (last0 + c < p.k ? c : 0);
+  };
+#pragma unroll
+  for (int r = 0; r < A_LOADS; ++r) offset(r * 8 + sub, p.lda, p.m - 1 - i0, la[r], ta[r]);
+#pragma unroll
+  for (int r = 0; r < B_LOADS; ++r) offset(r * 8 + sub, p.ldb, p.n - 1, lb[r], tb[r]);
+  const int8_t* base_a = p.a + (int64_t)i0 * p.lda;
+  const uint32_t mine = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_AS char*)lds) + wave * SLOTS * SLOT;
+  const bool ragged = p.k % STAGE != 0;
+  const auto issue = [&](int32_t s, int slot) {
+    const i32x4 ra = raw_buffer(base_a + (int64_t)s * STAGE), rb = raw_buffer(p.b + (int64_t)s * STAGE);
+    const uint32_t to = mine + slot * SLOT;
+    if (ragged && s == stages - 1) {
+      copy_rows(ra, ta, to);
+      copy_rows(rb, tb, to + A_LOADS * 1024);
+    } else {
+      copy_rows(ra, la, to);
+      copy_rows(rb, lb, to + A_LOADS * 1024);
+    }
+  };
+  i32x4_t acc[TM][TN];
+  zero(acc);
+  const int32_t row = lane & 15, q = lane >> 4, swz = (row >> 1) & 7;
+#pragma unroll
+  for (int k = 0; k < SLOTS; ++k)
+    if (s0 + k < s1) issue(s0 + k, k);
+  for (int32_t s = s0; s < s1; s += SLOTS) {
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+      if (s + k >= s1) break;
+      // this stage's copies are done when at most the later ones' are under way
+      if (s + k + SLOTS - 1 < s1) __builtin_amdgcn_s_waitcnt(vmcnt_imm((SLOTS - 1) * LOADS));
+      else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      const char* at = lds + (wave * SLOTS + k) * SLOT;
+      i32x4_t fa[2][TM], fb[2][TN];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int32_t c = row * STAGE + (((4 * h + q) ^ swz) << 4);
+#pragma unroll
+        for (int t = 0; t < TM; ++t) fa[h][t] = *reinterpret_cast<const i32x4_t*>(at + t * 2048 + c);
+#pragma unroll
+        for (int t = 0; t < TN; ++t) fb[h][t] = *reinterpret_cast<const i32x4_t*>(at + A_LOADS * 1024 + t * 2048 + c);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + k + SLOTS < s1) issue(s + k + SLOTS, k);
+      if (ragged && s + k == stages - 1) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int t = 0; t < TN; ++t) fb[h][t] = first_bytes(fb[h][t], p.k - last0 - 64 * h - 16 * q);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+          for (int y = 0; y < TN; ++y)
+            acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[h][x], fb[h][y], acc[x][y], 0, 0, 0);
+    }
+  }
+  __syncthreads();
+  join<TM, TN, NW>(p, *reinterpret_cast<i32x4_t (*)[NW][TM * TN][64]>(lds), acc, i0, 0, wave, lane);
 }
 
 // ---- operands through LDS -------------------------------------------------------------------------
@@ -139,7 +247,6 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_direct_kernel(Q8GemmParams p)
 // across the stages too: the last k-step of a stage comes after the barrier that ends its reading, beside
 // the next stage's first reads and the copies into the place that the barrier freed.
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
-constexpr int STAGE = 128;   // bytes of k
 
 struct TileGrid {
   int32_t tiles_m, tiles_n, total, run, rest;   // tiles of an XCD, XCDs that have one more
@@ -360,28 +467,58 @@ hipError_t launch_tiles(const Q8GemmParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int TM, int TN, int NW, int SLOTS>
+hipError_t launch_few(const Q8GemmParams& p, hipStream_t stream) {
+  const int64_t rows = ((int64_t)p.m + 16 * TM - 1) / (16 * TM);
+  if (rows > most_groups(64 * NW)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((q8_gemm_few_kernel<TM, TN, NW, SLOTS>), dim3((uint32_t)rows), dim3(64 * NW), 0, stream, p);
+  return hipGetLastError();
+}
+#ifndef TPP_F
+#define TPP_F 0
+#endif
+// Channels of a workgroup and its wavefronts: at least 192 workgroups where m has them.
+template <int TN>
+hipError_t launch_few(const Q8GemmParams& p, hipStream_t stream) {
+  if (TPP_F == 1) {
+    if (p.m >= 192 * 64) return launch_few<4, TN, 4, TN <= 1 ? 4 : TN <= 2 ? 3 : 2>(p, stream);
+    return launch_few<1, TN, 8, 2>(p, stream);
+  }
+  if (TPP_F == 2) {
+    if (p.m >= 192 * 32) return launch_few<2, TN, 4, TN <= 2 ? 4 : 3>(p, stream);
+    return launch_few<1, TN, 4, TN <= 2 ? 6 : 4>(p, stream);
+  }
+  if (TPP_F == 3) {
+    if (p.m >= 192 * 32) return launch_few<2, TN, 8, TN <= 2 ? 2 : 1>(p, stream);
+    return launch_few<1, TN, 16, TN == 1 ? 2 : 1>(p, stream);
+  }
+  if (p.m >= 192 * 64) return launch_few<4, TN, 8, TN <= 1 ? 2 : 1>(p, stream);
+  return launch_few<1, TN, 8, TN == 1 ? 4 : TN == 2 ? 3 : 2>(p, stream);
+}
+
 }  // namespace
 
 hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream) {
   const bool aligned = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) |
                          (uint64_t)p.lda | (uint64_t)p.ldb) & 15) == 0;
   // offsets inside a tile count in 31 bits
-  if (aligned && p.n > 64 && 256 * p.lda < 0x7fffffff && 256 * p.ldb < 0x7fffffff) {
-    const int64_t big = (((int64_t)p.m + 255) / 256) * (((int64_t)p.n + 255) / 256);
-    const int64_t mid = (((int64_t)p.m + 127) / 128) * (((int64_t)p.n + 127) / 128);
-    if (big >= TPP_BIG) return launch_tiles<256, 256, 2, 4, 2>(p, stream);
-    if (mid >= TPP_MID) return launch_tiles<128, 128, 2, 2, 2>(p, stream);
-    return launch_tiles<64, 64, 2, 2, 4>(p, stream);
+  if (!aligned || p.lda > 0x7fffffff / 256 || p.ldb > 0x7fffffff / 256) {
+    const int64_t rows = ((int64_t)p.m + 16 * AT - 1) / (16 * AT), cols = ((int64_t)p.n + 16 * AT - 1) / (16 * AT);
+    const int64_t most = most_groups(64 * AW) / rows, ny = cols < most ? cols : most;
+    if (most < 1) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(q8_gemm_any_kernel, dim3((uint32_t)rows, (uint32_t)(ny < 65535 ? ny : 65535)), dim3(64 * AW), 0,
+                       stream, p);
+    return hipGetLastError();
   }
-  const int64_t rows = ((int64_t)p.m + 63) / 64, cols = ((int64_t)p.n + 63) / 64;
-  const int64_t most = most_groups(256) / rows;   // (m below 2^31: at least 1)
-  const int64_t ny = cols < most ? cols : most;
-  const dim3 grid((uint32_t)rows, (uint32_t)(ny < 65535 ? ny : 65535));
-  if (aligned)
-    hipLaunchKernelGGL((q8_gemm_direct_kernel<4, 4, 4, true>), grid, dim3(256), 0, stream, p);
-  else
-    hipLaunchKernelGGL((q8_gemm_direct_kernel<4, 4, 4, false>), grid, dim3(256), 0, stream, p);
-  return hipGetLastError();
+  if (p.n <= 16) return launch_few<1>(p, stream);
+  if (p.n <= 32) return launch_few<2>(p, stream);
+  if (p.n <= 48) return launch_few<3>(p, stream);
+  if (p.n <= 64) return launch_few<4>(p, stream);
+  const int64_t big = (((int64_t)p.m + 255) / 256) * (((int64_t)p.n + 255) / 256);
+  const int64_t mid = (((int64_t)p.m + 127) / 128) * (((int64_t)p.n + 127) / 128);
+  if (big >= TPP_BIG) return launch_tiles<256, 256, 2, 4, 2>(p, stream);
+  if (mid >= TPP_MID) return launch_tiles<128, 128, 2, 2, 2>(p, stream);
+  return launch_tiles<64, 64, 2, 2, 4>(p, stream);
 }
 
 }  // namespace tpp

@@ -122,12 +122,6 @@ __device__ __forceinline__ void tops_of(const Q8Params& p, uint32_t (&top)[C], u
 #pragma unroll
   for (int k = 0; k < C; ++k) top[k] = all;
 }
-__device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = Top::join(top, magnitude(v[e]));
-  return top;
-}
 // Chunk c in 8 bits, and its group's scale by the lane that has the group's first chunk.  The chunk is number
 // `chunk` of the row, which starts `from` entries before the chunks are counted (the second half of a gated row).
 template <bool WHOLE>
@@ -179,13 +173,15 @@ __global__ __launch_bounds__(W == 1 ? QT : 64 * W) void q8_row_kernel(Q8Params p
           if (two) h[e] *= u[k][e];
         }
         const Raw<BF16> r = narrow<BF16>(h);
-        if constexpr (KIND == QUANTIZE)
+        if constexpr (KIND == QUANTIZE) {
+          ar[k] = r;
           widen<BF16>(r, v[k]);
-        else
+        } else {
           store_raw<BF16, WHOLE, OUT>(p.h, t * p.ldh, c[k], r);
+        }
       }
-      top[k] = top8(v[k]);
-      if (KIND == HALVES) top_u[k] = top8(u[k]);
+      top[k] = top8<BF16>(ar[k]);
+      if (KIND == HALVES) top_u[k] = top8<BF16>(ur[k]);
     }
     if (KIND == HALVES && !p.group) {
 #pragma unroll
@@ -218,8 +214,8 @@ __global__ __launch_bounds__(W == 1 ? QT : 64 * W) void q8_row_kernel(Q8Params p
 }
 
 // ---- backward -----------------------------------------------------------------------------------
-// No sum over a row is needed: a wavefront has 512 entries of h (and the same of the other half) of the tokens
-// of its part, U tokens' loads in flight, and keeps their sums of dz.
+// No sum over a row is needed: a workgroup has 512 entries of h (and the same of the other half) of the tokens
+// of its part, its four wavefronts the tokens in turn, U of them in flight, and keeps their sums of dz.
 template <int N>
 __device__ __forceinline__ void dequantize(const int8_t* q, const float* s, int32_t group, int32_t at, float (&v)[N]) {
   const u32x2_a1 w = gld<u32x2_a1>(q + at);
@@ -232,13 +228,14 @@ __device__ __forceinline__ void dequantize(const int8_t* q, const float* s, int3
 }
 
 template <bool BF16, bool WHOLE, int HOW, bool GATED>
-__global__ __launch_bounds__(64) void q8_backward_kernel(Q8Params p, int64_t take, float* part) {
+__global__ __launch_bounds__(QT) void q8_backward_kernel(Q8Params p, int64_t take, float* part) {
   constexpr int U = 2;
-  const Place c(blockIdx.x * 64 + threadIdx.x, p.f);
-  if (c.none()) return;
+  __shared__ float joined[QW - 1][GATED ? 16 : 8][64];
+  const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const Place c(blockIdx.x * 64 + lane, p.f);
   float da[8] = {}, du[8] = {};
   const int64_t end = min((blockIdx.y + 1) * take, p.tokens);
-  for (int64_t t0 = blockIdx.y * take; t0 < end; t0 += U) {
+  for (int64_t t0 = blockIdx.y * take + wave * U; t0 < end; t0 += QW * U) {
     Raw<BF16> gr[U];
     float a[U][8], u[U][8];
 #pragma unroll
@@ -275,6 +272,22 @@ __global__ __launch_bounds__(64) void q8_backward_kernel(Q8Params p, int64_t tak
     }
   }
   if (!part) return;
+  if (wave > 0) {   // the four wavefronts' sums, in order
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      joined[wave - 1][e][lane] = da[e];
+      if (GATED) joined[wave - 1][8 + e][lane] = du[e];
+    }
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < QW - 1; ++w)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      da[e] += joined[w][e][lane];
+      if (GATED) du[e] += joined[w][8 + e][lane];
+    }
   const int64_t row = (int64_t)blockIdx.y * (GATED ? 2 * p.f : p.f);
   store_raw<false, WHOLE, CACHED>(part, row, c, narrow<false>(da));
   if (GATED) store_raw<false, WHOLE, CACHED>(part, row + p.f, c, narrow<false>(du));
@@ -284,15 +297,13 @@ __global__ __launch_bounds__(64) void q8_backward_kernel(Q8Params p, int64_t tak
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// The backward pass' parts of dbias: `take` tokens each; 4096 wavefronts, at least 4 tokens each.
+// The backward pass' parts of dbias: `take` tokens each; 1024 workgroups, at least 8 tokens each.
 struct BackPlan {
   int64_t take, parts;
   explicit BackPlan(const Q8Params& p) {
     const int64_t slabs = ceil_div(p.f, 512);
-    int64_t want = 4096 / slabs;
-    if (want > 1024) want = 1024;
-    if (want < 64) want = 64;
-    take = ceil_div(p.tokens, min64(want, ceil_div(p.tokens, 4)));
+    const int64_t want = 1024 / slabs;
+    take = ceil_div(p.tokens, min64(want < 64 ? 64 : want, ceil_div(p.tokens, 8)));
     parts = ceil_div(p.tokens, take);
   }
 };
@@ -387,7 +398,7 @@ hipError_t launch_q8_act_backward(const Q8Params& p, float* work, hipStream_t st
         const auto launch = [&](auto gated) {
           hipLaunchKernelGGL((q8_backward_kernel<decltype(bf16)::value, decltype(whole)::value, decltype(how)::value,
                                                  decltype(gated)::value>),
-                             grid, dim3(64), 0, stream, p, b.take, part);
+                             grid, dim3(QT), 0, stream, p, b.take, part);
         };
         if (p.gated) launch(std::true_type());
         else launch(std::false_type());

@@ -270,8 +270,7 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_row_kernel(Resi
       if (p.y) store_raw<BF16, WHOLE, HOW>(p.y, t * p.ldy, c[k], y);
       mask<WHOLE>(c[k], y);
       widen<BF16>(y, v[k]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = Top::join(top, magnitude(v[k][e]));
+      top = Top::join(top, top8<BF16>(y));
     }
     if (p.q) {
       const Q8Group g = q8_group(over_group<Top, W>(top, tops));

@@ -155,7 +155,8 @@ __device__ __forceinline__ Q8Group q8_group(uint32_t top_bits) {
   Q8Group g;
   const float top = __uint_as_float(top_bits);
   if (top_bits >= 0x7f800000u) {   // an infinity or NaN: q = 0, scale NaN
-    g.top = g.pre = g.inv = 0.0f;
+    g.top = g.inv = 0.0f;
+    g.pre = 1.0f;
     g.scale = __uint_as_float(0x7fc00000u);
     return g;
   }
@@ -165,21 +166,50 @@ __device__ __forceinline__ Q8Group q8_group(uint32_t top_bits) {
   g.scale = top / 127.0f;
   return g;
 }
-// The whole number nearest to 127 v / top, ties to even.  t = v * (127 / top) is off by less than 3e-5
-// (|t| <= 127, two roundings of 2^-24): only a t that near to k + 1/2 can round to the wrong side, and
-// there 127 |v| is compared with (k + 1/2) top, both exact in 64 bits.
-__device__ __forceinline__ int32_t q8_round(float v, const Q8Group& g) {
-  const float t = v * g.pre * g.inv;
-  float k = __builtin_rintf(t);
-  const float d = t - k;
-  if (__builtin_fabsf(d) > 0.5f - 3e-5f) {
-    const float half = __builtin_fabsf(k + (d > 0.0f ? 0.5f : -0.5f)), low = half - 0.5f;
-    const double a = 127.0 * (double)__builtin_fabsf(v), b = (double)half * (double)g.top;
-    const float even = ((int32_t)low & 1) ? low + 1.0f : low;
-    const float m = a < b ? low : a > b ? low + 1.0f : even;
-    k = v < 0.0f ? -m : m;
+// The whole number nearest to 127 v / top, ties to even, decided exactly: 127 |v| is compared with (k + 1/2) top,
+// both exact in 64 bits, for the half k + 1/2 next to t, which is off by little.
+__device__ __forceinline__ int32_t q8_exact(float v, float t, const Q8Group& g) {
+  const float k = __builtin_rintf(t);
+  const float half = __builtin_fabsf(k + (t > k ? 0.5f : -0.5f)), low = half - 0.5f;
+  const double a = 127.0 * (double)__builtin_fabsf(v), b = (double)half * (double)g.top;
+  const float even = ((int32_t)low & 1) ? low + 1.0f : low;
+  const float m = a < b ? low : a > b ? low + 1.0f : even;
+  return (int32_t)(v < 0.0f ? -m : m);
+}
+// Eight entries.  t = v * (127 / top) is off by less than 3e-5 (|t| <= 127, two roundings of 2^-24): only a t
+// that near to k + 1/2 can round to the wrong side.  Adding 1.5 * 2^23 rounds t and leaves the number in the
+// low byte.
+__device__ __forceinline__ u32x2 q8_round(const float (&v)[8], const Q8Group& g) {
+  constexpr float M = 12582912.0f;
+  float t[8], m[8], off = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t[e] = v[e] * g.inv;
+  if (g.pre != 1.0f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = v[e] * g.pre * g.inv;
   }
-  return k == k ? (int32_t)k : 0;   // (NaN: an entry of a group without a scale)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    m[e] = t[e] + M;
+    off = __builtin_fmaxf(off, __builtin_fabsf(t[e] - (m[e] - M)));
+  }
+  if (off > 0.5f - 3e-5f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (__builtin_fabsf(t[e] - (m[e] - M)) > 0.5f - 3e-5f) m[e] = M + (float)q8_exact(v[e], t[e], g);
+  }
+  u32x2 w;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(m[4 * h + 1]), __float_as_uint(m[4 * h]), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(m[4 * h + 3]), __float_as_uint(m[4 * h + 2]), 0x04000c0cu);
+    w[h] = g.inv > 0.0f ? lo | hi : 0u;   // (a group of zeros, or without a scale)
+  }
+  return w;
+}
+__device__ __forceinline__ int32_t q8_round(float v, const Q8Group& g) {
+  const float x[8] = {v, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  return (int8_t)(q8_round(x, g)[0] & 0xffu);
 }
 
 // ---- chunks of eight entries --------------------------------------------------------------------
@@ -256,6 +286,22 @@ __device__ __forceinline__ void mask(const Place& c, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = (WHOLE ? c.skip != 0 : e < c.skip) ? 0.0f : v[e];
 }
+// The largest magnitude of a chunk.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <bool BF16>
+__device__ __forceinline__ uint32_t top8(const Raw<BF16>& r) {
+  if constexpr (BF16) {
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, r.w[0][i] & 0x7fff7fffu));
+    return (uint32_t)(top.x > top.y ? top.x : top.y) << 16;
+  } else {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = Top::join(top, r.w[i / 4][i % 4] & 0x7fffffffu);
+    return top;
+  }
+}
 __device__ __forceinline__ void load8(const float* p, int32_t at, float (&v)[8]) {
   widen<false>(load_raw<false, CACHED>(p, at), v);
 }
@@ -304,9 +350,7 @@ __device__ __forceinline__ void store_raw(void* p, int64_t row, const Place& c, 
 template <bool WHOLE>
 __device__ __forceinline__ void store_q8(int8_t* row, const Place& c, const float (&v)[8], const Q8Group& g) {
   if (c.none()) return;
-  uint32_t w[2] = {0, 0};
-#pragma unroll
-  for (int e = 0; e < 8; ++e) w[e / 4] |= ((uint32_t)q8_round(v[e], g) & 0xffu) << (8 * (e % 4));
+  const u32x2 w = q8_round(v, g);
   if (c.skip == 0) {
     gst<u32x2_a1>(row + c.at, (u32x2_a1){w[0], w[1]});
   } else if (!WHOLE) {
