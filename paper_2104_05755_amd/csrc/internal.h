@@ -391,12 +391,16 @@ hipError_t launch_q8_act_backward(const Q8Params& p, float* work, hipStream_t st
 struct Q8GemmParams {
   const int8_t *a, *b;
   const float *sa, *sb, *bias;
+  const void* x;   // instead of b and sb: activations, ldb apart
   void* c;
   int64_t lda, ldb, ldc;
   int32_t m, n, k, c_bf16;
   uint32_t flags;
 };
 hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream);
+// Few tokens' activations are turned into 8-bit rows by the product itself.
+bool q8_linear_at_once(const Q8GemmParams& p);
+hipError_t launch_q8_linear_at_once(const Q8GemmParams& p, bool bf16, hipStream_t stream);
 
 // out = the sum over `parts` rows of `width` floats, for each of `n` outputs of its own (fold_kernels in
 // residual_kernels.hip).

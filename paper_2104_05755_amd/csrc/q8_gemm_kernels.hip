@@ -49,9 +49,8 @@ __device__ __forceinline__ i32x4_t first_bytes(i32x4_t w, int32_t have) {
 }
 
 // Four channels of one token: scales, bias, activation, rounding and store.
-__device__ __forceinline__ void finish4(const Q8GemmParams& p, i32x4_t acc, int32_t i, int32_t j) {
+__device__ __forceinline__ void finish4(const Q8GemmParams& p, i32x4_t acc, int32_t i, int32_t j, float sb) {
   if (j >= p.n || i >= p.m) return;
-  const float sb = gld<float>(p.sb + j);
   float v[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -83,9 +82,10 @@ __device__ __forceinline__ void finish4(const Q8GemmParams& p, i32x4_t acc, int3
 }
 
 // A workgroup's wavefronts have each a share of k of its 16 TM x 16 TN tile: the sums of all, and the stores.
-template <int TM, int TN, int NW>
+template <int TM, int TN, int NW, typename F>
 __device__ __forceinline__ void join(const Q8GemmParams& p, i32x4_t (&part)[NW][TM * TN][64],
-                                     const i32x4_t (&acc)[TM][TN], int32_t i0, int32_t j0, int32_t wave, int32_t lane) {
+                                     const i32x4_t (&acc)[TM][TN], int32_t i0, int32_t j0, int32_t wave, int32_t lane,
+                                     const F& scale) {
 #pragma unroll
   for (int x = 0; x < TM; ++x)
 #pragma unroll
@@ -95,7 +95,8 @@ __device__ __forceinline__ void join(const Q8GemmParams& p, i32x4_t (&part)[NW][
     i32x4_t sum = part[0][t][lane];
 #pragma unroll
     for (int w = 1; w < NW; ++w) sum += part[w][t][lane];
-    finish4(p, sum, i0 + 16 * (t / TN) + 4 * (lane >> 4), j0 + 16 * (t % TN) + (lane & 15));
+    const int32_t j = j0 + 16 * (t % TN) + (lane & 15);
+    finish4(p, sum, i0 + 16 * (t / TN) + 4 * (lane >> 4), j, scale(min(j, p.n - 1)));
   }
   __syncthreads();
 }
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(64 * AW) void q8_gemm_any_kernel(Q8GemmParams p) {
         for (int y = 0; y < AT; ++y)
           acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[x], fb[y], acc[x][y], 0, 0, 0);
     }
-    join<AT, AT, AW>(p, part, acc, i0, (int32_t)j0, wave, lane);
+    join<AT, AT, AW>(p, part, acc, i0, (int32_t)j0, wave, lane, [&](int32_t j) { return gld<float>(p.sb + j); });
   }
 }
 
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(64 * AW) void q8_gemm_any_kernel(Q8GemmParams p) {
 constexpr int STAGE = 128;   // bytes of k
 
 template <int N>
-__device__ __forceinline__ void copy_rows(i32x4 from, const uint32_t (&at)[N], uint32_t to) {
+__device__ __forceinline__ void copy_rows(i32x4 from, const uint32_t* at, uint32_t to) {
   if constexpr (N == 6) {
     buffer_load_lds16_block<4>(from, at, to);
     buffer_load_lds16_block<2>(from, at + 4, to + 4096);
@@ -153,20 +154,28 @@ __device__ __forceinline__ void copy_rows(i32x4 from, const uint32_t (&at)[N], u
   }
 }
 
-template <int TM, int TN, int NW, int SLOTS>
+// OWN: the tokens are activations x, few enough (OWN_BYTES with k rounded up to whole stages) that each
+// workgroup makes their 8-bit rows itself, in LDS, beside the first weights: one launch for two.
+enum { ROWS8, OWN_F32, OWN_BF16 };
+constexpr int OWN_BYTES = 12288;
+template <int TM, int TN, int NW, int SLOTS, int FROM>
 __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
-  constexpr int A_LOADS = 2 * TM, B_LOADS = 2 * TN, LOADS = A_LOADS + B_LOADS, SLOT = LOADS * 1024;
+  constexpr bool OWN = FROM != ROWS8;
+  constexpr int A_LOADS = 2 * TM, B_LOADS = OWN ? 0 : 2 * TN, LOADS = A_LOADS + B_LOADS, SLOT = LOADS * 1024;
   constexpr int RING = NW * SLOTS * SLOT, JOIN = NW * TM * TN * 1024;
+  static_assert(!OWN || TN == 1, "up to 16 tokens");
   static_assert(RING <= 160 * 1024 && JOIN <= 160 * 1024, "LDS");
   static_assert(SLOTS * LOADS <= 64, "vmcnt");
   __shared__ __attribute__((aligned(1024))) char lds[RING > JOIN ? RING : JOIN];
+  __shared__ __attribute__((aligned(16))) char own[OWN ? OWN_BYTES : 16];
+  __shared__ uint32_t tops[16];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t i0 = blockIdx.x * 16 * TM;
   const int32_t stages = (p.k + STAGE - 1) / STAGE, share = (stages + NW - 1) / NW;
   const int32_t s0 = min(wave * share, stages), s1 = min(s0 + share, stages);
   // a lane copies one 16-byte chunk of a row; rows' chunks XOR-swizzled as in the tiles below
   const int32_t sub = lane >> 3, pos = lane & 7;
-  uint32_t la[A_LOADS], lb[B_LOADS], ta[A_LOADS], tb[B_LOADS];   // t: in a last stage that is not whole
+  uint32_t la[A_LOADS], lb[B_LOADS + 1], ta[A_LOADS], tb[B_LOADS + 1];   // t: in a last stage that is not whole
   const int32_t last0 = (stages - 1) * STAGE;
   const auto offset = [&](int32_t row, int64_t ld, int32_t rows, uint32_t& whole, uint32_t& tail) {
     const int32_t c = (pos ^ ((row >> 1) & 7)) * 16;
@@ -182,14 +191,14 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
   const uint32_t mine = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_AS char*)lds) + wave * SLOTS * SLOT;
   const bool ragged = p.k % STAGE != 0;
   const auto issue = [&](int32_t s, int slot) {
-    const i32x4 ra = raw_buffer(base_a + (int64_t)s * STAGE), rb = raw_buffer(p.b + (int64_t)s * STAGE);
+    const i32x4 ra = raw_buffer(base_a + (int64_t)s * STAGE);
     const uint32_t to = mine + slot * SLOT;
-    if (ragged && s == stages - 1) {
-      copy_rows(ra, ta, to);
-      copy_rows(rb, tb, to + A_LOADS * 1024);
-    } else {
-      copy_rows(ra, la, to);
-      copy_rows(rb, lb, to + A_LOADS * 1024);
+    if (ragged && s == stages - 1) copy_rows<A_LOADS>(ra, ta, to);
+    else copy_rows<A_LOADS>(ra, la, to);
+    if constexpr (!OWN) {
+      const i32x4 rb = raw_buffer(p.b + (int64_t)s * STAGE);
+      if (ragged && s == stages - 1) copy_rows<B_LOADS>(rb, tb, to + A_LOADS * 1024);
+      else copy_rows<B_LOADS>(rb, lb, to + A_LOADS * 1024);
     }
   };
   i32x4_t acc[TM][TN];
@@ -198,6 +207,42 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
 #pragma unroll
   for (int k = 0; k < SLOTS; ++k)
     if (s0 + k < s1) issue(s0 + k, k);
+  const int32_t pitch = stages * STAGE;
+  if constexpr (OWN) {
+    constexpr bool BF16 = FROM == OWN_BF16;
+    constexpr int C = OWN_BYTES / 8 / (64 * NW);   // chunks of 8 entries of a thread
+    const int32_t chunks = pitch / 8;
+    float v[C][8];
+    if (threadIdx.x < 16) tops[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int32_t at = c * 64 * NW + threadIdx.x, j = at / chunks, e0 = (at - j * chunks) * 8;
+      uint32_t top = 0;
+      if (j < p.n) {
+        const int64_t x = (int64_t)j * p.ldb + e0;
+        if (e0 + 8 <= p.k) {
+          widen<BF16>(load_raw<BF16, CACHED>(p.x, x), v[c]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[c][e] = e0 + e < p.k ? load1<BF16>(p.x, x + e) : 0.0f;
+        }
+        top = top8<BF16>(narrow<BF16>(v[c]));
+      }
+      top = over_lanes<Top, 16>(top);   // (a row's chunks are a multiple of 16)
+      if ((lane & 15) == 0 && j < p.n) atomicMax(&tops[j], top);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int32_t at = c * 64 * NW + threadIdx.x, j = at / chunks, ch = at - j * chunks;
+      if (j >= p.n) continue;
+      const int32_t place = ((ch >> 1) & 7) ^ ((j >> 1) & 7);
+      *reinterpret_cast<u32x2*>(own + j * pitch + (ch >> 4) * STAGE + place * 16 + (ch & 1) * 8) =
+          q8_round(v[c], q8_group(tops[j]));
+    }
+    __syncthreads();
+  }
   for (int32_t s = s0; s < s1; s += SLOTS) {
 #pragma unroll
     for (int k = 0; k < SLOTS; ++k) {
@@ -212,15 +257,22 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int32_t c = row * STAGE + (((4 * h + q) ^ swz) << 4);
+        if constexpr (OWN) {
+          const int32_t j = min(row, p.n - 1);
+          fb[h][0] = *reinterpret_cast<const i32x4_t*>(own + j * pitch + (s + k) * STAGE +
+                                                       (((4 * h + q) ^ ((j >> 1) & 7)) << 4));
+        }
 #pragma unroll
         for (int t = 0; t < TM; ++t) fa[h][t] = *reinterpret_cast<const i32x4_t*>(at + t * 2048 + c);
+        if constexpr (!OWN) {
 #pragma unroll
-        for (int t = 0; t < TN; ++t) fb[h][t] = *reinterpret_cast<const i32x4_t*>(at + A_LOADS * 1024 + t * 2048 + c);
+          for (int t = 0; t < TN; ++t) fb[h][t] = *reinterpret_cast<const i32x4_t*>(at + A_LOADS * 1024 + t * 2048 + c);
+        }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
       if (s + k + SLOTS < s1) issue(s + k + SLOTS, k);
-      if (ragged && s + k == stages - 1) {
+      if (!OWN && ragged && s + k == stages - 1) {   // (rows made here are zero behind k)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -236,7 +288,8 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
     }
   }
   __syncthreads();
-  join<TM, TN, NW>(p, *reinterpret_cast<i32x4_t (*)[NW][TM * TN][64]>(lds), acc, i0, 0, wave, lane);
+  join<TM, TN, NW>(p, *reinterpret_cast<i32x4_t (*)[NW][TM * TN][64]>(lds), acc, i0, 0, wave, lane,
+                   [&](int32_t j) { return OWN ? q8_group(tops[j]).scale : gld<float>(p.sb + j); });
 }
 
 // ---- operands through LDS -------------------------------------------------------------------------
@@ -297,27 +350,37 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_ti
   const int8_t* base_a = p.a + (int64_t)i0 * p.lda;
   const int8_t* base_b = p.b + (int64_t)j0 * p.ldb;
   const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_AS char*)lds);
-  const auto issue = [&](int32_t s) {
+  // its copies of stage s: of A, of B
+  const auto issue_a = [&](int32_t s) {
     const int32_t k0 = s * STAGE;
-    const uint32_t to = lds_at + (uint32_t)(s % SLOTS) * SLOT;
-    const i32x4 ra = raw_buffer(base_a + k0), rb = raw_buffer(base_b + k0);
+    const i32x4 from = raw_buffer(base_a + k0);
+    const uint32_t to = lds_at + (uint32_t)(s % SLOTS) * SLOT + wave * A_LOADS * 1024;
     if (TAIL && k0 + STAGE > p.k) {   // chunks behind k: the stage's first (the products mask them)
-      uint32_t ta[A_LOADS], tb[B_LOADS];
+      uint32_t at[A_LOADS];
 #pragma unroll
       for (int r = 0; r < A_LOADS; ++r) {
         const int32_t c = chunk_at((wave * A_LOADS + r) * 8 + sub) * 16;
-        ta[r] = k0 + c < p.k ? la[r] : la[r] - c;
+        at[r] = k0 + c < p.k ? la[r] : la[r] - c;
       }
+      buffer_load_lds16_block<A_LOADS>(from, at, to);
+    } else {
+      buffer_load_lds16_block<A_LOADS>(from, la, to);
+    }
+  };
+  const auto issue_b = [&](int32_t s) {
+    const int32_t k0 = s * STAGE;
+    const i32x4 from = raw_buffer(base_b + k0);
+    const uint32_t to = lds_at + (uint32_t)(s % SLOTS) * SLOT + A_BYTES + wave * B_LOADS * 1024;
+    if (TAIL && k0 + STAGE > p.k) {
+      uint32_t at[B_LOADS];
 #pragma unroll
       for (int r = 0; r < B_LOADS; ++r) {
         const int32_t c = chunk_at((wave * B_LOADS + r) * 8 + sub) * 16;
-        tb[r] = k0 + c < p.k ? lb[r] : lb[r] - c;
+        at[r] = k0 + c < p.k ? lb[r] : lb[r] - c;
       }
-      buffer_load_lds16_block<A_LOADS>(ra, ta, to + wave * A_LOADS * 1024);
-      buffer_load_lds16_block<B_LOADS>(rb, tb, to + A_BYTES + wave * B_LOADS * 1024);
+      buffer_load_lds16_block<B_LOADS>(from, at, to);
     } else {
-      buffer_load_lds16_block<A_LOADS>(ra, la, to + wave * A_LOADS * 1024);
-      buffer_load_lds16_block<B_LOADS>(rb, lb, to + A_BYTES + wave * B_LOADS * 1024);
+      buffer_load_lds16_block<B_LOADS>(from, lb, to);
     }
   };
   // this wavefront's copies of all but the newest `later` stages are done
@@ -362,7 +425,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_ti
       for (int y = 0; y < TN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[x], fb[y], acc[x][y], 0, 0, 0);
   };
 
-  for (int32_t s = 0; s < SLOTS && s < stages; ++s) issue(s);
+  for (int32_t s = 0; s < SLOTS && s < stages; ++s) {
+    issue_a(s);
+    issue_b(s);
+  }
   landed(min(stages, SLOTS) - 1);
   lds_barrier();
   i32x4_t fa[2][TM], fb[2][TN];
@@ -371,6 +437,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_ti
 #pragma unroll
     for (int kq = 0; kq + 1 < KQ; ++kq) {
       read(s, kq + 1, fa[(kq + 1) & 1], fb[(kq + 1) & 1]);
+      if (kq == 0 && s > 0 && s - 1 + SLOTS < stages) issue_b(s - 1 + SLOTS);
       __builtin_amdgcn_sched_barrier(0);   // the reads stay ahead of the products
       multiply(s, kq, fa[kq & 1], fb[kq & 1]);
       __builtin_amdgcn_sched_barrier(0);
@@ -379,7 +446,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_ti
       landed(min(stages - 2 - s, SLOTS - 2));
       lds_barrier();   // every wavefront has read all of stage s, and stage s + 1 is there
       read(s + 1, 0, fa[0], fb[0]);
-      if (s + SLOTS < stages) issue(s + SLOTS);
+      if (s + SLOTS < stages) issue_a(s + SLOTS);
       __builtin_amdgcn_sched_barrier(0);
     }
     multiply(s, KQ - 1, fa[(KQ - 1) & 1], fb[(KQ - 1) & 1]);
@@ -467,42 +534,44 @@ hipError_t launch_tiles(const Q8GemmParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int TM, int TN, int NW, int SLOTS>
+template <int TM, int TN, int NW, int SLOTS, int FROM = ROWS8>
 hipError_t launch_few(const Q8GemmParams& p, hipStream_t stream) {
   const int64_t rows = ((int64_t)p.m + 16 * TM - 1) / (16 * TM);
   if (rows > most_groups(64 * NW)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((q8_gemm_few_kernel<TM, TN, NW, SLOTS>), dim3((uint32_t)rows), dim3(64 * NW), 0, stream, p);
+  hipLaunchKernelGGL((q8_gemm_few_kernel<TM, TN, NW, SLOTS, FROM>), dim3((uint32_t)rows), dim3(64 * NW), 0, stream, p);
   return hipGetLastError();
 }
-#ifndef TPP_F
-#define TPP_F 0
-#endif
-// Channels of a workgroup and its wavefronts: at least 192 workgroups where m has them.
+// Channels of a workgroup, its wavefronts and their places: 32 channels where m has 192 workgroups of them
+// (48 tokens, 16384 channels of 1024: 11.0 us against 12.1 with 64 and 13.4 with 16), else 16; two workgroups
+// to a compute unit where the places leave room (one token, 16384 channels of 8192: 29.3 against 33.8).
 template <int TN>
 hipError_t launch_few(const Q8GemmParams& p, hipStream_t stream) {
-  if (TPP_F == 1) {
-    if (p.m >= 192 * 64) return launch_few<4, TN, 4, TN <= 1 ? 4 : TN <= 2 ? 3 : 2>(p, stream);
-    return launch_few<1, TN, 8, 2>(p, stream);
-  }
-  if (TPP_F == 2) {
-    if (p.m >= 192 * 32) return launch_few<2, TN, 4, TN <= 2 ? 4 : 3>(p, stream);
-    return launch_few<1, TN, 4, TN <= 2 ? 6 : 4>(p, stream);
-  }
-  if (TPP_F == 3) {
-    if (p.m >= 192 * 32) return launch_few<2, TN, 8, TN <= 2 ? 2 : 1>(p, stream);
-    return launch_few<1, TN, 16, TN == 1 ? 2 : 1>(p, stream);
-  }
-  if (p.m >= 192 * 64) return launch_few<4, TN, 8, TN <= 1 ? 2 : 1>(p, stream);
-  return launch_few<1, TN, 8, TN == 1 ? 4 : TN == 2 ? 3 : 2>(p, stream);
+  if (p.m >= 192 * 32) return launch_few<2, TN, TN <= 2 ? 4 : 8, TN <= 2 ? 2 : 1>(p, stream);
+  return launch_few<1, TN, 8, 1>(p, stream);
+}
+template <int FROM>
+hipError_t launch_own(const Q8GemmParams& p, hipStream_t stream) {
+  if (p.m >= 192 * 32) return launch_few<2, 1, 8, 1, FROM>(p, stream);
+  return launch_few<1, 1, 8, 2, FROM>(p, stream);
+}
+// Whether the kernels that copy rows into LDS can take the weights (tokens): 16-byte chunks, and offsets inside
+// a tile that count in 31 bits.
+bool copied(const int8_t* rows, int64_t ld) {
+  return ((reinterpret_cast<uintptr_t>(rows) | (uint64_t)ld) & 15) == 0 && ld <= 0x7fffffff / 256;
 }
 
 }  // namespace
 
+bool q8_linear_at_once(const Q8GemmParams& p) {
+  return p.n <= 16 && copied(p.a, p.lda) && (int64_t)p.n * ((p.k + STAGE - 1) / STAGE * STAGE) <= OWN_BYTES;
+}
+
+hipError_t launch_q8_linear_at_once(const Q8GemmParams& p, bool bf16, hipStream_t stream) {
+  return bf16 ? launch_own<OWN_BF16>(p, stream) : launch_own<OWN_F32>(p, stream);
+}
+
 hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream) {
-  const bool aligned = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) |
-                         (uint64_t)p.lda | (uint64_t)p.ldb) & 15) == 0;
-  // offsets inside a tile count in 31 bits
-  if (!aligned || p.lda > 0x7fffffff / 256 || p.ldb > 0x7fffffff / 256) {
+  if (!copied(p.a, p.lda) || !copied(p.b, p.ldb)) {
     const int64_t rows = ((int64_t)p.m + 16 * AT - 1) / (16 * AT), cols = ((int64_t)p.n + 16 * AT - 1) / (16 * AT);
     const int64_t most = most_groups(64 * AW) / rows, ny = cols < most ? cols : most;
     if (most < 1) return hipErrorInvalidConfiguration;
@@ -516,7 +585,7 @@ hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream) {
   if (p.n <= 64) return launch_few<4>(p, stream);
   const int64_t big = (((int64_t)p.m + 255) / 256) * (((int64_t)p.n + 255) / 256);
   const int64_t mid = (((int64_t)p.m + 127) / 128) * (((int64_t)p.n + 127) / 128);
-  if (big >= TPP_BIG) return launch_tiles<256, 256, 2, 4, 2>(p, stream);
+    if (big >= TPP_BIG) return launch_tiles<256, 256, 4, 4, 2>(p, stream);
   if (mid >= TPP_MID) return launch_tiles<128, 128, 2, 2, 2>(p, stream);
   return launch_tiles<64, 64, 2, 2, 4>(p, stream);
 }

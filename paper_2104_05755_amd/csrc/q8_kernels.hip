@@ -140,7 +140,7 @@ enum { QUANTIZE, PLAIN, HALVES, SPLIT };
 template <bool BF16, int W, int C, bool WHOLE, int HOW, int KIND>
 __global__ __launch_bounds__(W == 1 ? QT : 64 * W) void q8_row_kernel(Q8Params p) {
   constexpr int R = W == 1 ? QW : 1;
-  constexpr int IN = HOW == STREAM && KIND != SPLIT ? STREAM : CACHED, OUT = HOW;
+  constexpr int IN = HOW == STREAM && KIND != SPLIT ? STREAM : CACHED, OUT = KIND == QUANTIZE ? CACHED : HOW;
   __shared__ uint32_t part[W];
   const int32_t sub = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const int32_t lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;

@@ -206,14 +206,13 @@ __device__ __forceinline__ void norm_row(float (&v)[C][8], const Place (&c)[C], 
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[k][e] *= rs;
 }
-__device__ __forceinline__ void with_vectors(float (&v)[8], int32_t form, const float* w, const float* c,
+__device__ __forceinline__ void with_vectors(float (&v)[8], int32_t form, const float (&w)[8], const float* c,
                                              int32_t at) {
   if (form == TPP_NORM_NONE) return;
-  float x[8];
-  load8(w, at, x);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] *= x[e];
+  for (int e = 0; e < 8; ++e) v[e] *= w[e];
   if (form != TPP_NORM_LAYER || !c) return;
+  float x[8];
   load8(c, at, x);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += x[e];
@@ -234,7 +233,19 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_row_kernel(Resi
     for (int k = 0; k < C; ++k) br[k] = load_raw<BF16, HOW>(p.b, t * p.ldb + c[k].at);
 #pragma unroll
     for (int k = 0; k < C; ++k) xr[k] = load_raw<BF16, HOW>(p.x, t * p.ldx + c[k].at);
-    float v[C][8];
+    // the vectors: where the pass is no stream, under way with the rows rather than behind the sums (one token
+    // of 1024 4.0 -> 3.5 us of kernel; 8192 of 4096 53 -> 57, whose registers hold more rows back)
+    constexpr bool EARLY = HOW == CACHED;
+    float v[C][8], wa[C][8], wb[C][8];
+    const auto vector = [&](bool there, const float* w, float (&to)[C][8]) {
+      if (!there) return;
+#pragma unroll
+      for (int k = 0; k < C; ++k) load8(w, c[k].at, to[k]);
+    };
+    if constexpr (EARLY) {
+      vector(p.after, p.wa, wa);
+      vector(p.before && (p.y || p.q), p.wb, wb);
+    }
 #pragma unroll
     for (int k = 0; k < C; ++k) {
       mask<WHOLE>(c[k], br[k]);
@@ -244,7 +255,8 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_row_kernel(Resi
     const int64_t g0 = gate_row(p, t) * p.ldg;
 #pragma unroll
     for (int k = 0; k < C; ++k) {
-      with_vectors(v[k], p.after, p.wa, p.ca, c[k].at);
+      if (!EARLY && p.after) load8(p.wa, c[k].at, wa[k]);
+      with_vectors(v[k], p.after, wa[k], p.ca, c[k].at);
       if (p.gate_form) {
         float g[8];
         load8(p.gate, g0 + c[k].at, p.gate_bf16, g);
@@ -265,7 +277,8 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_row_kernel(Resi
     uint32_t top = 0;
 #pragma unroll
     for (int k = 0; k < C; ++k) {
-      with_vectors(v[k], p.before, p.wb, p.cb, c[k].at);
+      if (!EARLY && p.before) load8(p.wb, c[k].at, wb[k]);
+      with_vectors(v[k], p.before, wb[k], p.cb, c[k].at);
       Raw<BF16> y = narrow<BF16>(v[k]);
       if (p.y) store_raw<BF16, WHOLE, HOW>(p.y, t * p.ldy, c[k], y);
       mask<WHOLE>(c[k], y);

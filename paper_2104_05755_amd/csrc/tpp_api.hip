@@ -1576,6 +1576,9 @@ tpp_status tpp_q8_linear(const tpp_q8_gemm_desc* desc, const int8_t* a, const fl
   if (p.n == 0) return ok();
   if (c == x) return fail(TPP_ERR_INVALID_ARG, "c overlaps x");
   hipStream_t st = static_cast<hipStream_t>(stream);
+  p.x = x;
+  if (tpp::q8_linear_at_once(p))
+    return launched("8-bit product", tpp::launch_q8_linear_at_once(p, desc->b_type == TPP_DT_BF16, st));
   // the scales, then the rows, whose whole 16-byte chunks the product reads
   const int64_t ldq = ((int64_t)p.k + 15) / 16 * 16, scales = ((int64_t)p.n + 3) / 4 * 4;
   const int64_t need = scales + (int64_t)p.n * (ldq / 4);
