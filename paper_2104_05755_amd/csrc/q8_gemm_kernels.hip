@@ -8,12 +8,6 @@
 
 #include "internal.h"
 #include "rows_device.h"
-#ifndef TPP_BIG
-#define TPP_BIG 200
-#endif
-#ifndef TPP_MID
-#define TPP_MID 256
-#endif
 
 namespace tpp {
 namespace {
@@ -170,7 +164,7 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
   __shared__ __attribute__((aligned(16))) char own[OWN ? OWN_BYTES : 16];
   __shared__ uint32_t tops[16];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t i0 = blockIdx.x * 16 * TM;
+  const int32_t i0 = blockIdx.x * 16 * TM, j0 = OWN ? 0 : blockIdx.y * 16 * TN;
   const int32_t stages = (p.k + STAGE - 1) / STAGE, share = (stages + NW - 1) / NW;
   const int32_t s0 = min(wave * share, stages), s1 = min(s0 + share, stages);
   // a lane copies one 16-byte chunk of a row; rows' chunks XOR-swizzled as in the tiles below
@@ -186,8 +180,9 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
 #pragma unroll
   for (int r = 0; r < A_LOADS; ++r) offset(r * 8 + sub, p.lda, p.m - 1 - i0, la[r], ta[r]);
 #pragma unroll
-  for (int r = 0; r < B_LOADS; ++r) offset(r * 8 + sub, p.ldb, p.n - 1, lb[r], tb[r]);
+  for (int r = 0; r < B_LOADS; ++r) offset(r * 8 + sub, p.ldb, p.n - 1 - j0, lb[r], tb[r]);
   const int8_t* base_a = p.a + (int64_t)i0 * p.lda;
+  const int8_t* base_b = OWN ? nullptr : p.b + (int64_t)j0 * p.ldb;
   const uint32_t mine = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_AS char*)lds) + wave * SLOTS * SLOT;
   const bool ragged = p.k % STAGE != 0;
   const auto issue = [&](int32_t s, int slot) {
@@ -196,7 +191,7 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
     if (ragged && s == stages - 1) copy_rows<A_LOADS>(ra, ta, to);
     else copy_rows<A_LOADS>(ra, la, to);
     if constexpr (!OWN) {
-      const i32x4 rb = raw_buffer(p.b + (int64_t)s * STAGE);
+      const i32x4 rb = raw_buffer(base_b + (int64_t)s * STAGE);
       if (ragged && s == stages - 1) copy_rows<B_LOADS>(rb, tb, to + A_LOADS * 1024);
       else copy_rows<B_LOADS>(rb, lb, to + A_LOADS * 1024);
     }
@@ -288,7 +283,7 @@ __global__ __launch_bounds__(64 * NW) void q8_gemm_few_kernel(Q8GemmParams p) {
     }
   }
   __syncthreads();
-  join<TM, TN, NW>(p, *reinterpret_cast<i32x4_t (*)[NW][TM * TN][64]>(lds), acc, i0, 0, wave, lane,
+  join<TM, TN, NW>(p, *reinterpret_cast<i32x4_t (*)[NW][TM * TN][64]>(lds), acc, i0, j0, wave, lane,
                    [&](int32_t j) { return OWN ? q8_group(tops[j]).scale : gld<float>(p.sb + j); });
 }
 
@@ -536,9 +531,10 @@ hipError_t launch_tiles(const Q8GemmParams& p, hipStream_t stream) {
 
 template <int TM, int TN, int NW, int SLOTS, int FROM = ROWS8>
 hipError_t launch_few(const Q8GemmParams& p, hipStream_t stream) {
-  const int64_t rows = ((int64_t)p.m + 16 * TM - 1) / (16 * TM);
-  if (rows > most_groups(64 * NW)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((q8_gemm_few_kernel<TM, TN, NW, SLOTS, FROM>), dim3((uint32_t)rows), dim3(64 * NW), 0, stream, p);
+  const int64_t rows = ((int64_t)p.m + 16 * TM - 1) / (16 * TM), cols = ((int64_t)p.n + 16 * TN - 1) / (16 * TN);
+  if (rows * cols > most_groups(64 * NW)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((q8_gemm_few_kernel<TM, TN, NW, SLOTS, FROM>), dim3((uint32_t)rows, (uint32_t)cols), dim3(64 * NW),
+                     0, stream, p);
   return hipGetLastError();
 }
 // Channels of a workgroup, its wavefronts and their places: 32 channels where m has 192 workgroups of them
@@ -583,11 +579,18 @@ hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream) {
   if (p.n <= 32) return launch_few<2>(p, stream);
   if (p.n <= 48) return launch_few<3>(p, stream);
   if (p.n <= 64) return launch_few<4>(p, stream);
-  const int64_t big = (((int64_t)p.m + 255) / 256) * (((int64_t)p.n + 255) / 256);
-  const int64_t mid = (((int64_t)p.m + 127) / 128) * (((int64_t)p.n + 127) / 128);
-    if (big >= TPP_BIG) return launch_tiles<256, 256, 4, 4, 2>(p, stream);
-  if (mid >= TPP_MID) return launch_tiles<128, 128, 2, 2, 2>(p, stream);
-  return launch_tiles<64, 64, 2, 2, 4>(p, stream);
+  // The largest tile that gives most compute units one (256 x 256: 4096 x 4096 of 1024 36.9 us against 42.6 with
+  // 128 x 128, which take 51.1 against 61.5 for 2048 x 4096 of 4096, 128 large tiles); 64 x 64 where there are
+  // fewer than two of 128 x 128 to a unit's two places (1533 x 777 of 1001 14.8 against 29.3 with 256 x 256);
+  // wavefronts with shares of k where even those are few (538 x 192 of 1296 10.4 against 12.9, but 1533 x 777
+  // 18.8 against 14.9).  64 x 64 tiles have four places, or two where there are more tiles than the units hold
+  // with four (5146 x 581 of 704 20.8 against 24.1; 512 x 2048 of 8192 26.6 against 40.0 the other way).
+  const auto tiles = [&](int64_t side) { return ((p.m + side - 1) / side) * ((p.n + side - 1) / side); };
+  if (tiles(256) >= 200) return launch_tiles<256, 256, 4, 4, 2>(p, stream);
+  if (tiles(128) >= 256) return launch_tiles<128, 128, 2, 2, 2>(p, stream);
+  if (tiles(64) < 128) return launch_few<4>(p, stream);
+  if (tiles(64) <= 512) return launch_tiles<64, 64, 2, 2, 4>(p, stream);
+  return launch_tiles<64, 64, 2, 2, 2>(p, stream);
 }
 
 }  // namespace tpp

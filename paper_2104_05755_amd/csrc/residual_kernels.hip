@@ -778,7 +778,8 @@ void back_by_width(const ResidualParams& p, const F& f) {
 
 // The backward pass: whether its rows stay in registers, its sums too, how the tokens are cut, and the
 // workgroups.
-constexpr int64_t BACK_WAVES = 2048, LEAST_ROWS = 2;
+// (a token to a row team where there are few: 12 of 7616 fp32 layer norms TODO)
+constexpr int64_t BACK_WAVES = 2048, FEW_TOKENS = 256;
 struct BackPlan {
   bool rows, sums;
   Cut cut;
@@ -786,7 +787,7 @@ struct BackPlan {
   explicit BackPlan(const ResidualParams& p) : rows(p.f >= 8 && p.f <= 16384), sums(rows && p.f <= 8192) {
     int w = 8;
     if (sums) back_by_width(p, [&](auto ww, auto, auto) { w = decltype(ww)::value; });
-    cut = cut_tokens(p, sums ? min64(BACK_WAVES / w, ceil_div(p.tokens, LEAST_ROWS)) : MOST_PARTS);
+    cut = cut_tokens(p, sums ? min64(BACK_WAVES / w, p.tokens <= FEW_TOKENS ? p.tokens : ceil_div(p.tokens, 2)) : MOST_PARTS);
     groups = ceil_div(cut.parts, sums && w == 1 ? RW : 1);
   }
 };
