@@ -6,6 +6,8 @@
 // the lane.  Weights are its A, tokens its B, so a lane ends with four consecutive channels of one token.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "internal.h"
 #include "rows_device.h"
 
@@ -319,7 +321,9 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_ti
   constexpr int SLAB = 32 * WTM * 4;   // a wavefront's 32 columns of C on their way out
   constexpr int LDS = SLOTS * SLOT > NW * SLAB ? SLOTS * SLOT : NW * SLAB;
   static_assert(LDS <= 160 * 1024 && A_LOADS >= 1 && B_LOADS >= 1, "tile");
+  constexpr int THREADS = 64 * NW;
   __shared__ __attribute__((aligned(1024))) char lds[LDS];
+  __shared__ __attribute__((aligned(16))) float scales[BM], biases[BM], columns[BN];
   const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t wm = wave % WM, wn = wave / WM;
   int32_t tm_, tn_;
@@ -424,6 +428,13 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_ti
     issue_a(s);
     issue_b(s);
   }
+  // what the epilogue reads of the tile's channels and tokens (visible from the next barrier on)
+  const bool biased = p.flags & TPP_EPI_BIAS;
+  for (int32_t t = threadIdx.x; t < BM; t += THREADS) {
+    scales[t] = gld<float>(p.sa + min(i0 + t, p.m - 1));
+    biases[t] = biased ? gld<float>(p.bias + min(i0 + t, p.m - 1)) : 0.0f;
+  }
+  for (int32_t t = threadIdx.x; t < BN; t += THREADS) columns[t] = gld<float>(p.sb + min(j0 + t, p.n - 1));
   landed(min(stages, SLOTS) - 1);
   lds_barrier();
   i32x4_t fa[2][TM], fb[2][TN];
@@ -449,67 +460,68 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_ti
   }
   lds_barrier();
 
-  // C: a wavefront's 32 columns at a time through LDS, so that a store takes whole lines
+  // C: a wavefront's 32 columns at a time through LDS, so that a store takes whole lines; the large tiles' past
+  // the caches' replacement (C is 26 MB or more: the MLP block's first layer 66.5 -> 63.1 us)
   char* slab = lds + wave * SLAB;
-  const int32_t iw = i0 + wm * WTM;
-  const bool full = i0 + BM <= p.m;
+  const int32_t iw = i0 + wm * WTM, col = lane & 31;
+  const auto finish = [&](auto type, auto flags) {
+    constexpr bool BF16 = decltype(type)::value;
+    constexpr int V = BF16 ? 8 : 4, PER = WTM / V;   // entries of a 16-byte chunk, chunks of a column
 #pragma unroll
-  for (int y = 0; y < TN; ++y) {
-    const int32_t j = j0 + wn * WTN + y * 32;   // first column
-    const float sb = gld<float>(p.sb + min(j + (lane & 31), p.n - 1));
+    for (int y = 0; y < TN; ++y) {
+      const int32_t jw = wn * WTN + y * 32;   // first column in the tile
+      const float sb = columns[jw + col];
 #pragma unroll
-    for (int x = 0; x < TM; ++x)
+      for (int x = 0; x < TM; ++x)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int32_t r = x * 32 + 8 * q + 4 * half;   // first of four rows
-        float sa[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
-        if (full) {
-          const f32x4_a4 w = gld<f32x4_a4>(p.sa + iw + r);
-          sa[0] = w[0], sa[1] = w[1], sa[2] = w[2], sa[3] = w[3];
-        } else {
+        for (int q = 0; q < 4; ++q) {
+          const int32_t r = x * 32 + 8 * q + 4 * half;   // first of four rows
+          const f32x4 sa = *reinterpret_cast<const f32x4*>(scales + wm * WTM + r);
+          const f32x4 bias = *reinterpret_cast<const f32x4*>(biases + wm * WTM + r);
+          float v[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sa[e] = gld<float>(p.sa + min(iw + r + e, p.m - 1));
+          for (int e = 0; e < 4; ++e)
+            v[e] = activate((float)acc[x][y][4 * q + e] * sb * sa[e] + bias[e], (uint32_t)decltype(flags)::value);
+          if constexpr (BF16) {
+            const int32_t ch = (x * 4 + q) ^ (col & (PER - 1));
+            *reinterpret_cast<u32x2*>(slab + col * WTM * 2 + ch * 16 + half * 8) =
+                (u32x2){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+          } else {
+            const int32_t ch = ((x * 4 + q) * 2 + half) ^ (col & (PER - 1));
+            *reinterpret_cast<f32x4*>(slab + col * WTM * 4 + ch * 16) = (f32x4){v[0], v[1], v[2], v[3]};
+          }
+          __builtin_amdgcn_sched_barrier(0);   // (all quads' scales read at once do not fit the registers)
         }
-        if (p.flags & TPP_EPI_BIAS) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) bias[e] = gld<float>(p.bias + min(iw + r + e, p.m - 1));
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = activate((float)acc[x][y][4 * q + e] * sb * sa[e] + bias[e], p.flags);
-        const int32_t col = lane & 31;
-        if (p.c_bf16) {   // chunks of 8 rows
-          const int32_t ch = (x * 4 + q) ^ (col & (WTM / 8 - 1));
-          *reinterpret_cast<u32x2*>(slab + col * WTM * 2 + ch * 16 + half * 8) =
-              (u32x2){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-        } else {          // of 4
-          const int32_t ch = ((x * 4 + q) * 2 + half) ^ (col & (WTM / 4 - 1));
-          *reinterpret_cast<f32x4*>(slab + col * WTM * 4 + ch * 16) = (f32x4){v[0], v[1], v[2], v[3]};
-        }
-      }
-    const auto out = [&](auto rows) {
-      constexpr int V = decltype(rows)::value, PER = WTM / V;   // entries of a chunk, chunks of a column
 #pragma unroll
       for (int it = 0; it < 32 * PER / 64; ++it) {
-        const int32_t col = (it * 64 + lane) / PER, ch = (it * 64 + lane) % PER;
-        const u32x4 w = *reinterpret_cast<const u32x4*>(slab + col * WTM * (16 / V) + ((ch ^ (col & (PER - 1))) << 4));
-        const int32_t i = iw + ch * V;
-        if (j + col >= p.n || i >= p.m) continue;
-        char* to = static_cast<char*>(p.c) + ((int64_t)(j + col) * p.ldc + i) * (16 / V);
+        const int32_t c = (it * 64 + lane) / PER, ch = (it * 64 + lane) % PER;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(slab + c * WTM * (16 / V) + ((ch ^ (c & (PER - 1))) << 4));
+        const int32_t i = iw + ch * V, j = j0 + jw + c;
+        if (j >= p.n || i >= p.m) continue;
+        char* to = static_cast<char*>(p.c) + ((int64_t)j * p.ldc + i) * (16 / V);
         if (i + V <= p.m) {
-          gst<u32x4_a2>(to, (u32x4_a2)w);
+          if constexpr (BM == 256)
+            __builtin_nontemporal_store((u32x4_a2)w, (GLOBAL_AS u32x4_a2*)to);
+          else
+            gst<u32x4_a2>(to, (u32x4_a2)w);
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             if (i + e >= p.m) continue;
-            if constexpr (V == 8) gst<uint16_t>(to + 2 * e, (uint16_t)(w[e >> 1] >> (16 * (e & 1))));
+            if constexpr (BF16) gst<uint16_t>(to + 2 * e, (uint16_t)(w[e >> 1] >> (16 * (e & 1))));
             else gst<uint32_t>(to + 4 * e, w[e]);
           }
         }
       }
-    };
-    if (p.c_bf16) out(IntC<8>());
-    else out(IntC<4>());
-  }
+    }
+  };
+  const auto by_act = [&](auto type) {
+    if (p.flags & TPP_EPI_GELU_TANH) finish(type, IntC<TPP_EPI_GELU_TANH>());
+    else if (p.flags & TPP_EPI_RELU) finish(type, IntC<TPP_EPI_RELU>());
+    else finish(type, IntC<0>());
+  };
+  if (p.c_bf16) by_act(std::true_type());
+  else by_act(std::false_type());
 }
 
 template <int BM, int BN, int WM, int WN, int SLOTS>
