@@ -134,6 +134,8 @@ def prepare_step(step, dev: dict, device="cuda"):
     return step
 
 
+_ACT = {"none": tpp.TPP_ACT_NONE, "relu": tpp.TPP_ACT_RELU, "gelu_tanh": tpp.TPP_ACT_GELU_TANH,
+        "silu": tpp.TPP_ACT_SILU}
 _ROT = {"halves": tpp.TPP_ROT_HALVES, "pairs": tpp.TPP_ROT_PAIRS}
 
 
@@ -147,7 +149,8 @@ def kv_cache(k: torch.Tensor, v: torch.Tensor, dtype: str) -> tpp.tpp_kv_cache:
 
 def launch_step(st, dev: dict, stream: Optional[int] = None):
     """One step of a chained workload (see ``workloads.TransformStep``, ``ReduceStep``,
-    ``EmbeddingStep``, ``EquationStep``, ``AppendStep``, ``AttentionStep`` and ``EvictStep``)."""
+    ``EmbeddingStep``, ``EquationStep``, ``AppendStep``, ``AttentionStep``, ``EvictStep``,
+    ``ResidualStep``, ``QuantizeStep``, ``Q8GemmStep``, ``KeepStep`` and ``KeptBackwardStep``)."""
     if stream is None:
         stream = tpp.current_stream()
     if isinstance(st, DeviceCall):
@@ -174,6 +177,31 @@ def launch_step(st, dev: dict, stream: Optional[int] = None):
         tpp.tpp_cache_evict(kv_cache(dev[st.kc], dev[st.vc], "bf16"), st.seqs, st.max_len, st.budget,
                             dev[st.lens], pages, pages.shape[1], totals, pos, dev[st.horizon],
                             totals.shape[1], dev[st.lens], totals, pos, stream)
+    elif hasattr(st, "w_after"):    # residual stream and norms
+        f, at = st.features, lambda name: dev[name] if name else None
+        desc = tpp.tpp_residual_desc(f, tpp.TPP_DT_BF16, tpp.TPP_NORM_RMS, tpp.TPP_NORM_RMS,
+                                     tpp.TPP_GATE_NONE, tpp.TPP_DT_F32, st.scale, st.eps, 0)
+        tpp.tpp_residual_norm(desc, st.tokens, dev[st.x], f, dev[st.b], f, None, 0, dev[st.w_after], None,
+                              dev[st.w_before], None, dev[st.r], f, at(st.y), f, at(st.q), f,
+                              at(st.q_scale), stream)
+    elif hasattr(st, "quantized"):  # gated activation in 8-bit rows
+        desc = tpp.tpp_q8_desc(st.features, 0, tpp.TPP_DT_BF16, _ACT[st.act], 1)
+        tpp.tpp_q8_quantize(desc, st.tokens, dev[st.z], 2 * st.features, dev[st.q], st.features,
+                            dev[st.q_scale], 1, stream)
+    elif hasattr(st, "a_scale"):    # product of 8-bit rows
+        desc = tpp.tpp_q8_gemm_desc(st.m, st.n, st.k, st.k, st.k, st.m, tpp.TPP_DT_BF16,
+                                    tpp.TPP_DT_BF16, 0)
+        tpp.tpp_q8_gemm(desc, dev[st.a], dev[st.a_scale], dev[st.b], dev[st.b_scale], dev[st.c], None,
+                        stream)
+    elif hasattr(st, "keep_group"):  # activation, its input kept in 8 bits
+        f, s = st.features, dev[st.q_scale]
+        desc = tpp.tpp_q8_desc(f, st.keep_group, tpp.TPP_DT_BF16, _ACT[st.act], 0)
+        tpp.tpp_q8_act(desc, st.tokens, dev[st.z], f, dev[st.h], f, dev[st.q], f, s, s.shape[1], stream)
+    elif hasattr(st, "kept_group"):  # its backward pass
+        f, s = st.features, dev[st.q_scale]
+        desc = tpp.tpp_q8_desc(f, st.kept_group, tpp.TPP_DT_BF16, _ACT[st.act], 0)
+        tpp.tpp_q8_act_backward(desc, st.tokens, dev[st.q], f, s, s.shape[1], dev[st.gh], f, dev[st.dz],
+                                f, dev[st.h2], f, dev[st.dbias], stream)
     elif hasattr(st, "nodes"):      # matrix equation
         args = [(dev[name], ld, _DT[dt], bc) for name, ld, dt, bc in st.leaves]
         tpp.tpp_equation_execute(st.nodes, st.root, st.m, st.n, args, dev[st.out], st.ldo,

@@ -229,6 +229,77 @@ class EvictStep:
 
 
 @dataclass
+class ResidualStep:
+    """r = x + scale * N(b), the norm N (RMS) with the weights ``w_after``, and its norm with ``w_before``:
+    rows in bf16 to ``y``, in 8 bits to ``q`` with the tokens' scales in ``q_scale`` (either may be "")."""
+    tokens: int
+    features: int
+    scale: float
+    eps: float
+    x: str
+    b: str
+    w_after: str
+    w_before: str
+    r: str
+    y: str = ""
+    q: str = ""
+    q_scale: str = ""
+
+
+@dataclass
+class QuantizeStep:
+    """A gated activation of ``z`` (2 * features bf16 entries a token) in 8-bit rows."""
+    tokens: int
+    features: int
+    act: str
+    z: str
+    q: str
+    q_scale: str
+    quantized: bool = True
+
+
+@dataclass
+class Q8GemmStep:
+    """``c`` (bf16) from 8-bit weights ``a`` [m][k] with a scale for each channel and 8-bit tokens ``b``."""
+    m: int
+    n: int
+    k: int
+    a: str
+    a_scale: str
+    b: str
+    b_scale: str
+    c: str
+
+
+@dataclass
+class KeepStep:
+    """An activation of training: ``h`` = act(``z``), and z kept in 8-bit rows."""
+    tokens: int
+    features: int
+    act: str
+    keep_group: int
+    z: str
+    h: str
+    q: str
+    q_scale: str
+
+
+@dataclass
+class KeptBackwardStep:
+    """From the kept rows and the gradient ``gh`` of h: ``dz``, ``h2`` = act of what was kept, ``dbias``."""
+    tokens: int
+    features: int
+    act: str
+    kept_group: int
+    q: str
+    q_scale: str
+    gh: str
+    dz: str
+    h2: str
+    dbias: str
+
+
+@dataclass
 class Workload:
     name: str
     arrays: dict
@@ -584,6 +655,77 @@ def decode_step(seed: int = 11, seqs: int = 16, max_len: int = 512, budget: int 
              AttentionStep(seqs, q_heads, k_heads, dim, page, max_len, dim ** -0.5), out,
              EvictStep(seqs, k_heads, dim, page, max_len, budget)]
     return Workload("decode_step", arrays, [qkv, out], steps=steps)
+
+
+def q8_rows(w: np.ndarray):
+    """8-bit rows of fp32 rows w and their scales, for inputs."""
+    top = np.abs(w).max(1)
+    return np.rint(w * (127 / top)[:, None]).astype(np.int8), (top / np.float32(127)).astype(np.float32)
+
+
+def ffn_step(seed: int = 12, tokens: int = 24, hidden: int = 512, inter: int = 1408,
+             scale: float = 0.7, eps: float = 1e-5) -> Workload:
+    """The feed-forward half of a layer that serves tokens, in 8 bits, as a chain:
+      1. the residual stream behind the attention block, its norm in 8-bit rows
+      2. Z = W1 Y (gates and factors, 2 * inter channels)
+      3. silu(gates) * factors in 8-bit rows
+      4. O = W2 H
+      5. the stream behind it, and the norm before the next block.
+    8-bit weights of N(0, 1 / k) entries; a few features of the stream are large."""
+    rng = np.random.default_rng(seed)
+    big = np.where(rng.random(hidden) < 0.02, 6.0, 1.0)
+    x, b = (bf16_bits((_normal(rng, (tokens, hidden), s) * big).astype(np.float32)) for s in (1.0, 2.0))
+    w1, s1 = q8_rows(_normal(rng, (2 * inter, hidden), hidden ** -0.5))
+    w2, s2 = q8_rows(_normal(rng, (hidden, inter), inter ** -0.5))
+    vec = lambda: (1 + _normal(rng, (hidden,), 0.1)).astype(np.float32)
+    nan16 = lambda *s: np.full(s, 0x7FC0, np.uint16)
+    nan32 = lambda *s: np.full(s, np.nan, np.float32)
+    arrays = dict(x=x.reshape(tokens, hidden), b=b.reshape(tokens, hidden), w1=w1, s1=s1, w2=w2, s2=s2,
+                  na1=vec(), nb1=vec(), na2=vec(), nb2=vec(), r1=nan16(tokens, hidden),
+                  q1=np.zeros((tokens, hidden), np.int8), t1=nan32(tokens), z=nan16(tokens, 2 * inter),
+                  q2=np.zeros((tokens, inter), np.int8), t2=nan32(tokens), o=nan16(tokens, hidden),
+                  r2=nan16(tokens, hidden), y=nan16(tokens, hidden))
+    steps = [ResidualStep(tokens, hidden, scale, eps, "x", "b", "na1", "nb1", "r1", q="q1", q_scale="t1"),
+             Q8GemmStep(2 * inter, tokens, hidden, "w1", "s1", "q1", "t1", "z"),
+             QuantizeStep(tokens, inter, "silu", "z", "q2", "t2"),
+             Q8GemmStep(hidden, tokens, inter, "w2", "s2", "q2", "t2", "o"),
+             ResidualStep(tokens, hidden, scale, eps, "r1", "o", "na2", "nb2", "r2", y="y")]
+    return Workload("ffn_step", arrays, [], steps=steps)
+
+
+def mlp_kept(seed: int = 13, tokens: int = 256, hidden: int = 192, inter: int = 320,
+             group: int = 64) -> Workload:
+    """A training step of the MLP that keeps its activation's input in 8 bits, on whole column-major
+    matrices: Z = W1 X + b1, H = gelu(Z) with Z kept in 8-bit groups, Y = W2 H; then from dY
+      dH = W2^T dY,   dZ = dH * gelu'(Z'), H' = gelu(Z') and db1 from the kept Z',
+      dW2 = dY H'^T,  dX = W1^T dZ,  dW1 = dZ X^T."""
+    rng = np.random.default_rng(seed)
+    bf = lambda *s, std: bf16_bits(_normal(rng, s, std)).reshape(s)
+    nan16 = lambda *s: np.full(s, 0x7FC0, np.uint16)
+    nan32 = lambda *s: np.full(s, np.nan, np.float32)
+    arrays = dict(x=bf(tokens, hidden, std=1.0), w1=bf(hidden, inter, std=hidden ** -0.5),
+                  b1=_normal(rng, (inter,), 0.1), w2=bf(inter, hidden, std=inter ** -0.5),
+                  dy=bf(tokens, hidden, std=1.0), z=nan16(tokens, inter), h=nan16(tokens, inter),
+                  q=np.zeros((tokens, inter), np.int8), qs=nan32(tokens, inter // group),
+                  y=nan16(tokens, hidden), dh=nan16(tokens, inter), dz=nan16(tokens, inter),
+                  h2=nan16(tokens, inter), db1=nan32(inter), dw2=nan32(inter, hidden),
+                  dx=nan16(tokens, hidden), dw1=nan32(hidden, inter))
+    one = dict(gm=1, gn=1, a_step_m=0, b_step_n=0, c_step_m=0, c_step_n=0, bias_step_m=0)
+
+    def product(m, n, k, lda, ldb, ct, flags, a, b, c, bias=None):
+        return Call(m, n, k, lda, ldb, m, "bf16", ct, 0.0, "stride", 0, 0, set(flags), G=1, grid=dict(one),
+                    count=1, a=a, b=b, c=c, bias=bias)
+
+    z = product(inter, tokens, hidden, inter, hidden, "bf16", {"bias"}, "w1", "x", "z", "b1")
+    y = product(hidden, tokens, inter, hidden, inter, "bf16", (), "w2", "h", "y")
+    dh = product(inter, tokens, hidden, hidden, hidden, "bf16", {"a_trans"}, "w2", "dy", "dh")
+    dw2 = product(hidden, inter, tokens, hidden, inter, "f32", {"b_trans"}, "dy", "h2", "dw2")
+    dx = product(hidden, tokens, inter, inter, inter, "bf16", {"a_trans"}, "w1", "dz", "dx")
+    dw1 = product(inter, hidden, tokens, inter, hidden, "f32", {"b_trans"}, "dz", "x", "dw1")
+    steps = [z, KeepStep(tokens, inter, "gelu_tanh", group, "z", "h", "q", "qs"), y, dh,
+             KeptBackwardStep(tokens, inter, "gelu_tanh", group, "q", "qs", "dh", "dz", "h2", "db1"),
+             dw2, dx, dw1]
+    return Workload("mlp_kept", arrays, [z, y, dh, dw2, dx, dw1], steps=steps)
 
 
 CONFIGS = {
