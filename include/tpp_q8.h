@@ -18,7 +18,8 @@
  *     scale = max|v| / 127,    q = the whole number nearest to 127 v / max|v| (ties to even)
  * exactly (scale rounded to fp32, q the rounding of the true quotient).  A group of zeros has scale 0.
  * A group with an infinity or NaN has scale NaN and q = 0, so that all that is made of it is NaN.
- * Entries of q behind a row's last feature are not written.
+ * Entries of q behind a row's last feature are not written.  Outputs must not overlap inputs unless a call
+ * says so.
  */
 #ifndef TPP_Q8_H
 #define TPP_Q8_H
@@ -81,7 +82,8 @@ tpp_status tpp_q8_act_backward(const tpp_q8_desc* desc, int64_t tokens, const in
  * scale and then with the channel's, each in fp32.  Fastest where a, b, lda and ldb are multiples of 16
  * bytes: then whole 16-byte chunks are read, and what stands in them behind entry k counts for nothing. */
 typedef struct {
-  int32_t m, n, k;         /* >= 0 (n), > 0; k at most 131071: the sum fits 32 bits         */
+  int32_t m, n, k;         /* > 0, >= 0, > 0; m and n at most 2^31 - 512, k at most 131071:
+                              the sum fits 32 bits                                          */
   int64_t lda, ldb, ldc;   /* >= k, k, m                                                    */
   int32_t b_type;          /* tpp_q8_linear: of the tokens' activations                     */
   int32_t c_type;
@@ -90,7 +92,8 @@ typedef struct {
 
 /* a_scale: m floats, b_scale: n floats, bias: m floats (NULL without TPP_EPI_BIAS).
  * Errors: INVALID_ARG for a NULL desc, sizes, types, flags or leading dimensions out of their ranges or
- * a NULL pointer when there is work; UNSUPPORTED for k above 131071; HIP if a launch fails. */
+ * a NULL pointer when there is work; UNSUPPORTED for larger m, n or k, or a launch of 2^32 threads or
+ * more; HIP if a launch fails. */
 tpp_status tpp_q8_gemm(const tpp_q8_gemm_desc* desc, const int8_t* a, const float* a_scale,
                        const int8_t* b, const float* b_scale, void* c, const float* bias, void* stream);
 

@@ -11,7 +11,7 @@
  * asynchronous on `stream` (a hipStream_t as void*, NULL = the default stream), a tpp_status result and
  * tpp_last_error_message() for the detail.  Activations are column-major 2D blocks with a column per
  * token: feature i of token t is at x + t * ld + i.  Arithmetic is fp32; an output is rounded to its
- * type once (to nearest even).  The order of every sum depends only on sizes: results do not vary
+ * type once (to nearest even); the sums of squares have to stay in fp32's range.  The order of every sum depends only on sizes: results do not vary
  * between runs.
  */
 #ifndef TPP_RESIDUAL_H

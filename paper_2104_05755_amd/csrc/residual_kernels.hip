@@ -35,7 +35,8 @@ __device__ __forceinline__ float gate_slope(float g, int32_t form) {
   return (form == TPP_GATE_SIGMOID ? 1.0f : 4.0f) * e * s * s;
 }
 __device__ __forceinline__ int64_t gate_row(const ResidualParams& p, int64_t t) {
-  return p.gate_every ? t / p.gate_every : 0;
+  if (!p.gate_form || !p.gate_every) return 0;
+  return ((t | p.gate_every) >> 32) == 0 ? (uint32_t)t / (uint32_t)p.gate_every : t / p.gate_every;
 }
 
 // ---- any width ------------------------------------------------------------------------------------
@@ -272,24 +273,25 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_row_kernel(Resi
       mask<WHOLE>(c[k], r);
       widen<BF16>(r, v[k]);
     }
-    if (!p.y && !p.q) continue;
-    norm_row<W, C, WHOLE>(v, c, p.before, p.eps, inv_f, part[1]);
-    uint32_t top = 0;
+    if (p.y || p.q) {
+      norm_row<W, C, WHOLE>(v, c, p.before, p.eps, inv_f, part[1]);
+      uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < C; ++k) {
-      if (!EARLY && p.before) load8(p.wb, c[k].at, wb[k]);
-      with_vectors(v[k], p.before, wb[k], p.cb, c[k].at);
-      Raw<BF16> y = narrow<BF16>(v[k]);
-      if (p.y) store_raw<BF16, WHOLE, HOW>(p.y, t * p.ldy, c[k], y);
-      mask<WHOLE>(c[k], y);
-      widen<BF16>(y, v[k]);
-      top = Top::join(top, top8<BF16>(y));
-    }
-    if (p.q) {
-      const Q8Group g = q8_group(over_group<Top, W>(top, tops));
+      for (int k = 0; k < C; ++k) {
+        if (!EARLY && p.before) load8(p.wb, c[k].at, wb[k]);
+        with_vectors(v[k], p.before, wb[k], p.cb, c[k].at);
+        Raw<BF16> y = narrow<BF16>(v[k]);
+        if (p.y) store_raw<BF16, WHOLE, HOW>(p.y, t * p.ldy, c[k], y);
+        mask<WHOLE>(c[k], y);
+        widen<BF16>(y, v[k]);
+        top = Top::join(top, top8<BF16>(y));
+      }
+      if (p.q) {
+        const Q8Group g = q8_group(over_group<Top, W>(top, tops));
 #pragma unroll
-      for (int k = 0; k < C; ++k) store_q8<WHOLE>(p.q + t * p.ldq, c[k], v[k], g);
-      if ((W == 1 ? threadIdx.x & 63 : threadIdx.x) == 0) gst<float>(p.qs + t, g.scale);
+        for (int k = 0; k < C; ++k) store_q8<WHOLE>(p.q + t * p.ldq, c[k], v[k], g);
+        if ((W == 1 ? threadIdx.x & 63 : threadIdx.x) == 0) gst<float>(p.qs + t, g.scale);
+      }
     }
     if constexpr (W > 1) __syncthreads();   // the sums' places are free for the next row
   }

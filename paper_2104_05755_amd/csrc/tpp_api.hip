@@ -1480,6 +1480,9 @@ tpp_status check_q8_gemm(const tpp_q8_gemm_desc* d, const int8_t* a, const float
   if ((d->flags & TPP_EPI_RELU) && (d->flags & TPP_EPI_GELU_TANH))
     return fail(TPP_ERR_INVALID_ARG, "RELU and GELU_TANH exclude each other");
   if (d->k > 131071) return fail(TPP_ERR_UNSUPPORTED, "k %d is above 131071", d->k);
+  // rows and columns of a last tile count in 31 bits
+  if (d->m > INT32_MAX - 511 || d->n > INT32_MAX - 511)
+    return fail(TPP_ERR_UNSUPPORTED, "m or n is above 2^31 - 512");
   if (d->n > 0) {
     if (!a || !a_scale || !b || !c) return fail(TPP_ERR_INVALID_ARG, "NULL weights, scales, tokens or c");
     if ((d->flags & TPP_EPI_BIAS) && !bias) return fail(TPP_ERR_INVALID_ARG, "NULL bias");

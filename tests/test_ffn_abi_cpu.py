@@ -140,7 +140,8 @@ def test_products_refuse(tpp, which):
     for status, dkw in ((INV, dict(m=0)), (INV, dict(n=-1)), (INV, dict(k=0)), (INV, dict(lda=39)),
                         (INV, dict(ldb=39)), (INV, dict(ldc=63)), (INV, dict(b_type=2)), (INV, dict(c_type=3)),
                         (INV, dict(flags=6)), (INV, dict(flags=8)), (INV, dict(flags=32)),
-                        (UNS, dict(k=131072, lda=131072, ldb=131072))):
+                        (UNS, dict(k=131072, lda=131072, ldb=131072)), (UNS, dict(n=2 ** 31 - 511)),
+                        (UNS, dict(m=2 ** 31 - 1, ldc=2 ** 31))):
         refused(tpp, status, lambda: product(tpp, which, dkw))
     for kw in [dict(a=None), dict(sa=None), dict(c=None), dict(bias=None), dict(desc=False)] + (
             [dict(b=None), dict(sb=None)] if which == "gemm" else [dict(x=None), dict(c=Q)]):

@@ -63,6 +63,9 @@ ROWS = [
     (3, 16384, 0, "bf16", "gelu_tanh", 1, 0, 0),
     (3, 16384, 0, "f32", "silu", 1, 0, 0),
     (2, 40000, 0, "bf16", "silu", 1, 0, 0),
+    (2, 30000, 0, "f32", "gelu_tanh", 0, 0, 0),
+    (2, 16001, 32, "bf16", "silu", 1, 0, 0),
+    (2, 15000, 512, "f32", "silu", 1, 0, 1),
     (2, 33000, 32, "f32", "relu", 1, 0, 0),
     (1500, 72, 0, "bf16", "silu", 0, 0, 0),
     (1500, 40, 16, "f32", "gelu_tanh", 1, 0, 0),
@@ -239,6 +242,10 @@ PRODUCTS = [
     (1031, 1090, 400, 0, 16, 1, 0, "f32", ("bias", "gelu_tanh")),
     (2048, 2300, 128, 0, 0, 0, 0, "bf16", ()),
     (2050, 2048, 144, 0, 0, 2, 0, "f32", ("relu",)),
+    (192, 600, 1300, 12, 12, 0, 0, "bf16", ("gelu_tanh",)),   # few tiles: shares of k
+    (16, 900, 2283, 5, 5, 0, 0, "f32", ("bias",)),
+    (581, 4200, 200, 8, 8, 3, 0, "bf16", ("bias",)),          # many small tiles
+    (4100, 3900, 130, 14, 14, 0, 0, "bf16", ("bias", "relu")),  # large tiles with tails each way
     (130, 70, 333, 0, 0, 0, 3, "f32", ("bias",)),     # bases and rows at any byte
     (40, 9, 4100, 1, 2, 0, 1, "bf16", ()),
     (33, 200, 64, 0, 0, 0, 4, "f32", ()),
@@ -301,7 +308,9 @@ LINEAR = [c for c in PRODUCTS if c[2] < 5000]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("case", LINEAR, ids=str)
+@pytest.mark.parametrize("case", LINEAR + [
+    (700, 16, 760, 8, 0, 0, 0, "bf16", ("bias",)), (700, 17, 760, 8, 0, 0, 0, "f32", ()),   # one launch, and two
+    (6200, 3, 4000, 0, 3, 5, 0, "bf16", ("gelu_tanh",)), (50, 1, 12288, 0, 0, 0, 0, "f32", ())], ids=str)
 def test_linear(tpp, case, dtype):
     p = Product(case, 1)
     rng = np.random.default_rng(2)
