@@ -427,15 +427,17 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_backward_row_ke
   const bool after_mean = MEANS && p.after == TPP_NORM_LAYER, before_mean = MEANS && before && p.before == TPP_NORM_LAYER;
   Place c[C];
   places<W, C>(p.f, c);
-  float wb[C][8], dwa[C][8], dca[C][8], dwb[C][8], dcb[C][8];
+  // the vectors of a row team's features, or, where registers are short, loaded where they are used
+  constexpr int V = SUMS ? C : 1;
+  float wb[V][8], dwa[C][8], dca[C][8], dwb[C][8], dcb[C][8];
   fill(wb, 1.0f);
   fill(dwa, 0.0f);
   fill(dca, 0.0f);
   fill(dwb, 0.0f);
   fill(dcb, 0.0f);
-  if (before) {
+  if (SUMS && before) {
 #pragma unroll
-    for (int k = 0; k < C; ++k) load8(p.wb, c[k].at, wb[k]);
+    for (int k = 0; k < V; ++k) load8(p.wb, c[k].at, wb[k]);
   }
   const auto load = [&](BackRows<BF16, C>& x, int64_t t) {
 #pragma unroll
@@ -454,17 +456,20 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_backward_row_ke
     const int64_t t1 = min(min(t0 + cut.rows, (gate + 1) * cut.every), p.tokens);
     BackRows<BF16, C> raw = {};
     if (AHEAD && t0 < t1) load(raw, t0);
-    float gw[C][8], A[C][8], B[C][8];   // gw = scale G wa
+    float gw[V][8], A[C][8], B[C][8];   // gw = scale G wa
     fill(A, 0.0f);
     fill(B, 0.0f);
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
+    const auto branch = [&](int k, float (&to)[8]) {
       float w[8], g[8];
       if (after) load8(p.wa, c[k].at, w);
       if (p.gate_form) load8(p.gate, gate * p.ldg + c[k].at, p.gate_bf16, g);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        gw[k][e] = p.scale * (p.gate_form ? gate_value(g[e], p.gate_form) : 1.0f) * (after ? w[e] : 1.0f);
+        to[e] = p.scale * (p.gate_form ? gate_value(g[e], p.gate_form) : 1.0f) * (after ? w[e] : 1.0f);
+    };
+    if constexpr (SUMS) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) branch(k, gw[k]);
     }
     for (int64_t t = t0; t < t1; ++t) {
       if constexpr (!AHEAD) load(raw, t);
@@ -502,13 +507,15 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_backward_row_ke
       }
       float q[MEANS ? 4 : 3] = {squares_of(b), squares_of(r), 0.0f};
 #pragma unroll
-      for (int k = 0; k < C; ++k)
+      for (int k = 0; k < C; ++k) {
+        if (!SUMS && before) load8(p.wb, c[k].at, wb[0]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float u = y[k][e] * wb[k][e];
+          const float u = y[k][e] * wb[SUMS ? k : 0][e];
           q[2] = __builtin_fmaf(u, r[k][e], q[2]);
           if constexpr (MEANS) q[3] += u;
         }
+      }
       row_sums<W>(q, part1);
       const float rb = after ? rsqrt_of(q[0] * inv_f + p.eps) : 1.0f;
       const float rr = before ? rsqrt_of(q[1] * inv_f + p.eps) : 1.0f;
@@ -525,11 +532,15 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_backward_row_ke
       float o[MEANS ? 2 : 1] = {0.0f};
 #pragma unroll
       for (int k = 0; k < C; ++k) {
+        if constexpr (!SUMS) {
+          if (before) load8(p.wb, c[k].at, wb[0]);
+          branch(k, gw[0]);
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float ty = y[k][e] * rr;
           if constexpr (SUMS) dwb[k][e] = __builtin_fmaf(ty, r[k][e], dwb[k][e]);
-          d[k][e] = __builtin_fmaf(along_r, r[k][e], __builtin_fmaf(ty, wb[k][e], d[k][e]));
+          d[k][e] = __builtin_fmaf(along_r, r[k][e], __builtin_fmaf(ty, wb[SUMS ? k : 0][e], d[k][e]));
           if constexpr (MEANS) {
             if constexpr (SUMS) dcb[k][e] += y[k][e];
             d[k][e] -= level_r;
@@ -542,7 +553,7 @@ __global__ __launch_bounds__(W == 1 ? RT : 64 * W) void residual_backward_row_ke
           if constexpr (MEANS && SUMS) B[k][e] += d[k][e];
           const float td = d[k][e] * rb;
           if constexpr (SUMS) A[k][e] = __builtin_fmaf(td, b[k][e], A[k][e]);
-          d[k][e] = td * gw[k][e];
+          d[k][e] = td * gw[SUMS ? k : 0][e];
           o[0] = __builtin_fmaf(d[k][e], b[k][e], o[0]);
           if constexpr (MEANS) o[1] += d[k][e];
         }
@@ -775,6 +786,7 @@ void back_by_width(const ResidualParams& p, const F& f) {
   if (chunks <= 4) return f(IntC<4>(), IntC<1>(), sums);
   if (chunks <= 8) return f(IntC<8>(), IntC<1>(), sums);
   if (chunks <= 16) return f(IntC<8>(), IntC<2>(), sums);
+  if (chunks <= 24) return f(IntC<8>(), IntC<3>(), std::false_type());
   return f(IntC<8>(), IntC<4>(), std::false_type());
 }
 
