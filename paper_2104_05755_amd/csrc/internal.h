@@ -347,7 +347,7 @@ struct EvictParams {
 int64_t evict_work_floats(const EvictParams& p);
 hipError_t launch_evict(const EvictParams& p, float* work, hipStream_t stream);
 
-// The residual stream's norms (residual_kernels.hip).
+// The residual stream's norms (residual_kernels.hip, residual_backward_kernels.hip).
 struct ResidualParams {
   const void *x, *b, *gate;   // forward: the stream; both: the block's output, its gate
   const float *wa, *ca, *wb, *cb;
@@ -402,8 +402,8 @@ hipError_t launch_q8_gemm(const Q8GemmParams& p, hipStream_t stream);
 bool q8_linear_at_once(const Q8GemmParams& p);
 hipError_t launch_q8_linear_at_once(const Q8GemmParams& p, bool bf16, hipStream_t stream);
 
-// out = the sum over `parts` rows of `width` floats, for each of `n` outputs of its own (fold_kernels in
-// residual_kernels.hip).
+// out = the sum over `parts` rows of `width` floats, for each of `n` outputs of its own
+// (residual_backward_kernels.hip).
 struct FoldJob {
   const float* from;   // the first part; parts follow `width` floats apart
   int64_t parts;       // of one output row

@@ -3,8 +3,8 @@
 // include/tpp_q8.h: argument checks, the dispatch cache, kernel selection and launches.  Host code
 // only; the kernels live in brgemm_kernels.hip, brgemm_dl_kernels.hip, reduce_kernels.hip,
 // transform_kernels.hip, embedding_kernels.hip, equation.hip (which also holds the equation planner),
-// rope_kernels.hip, attention_kernels.hip, cache_kernels.hip, residual_kernels.hip, q8_kernels.hip and
-// q8_gemm_kernels.hip.
+// rope_kernels.hip, attention_kernels.hip, cache_kernels.hip, residual_kernels.hip,
+// residual_backward_kernels.hip, q8_kernels.hip and q8_gemm_kernels.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
