@@ -4,7 +4,7 @@
 // The matrix instructions v_mfma_i32_16x16x64_i8 and v_mfma_i32_32x32x32_i8 take 16 consecutive bytes of a row
 // from each lane and leave four (times four) consecutive rows of one column in it.  Weights are A, tokens B, so a
 // lane ends with consecutive channels of one token.  2 m n k operations, twice bf16's rate: many tokens are bound
-// by the matrix instructions and what feeds them (the clock falls to 1.5 to 2 GHz under them), few tokens by
+// by the matrix instructions and what feeds them (the clock falls to 1.6 to 1.8 GHz under them), few tokens by
 // the weights' bytes.
 //
 // 8192 tokens through 4096 -> 16384 with their quantisation 491 us, 2.24 POP/s, where torch's product of the rows

@@ -4,8 +4,8 @@
 // A group's entries become q = 127 v / max|v| rounded to whole numbers, scale = max|v| / 127: about 9 operations
 // an entry of 1 to 4 bytes (30 with an activation): bound by HBM.
 //
-// 8192 tokens of 4096 bf16: a GELU with its input kept 34 us, 5.0 TB/s, its backward pass 52 us, 4.7 TB/s, and 4.7
-// the fold of dbias (a copy of as much: 78 us in all); quantised for a product 27 us.  A workgroup to a row and a
+// 8192 tokens of 4096 bf16: a GELU with its input kept 34 us, 4.9 TB/s, its backward pass 52 us, 4.5 TB/s, and 4.7
+// the fold of dbias (a copy of as much: 78 us in all); quantised for a product 33 us.  A workgroup to a row and a
 // pass for the maximum: 113, 80 and 75 us.
 #include <hip/hip_runtime.h>
 

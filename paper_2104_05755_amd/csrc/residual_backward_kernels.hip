@@ -8,12 +8,12 @@
 // and the gate's gradients are sums over tokens: workgroups keep them for the tokens that they take and store
 // one partial row each, which a second kernel adds in order (no atomics: the bits do not vary between runs).
 //
-// 8192 tokens of 4096 bf16: 85.5 us, 4.7 TB/s, 4.7 of them the fold (a copy of as much: 78 us).  1533 of 1001
+// 8192 tokens of 4096 bf16: 86 to 89 us, 4.5 to 4.7 TB/s, 4.7 of them the fold (a copy of as much: 78 us).  1533 of 1001
 // fp32, layer norms and a gate for every 100 tokens: 24 us, where a copy takes 7.2: the kernel, 17 us, is two
 // turns of a loop in which rows and three exchanges wait for each other, the fold 7.  From a workgroup to a row
-// and a second reading for the sums: 707 and 40 us.  One chunk of 8 entries to a lane carried best (two: 92 us,
-// 49), as did 2048 wavefronts (4096: 100 us, 1024: 87); a second token's rows under way gained nothing (84.0
-// against 85.2, 31 against 29).
+// and a second reading for the sums: 707 and 40 us.  One chunk of 8 entries to a lane carried best (85 us
+// against 92 with two, and 35 against 49), as did 2048 wavefronts (4096: 92 us against 84, 1024: 103 against 86); a second token's
+// rows under way gained little and cost elsewhere (84.0 against 85.2, but 31 against 29).
 #include <hip/hip_runtime.h>
 
 #include "residual_device.h"
@@ -564,7 +564,7 @@ void back_by_width(const ResidualParams& p, const F& f) {
 
 // The backward pass: whether its rows stay in registers, its sums too, how the tokens are cut, and the
 // workgroups.  A row team has two tokens at least, whose parts would else be as many as the rows; few tokens
-// have a team each (300 of 4096 with a gate for every 7: 15.9 us against 19.8).
+// have a team each (300 of 4096 with a gate for every 7: 15.9 us against 18.4).
 constexpr int64_t BACK_WAVES = 2048, FEW_TOKENS = 256;
 struct BackPlan {
   bool rows, sums;
