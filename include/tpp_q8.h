@@ -17,7 +17,9 @@
  * 8-bit rows.  The entries v of a group are q * scale with
  *     scale = max|v| / 127,    q = the whole number nearest to 127 v / max|v| (ties to even)
  * exactly (scale rounded to fp32, q the rounding of the true quotient).  A group of zeros has scale 0.
- * A group with an infinity or NaN has scale NaN and q = 0, so that all that is made of it is NaN.
+ * A group with an infinity or NaN has scale NaN and q = 0, so that all that a product or the backward
+ * pass of an activation makes of it is NaN (but for a product with TPP_EPI_RELU, whose x > 0 ? x : +0 is
+ * 0 then, as everywhere in the library).
  * Entries of q behind a row's last feature are not written.  Outputs must not overlap inputs unless a call
  * says so.
  */
@@ -69,8 +71,8 @@ tpp_status tpp_q8_act(const tpp_q8_desc* desc, int64_t tokens, const void* z, in
  * the activation h2 = act(z') (for the next layer's weight gradient), and dbias = the sum of dz (not
  * rounded) over all tokens, one fp32 for each entry of z, overwritten (tokens == 0: zeros).  Each may be
  * NULL where it is not wanted; outputs must not overlap inputs, except h2, which may be gh (same ld).
- * act'(0) of RELU is 0.  dbias' partial sums go to a work buffer as tpp_reduce's do, under stream capture to one of
- * the capture's own.
+ * act'(0) of RELU is 0; act and act' of a NaN are NaN, but for NONE's slope, which is 1.  dbias' partial
+ * sums go to a work buffer as tpp_reduce's do, under stream capture to one of the capture's own.
  * Errors: as tpp_q8_quantize; NO_MEMORY if there is no work buffer to be had. */
 tpp_status tpp_q8_act_backward(const tpp_q8_desc* desc, int64_t tokens, const int8_t* q, int64_t ldq,
                                const float* scale, int64_t lds, const void* gh, int64_t ldgh, void* dz,

@@ -120,11 +120,12 @@ __device__ __forceinline__ float act_value(float z, int32_t act) {
   if (act == TPP_ACT_SILU) return z * sigmoid(z);
   return z;
 }
-// act(z) and act'(z) together: the exponential is shared.
+// act(z) and act'(z) together: the exponential is shared.  A NaN, which is what a group of 8 bits without a scale
+// holds, gives a NaN of both behind RELU too (z > 0 ? .. would make a zero of it).
 __device__ __forceinline__ void act_both(float z, int32_t act, float& value, float& slope) {
   if (act == TPP_ACT_RELU) {
-    value = z > 0.0f ? z : 0.0f;
-    slope = z > 0.0f ? 1.0f : 0.0f;
+    value = z <= 0.0f ? 0.0f : z;
+    slope = z <= 0.0f ? 0.0f : z != z ? z : 1.0f;
   } else if (act == TPP_ACT_GELU_TANH) {   // gelu_tanh and gelu_tanh_grad with one exponential
     const float x = fminf(fmaxf(z, -9.0f), 9.0f);
     const float e = __builtin_amdgcn_exp2f(x * __builtin_fmaf(-0.10294324f, x * x, -2.3022082f));

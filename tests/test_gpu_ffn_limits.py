@@ -1,0 +1,106 @@
+"""The feed-forward operators at the ends of what they take: groups without a scale behind every
+activation."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from ffn_common import blank, code, down, draw, untouched, up
+from helpers import values
+from test_gpu_q8 import act_code
+
+pytestmark = pytest.mark.gpu
+ACTS = ("none", "relu", "gelu_tanh", "silu")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+
+
+@pytest.fixture(scope="module")
+def tpp():
+    import paper_2104_05755_amd as tpp
+    return tpp
+
+
+def act_backward(tpp, q, scale, group, gh, act, gated, dtype):
+    """(dz, h2, dbias) of rows q with their scales, as float64."""
+    T, W = q.shape
+    F = W >> gated
+    d = tpp.tpp_q8_desc(F, group, code(tpp, dtype), act_code(tpp, act), gated)
+    dz, h2, db = blank(T, W + 1, dtype), blank(T, F + 1, dtype), blank(1, W, "f32")
+    tpp.tpp_q8_act_backward(d, T, up(q), W, up(scale), scale.shape[1], up(gh), gh.shape[1], dz, W + 1, h2, F + 1, db,
+                            tpp.current_stream())
+    dz, h2 = down(dz), down(h2)
+    assert untouched(dz, W) and untouched(h2, F)
+    return values(dz, dtype)[:, :W], values(h2, dtype)[:, :F], down(db)[0].astype(np.float64)
+
+
+# ---- groups without a scale -------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("features,group", [(96, 32), (100, 16), (96, 0), (5, 0)])   # the last: a row below 8 entries
+@pytest.mark.parametrize("act", ACTS)
+def test_gradients_of_groups_without_a_scale(tpp, act, features, group, dtype):
+    """A scale of NaN makes NaN of all that the backward pass makes of its group, whatever the activation, and of
+    nothing else."""
+    rng = np.random.default_rng(features + group)
+    for gated in (0, 1):
+        W, T = features << gated, 6
+        g = group or W
+        q = rng.integers(-127, 128, (T, W)).astype(np.int8)
+        scale = rng.uniform(0.5, 2, (T, -(-W // g))).astype(np.float32) / 64
+        gh = draw(rng, T, features, features, dtype)
+        bad = np.zeros(scale.shape, bool)
+        bad[1, 0] = bad[3, -1] = bad[4, scale.shape[1] // 2] = True
+        scale[bad] = np.nan
+        entry = np.repeat(bad, g, 1)[:, :W]
+        q[entry] = 0
+        dz, h2, db = act_backward(tpp, q, scale, group, gh, act, gated, dtype)
+        a, u = entry[:, :features], entry[:, features:]
+        want_h = a | u if gated else a
+        want_dz = np.concatenate([a | u, a], 1) if gated else a
+        if act == "none" and not gated:   # the slope is 1 whatever the entry: dz = gh
+            want_dz = np.zeros_like(a)
+        elif act == "none":               # dz of the first half: gh u
+            want_dz = np.concatenate([u, a], 1)
+        assert np.array_equal(np.isnan(h2), want_h)
+        assert np.array_equal(np.isnan(dz), want_dz)
+        assert np.array_equal(np.isnan(db), want_dz.any(0))
+
+
+@pytest.mark.parametrize("group", [0, 32])
+def test_an_infinity_is_seen_behind_relu(tpp, group):
+    """From an infinity in z to the gradients: the forward call's h keeps it, and the backward pass, which has
+    lost the group's entries, gives NaN."""
+    rng = np.random.default_rng(1)
+    z = draw(rng, 3, 64, 64, "f32")
+    z[1, 40] = np.inf
+    d = tpp.tpp_q8_desc(64, group, tpp.TPP_DT_F32, tpp.TPP_ACT_RELU, 0)
+    q, s = torch.zeros((3, 64), dtype=torch.int8, device="cuda"), torch.zeros((3, 64 // group if group else 1), device="cuda")
+    h = blank(3, 64, "f32")
+    tpp.tpp_q8_act(d, 3, up(z), 64, h, 64, q, 64, s, s.shape[1], tpp.current_stream())
+    assert np.array_equal(down(h), np.where(z > 0, z, 0))
+    dz, h2, db = act_backward(tpp, down(q), down(s), group, draw(rng, 3, 64, 64, "f32"), "relu", 0, "f32")
+    lost = np.zeros((3, 64), bool)
+    lost[1, 32 if group else 0:] = True
+    assert np.array_equal(np.isnan(h2), lost) and np.array_equal(np.isnan(dz), lost)
+    assert np.array_equal(np.isnan(db), lost.any(0))
+
+
+@pytest.mark.parametrize("n", [3, 70, 2100])
+def test_products_of_tokens_without_a_scale(tpp, n):
+    """Their columns are NaN behind no activation and GELU; TPP_EPI_RELU is x > 0 ? x : +0 here as in every other
+    product, so 0 behind it."""
+    rng = np.random.default_rng(n)
+    a, b = (rng.integers(-127, 128, (r, 64)).astype(np.int8) for r in (300, n))
+    sa, sb = np.full(300, 0.01, np.float32), rng.uniform(0.5, 1, n).astype(np.float32)
+    b[1], sb[1] = 0, np.nan
+    for flags in (0, tpp.TPP_EPI_GELU_TANH, tpp.TPP_EPI_RELU):
+        d = tpp.tpp_q8_gemm_desc(300, n, 64, 64, 64, 300, tpp.TPP_DT_F32, tpp.TPP_DT_F32, flags)
+        c = blank(n, 300, "f32")
+        tpp.tpp_q8_gemm(d, up(a), up(sa), up(b), up(sb), c, None, tpp.current_stream())
+        c = down(c)
+        assert (c[1] == 0).all() if flags == tpp.TPP_EPI_RELU else np.isnan(c[1]).all()
+        assert np.isfinite(np.delete(c, 1, 0)).all()
