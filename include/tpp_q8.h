@@ -66,7 +66,8 @@ tpp_status tpp_q8_quantize(const tpp_q8_desc* desc, int64_t tokens, const void* 
 tpp_status tpp_q8_act(const tpp_q8_desc* desc, int64_t tokens, const void* z, int64_t ldz, void* h,
                       int64_t ldh, int8_t* q, int64_t ldq, float* scale, int64_t lds, void* stream);
 
-/* The backward pass from z' = q * scale and the gradient gh of h: the gradient of z,
+/* The backward pass from z' = q * scale (in fp32, so infinite beyond its largest number) and the gradient
+ * gh of h: the gradient of z,
  *     dz = gh * act'(z')      (gated, with a and u the halves of z': gh * u * act'(a) and gh * act(a))
  * the activation h2 = act(z') (for the next layer's weight gradient), and dbias = the sum of dz (not
  * rounded) over all tokens, one fp32 for each entry of z, overwritten (tokens == 0: zeros).  Each may be

@@ -122,23 +122,24 @@ __device__ __forceinline__ float act_value(float z, int32_t act) {
 }
 // act(z) and act'(z) together: the exponential is shared.  A NaN, which is what a group of 8 bits without a scale
 // holds, gives a NaN of both behind RELU too (z > 0 ? .. would make a zero of it).
+// s = 1 / (1 + e) falls to 0 where e passes fp32's range, far left of zero, and z s with it; 1 - s = e s (no
+// difference of near values) is taken of an e that stays finite, where s = 0 leaves nothing of the slope.
 __device__ __forceinline__ void act_both(float z, int32_t act, float& value, float& slope) {
+  constexpr float BIG = 0x1p126f;
   if (act == TPP_ACT_RELU) {
     value = z <= 0.0f ? 0.0f : z;
     slope = z <= 0.0f ? 0.0f : z != z ? z : 1.0f;
   } else if (act == TPP_ACT_GELU_TANH) {   // gelu_tanh and gelu_tanh_grad with one exponential
-    const float x = fminf(fmaxf(z, -9.0f), 9.0f);
-    const float e = __builtin_amdgcn_exp2f(x * __builtin_fmaf(-0.10294324f, x * x, -2.3022082f));
+    const float e = __builtin_amdgcn_exp2f(z * __builtin_fmaf(-0.10294324f, z * z, -2.3022082f));
     const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    const float x = __builtin_amdgcn_fmed3f(z, -9.0f, 9.0f);   // (beyond it the slope is s to within 3e-27)
     value = z * s;
-    slope = s * __builtin_fmaf(1.5957691f * x * (e * s), __builtin_fmaf(0.134145f, x * x, 1.0f), 1.0f);
-    slope = z != z ? z : slope;   // (the clamp drops a NaN)
+    slope = s * __builtin_fmaf(1.5957691f * x * (fminf(e, BIG) * s), __builtin_fmaf(0.134145f, x * x, 1.0f), 1.0f);
   } else if (act == TPP_ACT_SILU) {
-    const float e = __builtin_amdgcn_exp2f(fminf(z * -1.44269504f, 126.0f));   // 1 - s = e s, finite
+    const float e = __builtin_amdgcn_exp2f(z * -1.44269504f);
     const float s = __builtin_amdgcn_rcpf(1.0f + e);
     value = z * s;
-    slope = s + z * (e * s) * s;
-    slope = z != z ? z : slope;   // (so does the minimum)
+    slope = __builtin_fmaf(z * (fminf(e, BIG) * s), s, s);
   } else {
     value = z;
     slope = 1.0f;

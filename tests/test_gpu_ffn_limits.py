@@ -1,12 +1,14 @@
 """The feed-forward operators at the ends of what they take: groups without a scale behind every
-activation."""
+activation, activations far from zero.
+
+Bounds (u = 2^-24) beside each test; a bf16 output adds half a unit of its own."""
 from __future__ import annotations
 
 import numpy as np
 import pytest
 import torch
 
-from ffn_common import blank, code, down, draw, untouched, up
+from ffn_common import U, blank, code, down, draw, untouched, up
 from helpers import values
 from test_gpu_q8 import act_code
 
@@ -104,3 +106,62 @@ def test_products_of_tokens_without_a_scale(tpp, n):
         c = down(c)
         assert (c[1] == 0).all() if flags == tpp.TPP_EPI_RELU else np.isnan(c[1]).all()
         assert np.isfinite(np.delete(c, 1, 0)).all()
+
+
+# ---- activations far from zero ------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gated", [0, 1])
+@pytest.mark.parametrize("features", [320, 5])
+@pytest.mark.parametrize("act", ["relu", "gelu_tanh", "silu"])
+def test_gradients_far_from_zero(tpp, act, gated, features, dtype):
+    """|z'| from 90 to 3e38.  To the right act(z) = z and act' = 1 to far below u (1 - s < exp(-90)); z' rounds
+    once, s once, their product once, products with gh and u once each: 6 u of the magnitude.  To the left both are 0
+    to within 90 exp(-90) < 1e-37."""
+    rng = np.random.default_rng(features)
+    tops = [90.0, 1e3, 1e6, 1e10, 1e18, 1e19, 1e20, 1e27, 1e30, 1e33, 1e36, 1e38, 3e38]
+    T = len(tops)
+    q = rng.choice(np.r_[-127, np.arange(-127, -99), np.arange(100, 128), 127], (T, features)).astype(np.int8)
+    scale = np.float32(tops)[:, None] / np.float32(100)   # |z'| >= top
+    scale = np.minimum(scale, np.float32(3e38) / 127)
+    q[:, 0], q[:, 1] = -127, 127
+    gh = draw(rng, T, features, features, dtype)
+    if dtype == "f32":
+        gh = np.clip(gh, -1, 1)        # (gh act stays finite)
+    else:
+        gh = draw(rng, T, features, features, dtype, std=0.03)
+    a = q.astype(np.float64) * scale
+    if gated:
+        # the second half: one group of its own, of values about 1
+        group = 0 if features == 5 else 64
+        u8 = rng.integers(1, 128, (T, features)).astype(np.int8)
+        if group:
+            s_u = np.full((T, features // group), np.float32(1 / 64))
+            qq, ss = np.concatenate([q, u8], 1), np.concatenate([np.repeat(scale, features // group, 1), s_u], 1)
+            u = u8 / 64.0
+        else:                          # one scale for the row: u is as large as a; keep it to the tops that fit
+            qq, ss = np.concatenate([q, np.ones_like(u8)], 1), scale
+            u = np.ones_like(a) * scale
+    else:
+        group, qq, ss, u = 0, q, scale, 1.0
+    dz, h2, _ = act_backward(tpp, qq, ss, group, gh, act, gated, dtype)
+    g = values(gh, dtype)[:, :features]
+    right = a > 0
+    big = np.float64(np.finfo(np.float32).max) * (1 - 2.0 ** -6)
+
+    def check(got, ref, what):
+        ref = np.broadcast_to(ref, got.shape)
+        fits = right & (np.abs(ref) < big)
+        half = 2.0 ** -8 if dtype == "bf16" else U
+        off = np.abs(got - ref)[fits]
+        assert (off <= (6 * U + half) * np.abs(ref[fits]) + 1e-37).all(), what
+        return got[~right]
+
+    factor = np.abs(np.broadcast_to(u, a.shape))[~right]
+    gm = np.abs(g)[~right]
+    left = check(h2, a * u, "h2")
+    assert (np.abs(left) <= 1e-37 * factor).all(), f"h2 left of zero: {np.abs(left).max()}"
+    left = check(dz[:, :features], g * u, "dz")
+    assert (np.abs(left) <= 1e-37 * (1 + gm * factor)).all(), f"dz left of zero: {np.abs(left).max()}"
+    if gated:
+        left = check(dz[:, features:], g * a, "dz of the factor")
+        assert (np.abs(left) <= 1e-37 * gm).all(), f"dz of the factor left of zero: {np.abs(left).max()}"
