@@ -70,8 +70,9 @@ tpp_status tpp_residual_norm(const tpp_residual_desc* desc, int64_t tokens, cons
  *     dgate = G'(g) * sum over the gate's tokens of scale * dx * N_after(b)
  * and those of the norms' vectors (`features` fp32 each, overwritten), summed over all tokens.  dx goes
  * on unrounded.  Every output may be NULL where it is not wanted.  dgate has the gate's type and rows,
- * lddg apart, each written once.  Outputs must not overlap inputs (dx being gr or gy, db being b, r, gr
- * or gy are refused).  tokens == 0 gives zero vectors, and a zero dgate where gate_every is 0.
+ * lddg apart, each written once.  Outputs must not overlap inputs or each other (dx or db being b, r, gr
+ * or gy, and two outputs being one, are refused).  tokens == 0 gives zero vectors, and a zero dgate where
+ * gate_every is 0.
  * The vectors' partial sums (and for rows of more than 8192 features 24 bytes a token) go to a work
  * buffer as tpp_reduce's do, under stream capture to one of the capture's own.
  * Errors: as tpp_residual_norm; NO_MEMORY if there is no work buffer to be had. */

@@ -1411,6 +1411,11 @@ tpp_status tpp_residual_norm_backward(const tpp_residual_desc* desc, int64_t tok
   for (const void* out : {static_cast<const void*>(dx), static_cast<const void*>(db)})
     if (out && (out == b || out == r || out == gr || out == gy))
       return fail(TPP_ERR_INVALID_ARG, "dx or db overlaps an input");
+  const void* outs[] = {dx, db, dgate, dw_after, dc_after, dw_before, dc_before};
+  for (int i = 0; i < 7; ++i)
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j])
+        return fail(TPP_ERR_INVALID_ARG, "two gradients have one place");
   float* work = nullptr;
   std::unique_lock<std::mutex> hold;   // held from the work-buffer lookup to the launch
   const int64_t need = tpp::residual_backward_work_floats(p);

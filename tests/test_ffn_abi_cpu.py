@@ -147,3 +147,13 @@ def test_products_refuse(tpp, which):
             [dict(b=None), dict(sb=None)] if which == "gemm" else [dict(x=None), dict(c=Q)]):
         refused(tpp, INV, lambda: product(tpp, which, **kw))
     product(tpp, which, dict(n=0), a=None, c=None, bias=None)
+
+
+OUTPUTS = ("dx", "db", "dgate", "dwa", "dca", "dwb", "dcb")
+
+
+@pytest.mark.parametrize("first,second", [(a, b) for i, a in enumerate(OUTPUTS) for b in OUTPUTS[i + 1:]], ids=str)
+def test_residual_backward_refuses_one_place_for_two_gradients(tpp, first, second):
+    """Of two gradients stored to one place the call would lose one."""
+    at = {k: 0x100000 * (i + 2) for i, k in enumerate(OUTPUTS)}
+    refused(tpp, "TPP_ERR_INVALID_ARG", lambda: norm_bwd(tpp, **dict(at, **{second: at[first]})))
