@@ -102,8 +102,9 @@ tpp_status tpp_q8_gemm(const tpp_q8_gemm_desc* desc, const int8_t* a, const floa
 
 /* The same of activations x (b_type, entry (p, j) at x + j * ldb + p), each token turned into an 8-bit
  * row first, as tpp_q8_quantize with act NONE and group 0 does it.  The rows go to a work buffer as
- * tpp_reduce's do (k bytes a token), under stream capture to one of the capture's own (up to 16 tokens
- * of 12288 entries in all need none).
+ * tpp_reduce's do (k bytes a token), under stream capture to one of the capture's own.  None is needed, and
+ * there is one launch instead of two, where n <= 16, n * (k rounded up to a multiple of 128) <= 12288, and a
+ * and lda are multiples of 16 bytes with lda <= 8388607.
  * Errors: as tpp_q8_gemm; NO_MEMORY if there is no work buffer to be had. */
 tpp_status tpp_q8_linear(const tpp_q8_gemm_desc* desc, const int8_t* a, const float* a_scale,
                          const void* x, void* c, const float* bias, void* stream);
