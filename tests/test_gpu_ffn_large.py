@@ -1,5 +1,6 @@
 """The feed-forward operators at the sizes that training and serving have: products whose k refills every
-place in LDS several times, in each tile and each few-token form.
+place in LDS several times, in each tile and each few-token form; rows past each size from which loads and stores
+go past the caches' replacement, and columns of tokens that go round their loop often.
 
 The bounds are those of test_gpu_q8, whose cases stay below all of that."""
 from __future__ import annotations
@@ -81,3 +82,41 @@ def test_layers_of_wide_inputs(tpp, n, k):
     total = q.astype(np.float64) @ p.a[:, :k].astype(np.float64).T
     close(down(c), *p.finish(total, s[:, 0]), "c")
     close(down(apart), *p.finish(total, s[:, 0]), "c of rows made apart")
+
+
+# ---- 8-bit rows ---------------------------------------------------------------------------------------
+# tokens, features, group, dtype, act, gated, extra ld, first entry
+ROWS = [
+    (1500, 2048, 128, "bf16", "gelu_tanh", 0, 0, 0),    # outputs above 8 MB
+    (1700, 1001, 64, "f32", "silu", 0, 1, 1),
+    (1500, 1001, 64, "f32", "silu", 1, 1, 0),           # halves that lie otherwise
+    (1500, 1024, 64, "bf16", "silu", 1, 0, 0),          # both halves together
+    (6600, 4096, 128, "bf16", "gelu_tanh", 0, 0, 0),    # all above 128 MB
+    (2450, 4096, 0, "f32", "silu", 1, 0, 0),
+    (2450, 4099, 32, "f32", "gelu_tanh", 1, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", ROWS, ids=str)
+def test_large_act_and_backward(tpp, case):
+    q8.test_act_and_backward(tpp, case)
+
+
+@pytest.mark.parametrize("case", [
+    (28100, 1600, 0, "bf16", "none", 0, 0, 0), (7000, 1000, 64, "f32", "relu", 0, 0, 0),
+    (30000, 999, 0, "f32", "none", 0, 1, 0), (6000, 8192, 64, "bf16", "relu", 0, 0, 0)], ids=str)
+def test_large_quantize(tpp, case):
+    """Rows of values as they are: exact."""
+    T, F, group, dtype, act, _, pad, _ = case
+    rng = np.random.default_rng(T)
+    z = np.tile(draw(rng, 500, F, F + pad, dtype), (T // 500 + 1, 1))[:T].copy()   # (of which the oracle does 500)
+    c = q8.Rows((3, F, group, dtype, act, 0, pad, 0))
+    q, s = torch.full((T, F + 5), 77, dtype=torch.int8, device="cuda"), torch.full((T, c.groups(F) + 1), 55.0, device="cuda")
+    tpp.tpp_q8_quantize(c.desc(tpp), T, up(z), F + pad, q, F + 5, s, s.shape[1], tpp.current_stream())
+    v = values(z[:500], dtype)[:, :F]
+    want, scale = oracle.q8_rows(np.where(v > 0, v, 0) if act == "relu" else v, group)
+    q, s = down(q), down(s)
+    for t in range(0, T, 500):
+        n = min(500, T - t)
+        assert np.array_equal(q[t:t + n, :F], want[:n]) and np.array_equal(s[t:t + n, :-1], scale[:n])
+    assert (q[:, F:] == 77).all() and (s[:, -1] == 55.0).all()
