@@ -1,8 +1,8 @@
 """The feed-forward operators at the sizes that training and serving have: products whose k refills every
 place in LDS several times, in each tile and each few-token form; rows past each size from which loads and stores
-go past the caches' replacement, and columns of tokens that go round their loop often.
+go past the caches' replacement; row teams and columns of tokens that go round their loops often.
 
-The bounds are those of test_gpu_q8, whose cases stay below all of that."""
+The bounds are those of test_gpu_q8 and test_gpu_residual, whose cases stay below all of that."""
 from __future__ import annotations
 
 import numpy as np
@@ -11,6 +11,7 @@ import torch
 
 import oracle
 import test_gpu_q8 as q8
+import test_gpu_residual as res
 from ffn_common import blank, close, down, draw, untouched, up
 from helpers import values
 
@@ -120,3 +121,41 @@ def test_large_quantize(tpp, case):
         n = min(500, T - t)
         assert np.array_equal(q[t:t + n, :F], want[:n]) and np.array_equal(s[t:t + n, :-1], scale[:n])
     assert (q[:, F:] == 77).all() and (s[:, -1] == 55.0).all()
+
+
+# ---- norms ----------------------------------------------------------------------------------------------
+# tokens, features, after, before, gate, gate_every, dtype, gate type, extra ld, first entry
+NORMS = [
+    (9001, 500, "layer", "layer", "tanh", 7, "bf16", "bf16", 4, 0),       # a wavefront to a row
+    (9001, 504, "rms", "rms", "identity", 0, "bf16", "f32", 0, 0),
+    (6000, 1024, "rms", "layer", "identity", 1000, "bf16", "bf16", 0, 0),  # two
+    (3000, 2047, "layer", "rms", "sigmoid", 700, "f32", "bf16", 0, 1),     # four
+    (1100, 4096, "rms", "rms", "identity", 0, "bf16", "f32", 0, 0),        # eight
+    (1100, 4095, "layer", "layer", "tanh", 100, "f32", "f32", 1, 0),
+    (1100, 5000, "layer", "rms", "identity", 0, "f32", "f32", 0, 0),       # eight, two chunks to a lane
+    (1100, 8192, "rms", "rms", "none", 0, "bf16", "f32", 0, 0),
+    (900, 9000, "rms", "layer", "identity", 256, "bf16", "bf16", 0, 0),    # sums by a kernel of their own
+    (520, 16384, "rms", "rms", "tanh", 130, "f32", "f32", 0, 0),
+    (5500, 2048, "layer", "rms", "sigmoid", 0, "f32", "bf16", 0, 0),       # all above 256 MB
+    (5500, 4096, "rms", "rms", "identity", 0, "bf16", "f32", 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", NORMS, ids=str)
+def test_large_norms(tpp, case):
+    c = res.Case(case)
+    r, y, q, qs = res.forward(tpp, c)
+    res.check_forward(c, r, y, q, qs)
+    r2, y2, _, _ = res.forward(tpp, c, in_place=True, q=False)
+    assert np.array_equal(r2[:, :c.F], r[:, :c.F]) and np.array_equal(y2[:, :c.F], y[:, :c.F])
+
+
+@pytest.mark.parametrize("case", NORMS, ids=str)
+def test_large_norms_backward(tpp, case):
+    c = res.Case(case, 1)
+    r = draw(np.random.default_rng(5), c.T, c.F, c.ld, c.dtype, 1.5, 0.2)
+    got = res.backward(tpp, c, r)
+    res.check_backward(c, r, got)
+    again = res.backward(tpp, c, r, want={"dx", "dw_after", "dgate"})
+    for k in ("dx", "dw_after", "dgate"):
+        assert got[k] is None or np.array_equal(got[k], again[k], equal_nan=True), k
