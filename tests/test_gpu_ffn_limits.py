@@ -1,5 +1,5 @@
 """The feed-forward operators at the ends of what they take: groups without a scale behind every
-activation, activations far from zero.
+activation, activations far from zero, norms of rows far below 1.
 
 Bounds (u = 2^-24) beside each test; a bf16 output adds half a unit of its own."""
 from __future__ import annotations
@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 import torch
 
-from ffn_common import U, blank, code, down, draw, untouched, up
+from ffn_common import U, blank, close, code, down, draw, untouched, up
 from helpers import values
 from test_gpu_q8 import act_code
 
@@ -165,3 +165,38 @@ def test_gradients_far_from_zero(tpp, act, gated, features, dtype):
     if gated:
         left = check(dz[:, features:], g * a, "dz of the factor")
         assert (np.abs(left) <= 1e-37 * gm).all(), f"dz of the factor left of zero: {np.abs(left).max()}"
+
+
+# ---- norms of rows far below 1 -----------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("features", [5, 600, 1001, 6000, 20001])
+@pytest.mark.parametrize("after,before", [("rms", "none"), ("none", "rms"), ("layer", "rms"), ("none", "layer")])
+@pytest.mark.parametrize("k", [-40, -56])
+def test_norms_of_small_rows(tpp, monkeypatch, k, after, before, features, dtype):
+    """Rows of 2^k with eps = 0 and nothing beside them in the stream: the norms do not see the factor, down to mean
+    squares below 2^-100.  Bounds: those of test_gpu_residual with eps = 0."""
+    import test_gpu_residual as res
+    monkeypatch.setattr(res, "EPS", 0.0)
+    c = res.Case((2, features, after, before, "none", 0, dtype, "f32", 0, 0), 7, mean=0.0)
+    small = np.float32(2.0 ** k)
+    tiny = lambda a: a * small if dtype == "f32" else _bits(values(a, "bf16") * float(small))
+    c.b = tiny(c.b)
+    c.x = np.zeros_like(c.x)
+    r, y, q, qs = res.forward(tpp, c)
+    res.check_forward(c, r, y, q, qs)
+    if after == "none":   # (the bound there is that of values about 1; r = scale b: scale's rounding and the product's)
+        close(r, c.scale * values(c.b, dtype), 2 * U * np.abs(values(c.b, dtype)), "r")
+    assert np.isfinite(values(r, dtype)[:, :features]).all() and (y is None or np.isfinite(values(y, dtype)[:, :features]).all())
+    # backward: the small row is the one that is normed
+    if after != "none" and before != "none":
+        return
+    r = draw(np.random.default_rng(9), 2, features, features, dtype)
+    if before != "none":
+        r = tiny(r)
+    got = res.backward(tpp, c, r)
+    res.check_backward(c, r, got)
+
+
+def _bits(v):
+    import workloads as wk
+    return wk.bf16_bits(v.astype(np.float32)).reshape(v.shape)
