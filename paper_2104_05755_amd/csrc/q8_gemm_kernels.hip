@@ -112,8 +112,8 @@ __device__ __forceinline__ void zero(i32x4_t (&acc)[TM][TN]) {
 }
 
 // ---- rows at any byte -----------------------------------------------------------------------------
-// Fragments straight from memory: bound by the look-ups of 16 rows for every 16 lanes.  Against rows at multiples of
-// 16 bytes, 8192 tokens of 4096 -> 16384 7321 us and 479, 8192 of 1024 -> 4096 509 and 42, 48 of 4096 -> 16384 61
+// Fragments straight from memory, 16 bytes at any address of 16 rows to every 16 lanes.  Against rows at multiples
+// of 16 bytes, 8192 tokens of 4096 -> 16384 7321 us and 479, 8192 of 1024 -> 4096 509 and 42, 48 of 4096 -> 16384 61
 // and 15, one of 1024 -> 4096 14 and 4.
 constexpr int AT = 4, AW = 4;   // 16-row tiles each way, wavefronts
 __global__ __launch_bounds__(64 * AW) void q8_gemm_any_kernel(Q8GemmParams p) {
@@ -324,7 +324,7 @@ __device__ __forceinline__ void tile_of(const TileGrid& g, int32_t& tm, int32_t&
 }
 
 template <int BM, int BN, int WM, int WN, int SLOTS, bool TAIL>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 2 : 2) void q8_gemm_tile_kernel(Q8GemmParams p, TileGrid grid) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void q8_gemm_tile_kernel(Q8GemmParams p, TileGrid grid) {
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
   constexpr int A_BYTES = BM * STAGE, SLOT = A_BYTES + BN * STAGE;
   constexpr int A_LOADS = A_BYTES / 1024 / NW, B_LOADS = BN * STAGE / 1024 / NW, LOADS = A_LOADS + B_LOADS;

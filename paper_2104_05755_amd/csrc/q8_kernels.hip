@@ -298,10 +298,6 @@ __global__ __launch_bounds__(QT) void q8_backward_kernel(Q8Params p, int64_t tak
 }
 
 // ---- launches -------------------------------------------------------------------------------------
-constexpr int64_t MB = int64_t(1) << 20;
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
-
 // The backward pass' parts of dbias: `take` tokens each; 1024 workgroups, at least 8 tokens each.
 struct BackPlan {
   int64_t take, parts;
@@ -313,14 +309,6 @@ struct BackPlan {
   }
 };
 
-template <typename F>
-void by_type(const Q8Params& p, const F& f) {
-  const std::true_type yes;
-  const std::false_type no;
-  const bool whole = p.f % 8 == 0;
-  if (p.bf16) whole ? f(yes, yes) : f(yes, no);
-  else whole ? f(no, yes) : f(no, no);
-}
 // How `in` and `out` bytes go through the caches: outputs beyond the L2s' reach past their replacement, and
 // where all is more than half of the last-level cache inputs too (a GELU kept and its backward pass, 4096
 // features bf16: 1024 tokens 21.4 us, 19.2 and 20.3; 4096 tokens 54.9, 44.2 and 49.5; 8192 tokens 95.3, 88.1
@@ -347,7 +335,7 @@ constexpr int32_t MOST_ROW = 32768;   // entries of a row in registers
 
 template <int KIND>
 void launch_rows(const Q8Params& p, int64_t in, int64_t out, hipStream_t stream) {
-  by_type(p, [&](auto bf16, auto whole) {
+  by_type(p.bf16, p.f, [&](auto bf16, auto whole) {
     const auto by_kind = [&](const auto& f) {   // (8-bit rows for a product are read next: kept)
       if constexpr (KIND == QUANTIZE) in + out > 128 * MB ? f(IntC<STREAM>()) : f(IntC<CACHED>());
       else if constexpr (KIND == SPLIT) out > 8 * MB ? f(IntC<STREAM_OUT>()) : f(IntC<CACHED>());
@@ -406,7 +394,7 @@ hipError_t launch_q8_act_backward(const Q8Params& p, float* work, hipStream_t st
   const int64_t es = p.bf16 ? 2 : 4, wide = (int64_t)p.f << p.gated;
   if (p.f >= 8) {
     const dim3 grid((uint32_t)ceil_div(p.f, 512), (uint32_t)b.parts);
-    by_type(p, [&](auto bf16, auto whole) {
+    by_type(p.bf16, p.f, [&](auto bf16, auto whole) {
       by_how(p.tokens * (p.f * es + wide), p.tokens * (p.f + wide) * es, [&](auto how) {
         const auto launch = [&](auto gated) {
           hipLaunchKernelGGL((q8_backward_kernel<decltype(bf16)::value, decltype(whole)::value, decltype(how)::value,

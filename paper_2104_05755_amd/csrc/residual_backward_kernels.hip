@@ -638,7 +638,7 @@ hipError_t launch_residual_backward(const ResidualParams& p, float* work, hipStr
       rows = cut_tokens(p, min64(p.tokens, 1 << 20));
       groups = rows.parts;
     }
-    by_type(p, [&](auto bf16, auto whole) {
+    by_type(p.bf16, p.f, [&](auto bf16, auto whole) {
       by_how(how, [&](auto h) {
         back_by_width(p, [&](auto w, auto cc, auto sums) {
           constexpr int W = decltype(w)::value, C = decltype(cc)::value;
@@ -664,7 +664,7 @@ hipError_t launch_residual_backward(const ResidualParams& p, float* work, hipStr
   if (!wanted) return hipGetLastError();
   if (b.rows && !b.sums) {
     const dim3 columns((uint32_t)ceil_div(p.f, 8 * RT), (uint32_t)b.groups);
-    by_type(p, [&](auto bf16, auto whole) {
+    by_type(p.bf16, p.f, [&](auto bf16, auto whole) {
       by_means([&](auto m) {
         hipLaunchKernelGGL((residual_columns_kernel<decltype(bf16)::value, decltype(whole)::value, decltype(m)::value>),
                            columns, dim3(RT), 0, stream, p, c, stats, part, gate_part);

@@ -1,10 +1,8 @@
 // residual_device.h -- what the forward and the backward kernels of the residual stream's norms share: gates,
-// statistics of a row, and the choice of an instance.
+// statistics of a row, and the widest row in registers.
 #pragma once
 
 #include <hip/hip_runtime.h>
-
-#include <type_traits>
 
 #include "internal.h"
 #include "rows_device.h"
@@ -80,19 +78,7 @@ __device__ __forceinline__ float squares_of(const float (&v)[C][8]) {
   return s;
 }
 
-// ---- launches -------------------------------------------------------------------------------------
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
-template <typename F>
-void by_type(const ResidualParams& p, const F& f) {
-  const std::true_type yes;
-  const std::false_type no;
-  const bool whole = p.f % 8 == 0;
-  if (p.bf16) whole ? f(yes, yes) : f(yes, no);
-  else whole ? f(no, yes) : f(no, no);
-}
 constexpr int32_t MOST_ROW = 16384;       // entries of a row in registers
-constexpr int64_t MB = int64_t(1) << 20;
 
 }  // namespace rows
 }  // namespace tpp

@@ -184,7 +184,7 @@ hipError_t launch_residual(const ResidualParams& p, hipStream_t stream) {
     // Beyond the L2s' reach what is moved once goes past the caches' replacement, in and out: 1024 tokens of
     // 4096 bf16 (two outputs of 8 MB) 7.4 us against 10.1, 8192 55.5 against 61.0 (outputs alone: 8.2, 60.0).
     const bool stream_it = p.tokens * p.f * (p.bf16 ? 2 : 4) * (p.y ? 2 : 1) > 8 * MB;
-    by_type(p, [&](auto bf16, auto whole) {
+    by_type(p.bf16, p.f, [&](auto bf16, auto whole) {
       by_width(p, [&](auto w, auto c) {
         constexpr int W = decltype(w)::value, C = decltype(c)::value, R = W == 1 ? RW : 1;
         const auto launch = [&](auto how) {

@@ -1,9 +1,11 @@
 // rows_device.h -- device-side pieces shared by the kernels over rows of features (residual_kernels.hip,
-// q8_kernels.hip, q8_gemm_kernels.hip): sums and maxima over lanes and workgroups, activations, and the
-// rounding to 8-bit rows.
+// q8_kernels.hip, q8_gemm_kernels.hip): sums and maxima over lanes and workgroups, activations, the
+// rounding to 8-bit rows, and what their launches choose by.
 #pragma once
 
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "brgemm_device.h"
 #include "internal.h"
@@ -360,6 +362,20 @@ __device__ __forceinline__ void store_q8(int8_t* row, const Place& c, const floa
     for (int e = 1; e < 8; ++e)
       if (e >= c.skip) gst<uint8_t>(row + c.at + e, (uint8_t)(w[e / 4] >> (8 * (e % 4))));
   }
+}
+
+// ---- launches -------------------------------------------------------------------------------------
+constexpr int64_t MB = int64_t(1) << 20;
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
+// f(bf16, whether rows of `width` entries are whole chunks).
+template <typename F>
+void by_type(bool bf16, int32_t width, const F& f) {
+  const std::true_type yes;
+  const std::false_type no;
+  const bool whole = width % 8 == 0;
+  if (bf16) whole ? f(yes, yes) : f(yes, no);
+  else whole ? f(no, yes) : f(no, no);
 }
 
 }  // namespace rows
