@@ -9,8 +9,9 @@
 // one partial row each, which a second kernel adds in order (no atomics: the bits do not vary between runs).
 //
 // 8192 tokens of 4096 bf16: 86 to 89 us, 4.5 to 4.7 TB/s, 4.7 of them the fold (a copy of as much: 78 us).  1533 of 1001
-// fp32, layer norms and a gate for every 100 tokens: 24 us, where a copy takes 7.2: the kernel, 17 us, is two
-// turns of a loop in which rows and three exchanges wait for each other, the fold 7.  From a workgroup to a row
+// fp32, layer norms and a gate for every 100 tokens: 24 us, where a copy takes 7.2: a row of parts for every two
+// tokens is 16 MB beside the 37 that must move; the kernel, 17 us, waits half of the time in two turns of a loop
+// with three exchanges, the fold, 7, fetches 32 MB (its columns of rows of 1001 share lines).  From a workgroup to a row
 // and a second reading for the sums: 707 and 40 us.  One chunk of 8 entries to a lane carried best (85 us
 // against 92 with two, and 35 against 49), as did 2048 wavefronts (4096: 92 us against 84, 1024: 103 against 86); a second token's
 // rows under way gained little and cost elsewhere (84.0 against 85.2, but 31 against 29).
